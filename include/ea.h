@@ -440,6 +440,142 @@ int ea_exprog_preamble(int32_t rank, const int32_t* prod_nblocks, const int64_t*
    (bad arguments, or an invalid program), EA_ERR_SPEC (syntax). */
 int ea_exprog_simulate(const char* text, double link_gbs, double hbm_gbs, double* seconds);
 
+/* ---- head rows of a QKV activation -------------------------------------
+   Between the QKV product and attention (repartition's place in the block):
+   every query and key head row u is normed, rotated by its position and
+   written where attention reads it, value rows are moved along, in one pass.
+     n = w * u / sqrt(mean(u^2) + eps)                   (w NULL: n = u)
+     (n_i, n_j) -> (n_i cos a - n_j sin a, n_j cos a + n_i sin a),
+     a = position * inv_freq[f]: pairs (f, f + rotary/2), or, interleaved,
+     (2f, 2f + 1), of the row's first `rotary` elements; the others stay.
+   Angles are taken in 64 bits, arithmetic is f32, rounded once.  f32, bf16,
+   f16; d_head a multiple of 8 from 8 to 512. */
+typedef struct ea_heads_params {
+  int32_t d_head;
+  float eps;                /* of the norms                                      */
+  int32_t rotary;           /* rotated elements of a head: even, 0 .. d_head     */
+  int32_t interleaved;      /* 0: pairs (f, f + rotary/2), 1: (2f, 2f + 1)       */
+  const float* inv_freq;    /* device, rotary/2 frequencies (NULL if rotary 0)   */
+  const int32_t* positions; /* device, one a row; NULL: the row's index          */
+  const int32_t* slots;     /* device, one a row, or NULL.  Given: k and v are
+                               pages of a cache, and a row's keys and values go
+                               to page slot / page_size, row slot % page_size; a
+                               slot outside the cache (-1: padding) stores none.
+                               A slot given twice holds either row.            */
+} ea_heads_params;
+/* qkv: [T, (Hq + 2 Hkv) d], columns [Q heads | K heads | V heads].  q: rank 2
+   [T, Hq d], or rank 3 or 4 [.., Hq, T, d] (leading extent 1): token-major or
+   head-major.  k, v: the same forms with Hkv heads, or with slots the pages
+   [pages, Hkv, page_size, d], one block a page.  Partitions: equal blocks (the
+   last may be shorter), columns at multiples of d, d never split
+   (EA_ERR_UNSUPPORTED otherwise).  wq, wk: norm weights [d], both or neither,
+   of any dtype.  All others of one dtype; memory must not overlap.
+   Asynchronous on `stream`: no plan, no workspace, never allocates.
+   Errors: EA_ERR_ARG, EA_ERR_DTYPE, EA_ERR_UNSUPPORTED, EA_ERR_HIP. */
+int ea_heads(const ea_relation* qkv, const ea_relation* wq, const ea_relation* wk, ea_relation* q, ea_relation* k,
+             ea_relation* v, const ea_heads_params* params, void* stream);
+/* Its gradient: from dq, dk, dv (forms as q, k, v; slots must be NULL) the
+   gradient dqkv (dqkv's shape and partition are qkv's) and, where norm weights
+   are given and dwq / dwk are not NULL, theirs ([d], of any dtype), summed over
+   rows and heads in f32 in a fixed order.  workspace: 256-byte aligned, of
+   ea_heads_backward_workspace's size where a weight's gradient is asked for;
+   its contents need no initial value, its counter area stays untouched. */
+int ea_heads_backward_workspace(int32_t d_head, int64_t* ws_bytes);
+int ea_heads_backward(const ea_relation* qkv, const ea_relation* wq, const ea_relation* wk, const ea_relation* dq,
+                      const ea_relation* dk, const ea_relation* dv, ea_relation* dqkv, ea_relation* dwq,
+                      ea_relation* dwk, const ea_heads_params* params, void* workspace, int64_t ws_bytes,
+                      void* stream);
+
+/* ---- attention over a paged cache ----------------------------------------
+   A cache is a relation [pages, Hkv, page_size, d] with one block a page (K and
+   V each); a sequence's keys are listed by its row of a page table: key j is
+   row j % page_size of page table[s][j / page_size].  Query row i of a
+   sequence's n_q newest tokens sees keys j < length - n_q + i + 1 (all of them
+   for the last); a row that sees none gets zeros.  Query head h reads
+   key-value head h / (Hq / Hkv).
+   Shared prefixes: group g is sequences group_start[g] .. group_start[g+1)-1,
+   whose first group_shared[g] keys lie in the same pages; those are read once
+   for the whole group, through its first sequence's table row, and joined with
+   each sequence's own keys by the online-softmax aggregation.  Sequences
+   before the first group or behind the last share nothing.
+   Lengths, tables and groups are device arrays read when the kernels run, so a
+   captured call follows them.  Lengths are taken as at most a table row's
+   keys; a key whose page lies outside the cache is invisible.  Rows behind the
+   last sequence's stay as they were.  Keys and values that a row does not see
+   must be finite where the same call sees them in another row. */
+#define EA_PAGED_MAX_SEQ 4096
+typedef struct ea_paged {
+  float scale;                 /* of the scores: positive, finite                  */
+  int32_t n_seq;
+  const int32_t* q_start;      /* [n_seq + 1] ascending first query rows; NULL: one
+                                  row a sequence                                   */
+  const int32_t* lengths;      /* [n_seq] keys                                     */
+  const int32_t* table;        /* [n_seq][stride] pages                            */
+  int32_t stride;
+  int32_t n_group;             /* 0: nothing is shared                             */
+  const int32_t* group_start;  /* [n_group + 1] ascending                          */
+  const int32_t* group_shared; /* [n_group] keys                                   */
+} ea_paged;
+/* q, out: [rows, Hq d] or [.., Hq, rows, d] (forms as ea_heads' q).  bf16 or
+   f16, d 64 or 128; scores and sums in f32, weights rounded to the dtype for
+   the product with V.  n_seq + n_group <= EA_PAGED_MAX_SEQ, rows * Hq < 2^31.
+   workspace: as ea_joinagg's, of at least ea_attention_paged_workspace's bytes
+   for these operands (its counter area stays untouched); asynchronous, never
+   allocates, deterministic.  Errors: EA_ERR_ARG, EA_ERR_DTYPE,
+   EA_ERR_UNSUPPORTED, EA_ERR_CAPACITY, EA_ERR_HIP. */
+int ea_attention_paged_workspace(const ea_relation* q, const ea_relation* k, const ea_paged* batch, int64_t* ws_bytes);
+int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_relation* v, ea_relation* out,
+                       const ea_paged* batch, void* workspace, int64_t ws_bytes, void* stream);
+
+/* ---- the page table of a cache --------------------------------------------
+   State, in device int32 arrays: table[n_seq][stride], lengths[n_seq] and
+   refs[n_pages], how many table entries name a page (0: free).  Whole pages may
+   be shared; a partly filled last page has one owner.  Pages are handed out
+   lowest first, so results are the same on every run.  status[0] says what
+   became of a call: EA_PAGES_OK, or a reason for which nothing was done and
+   the outputs hold the state as it came; status[1] is the number of free pages
+   afterwards.  Entries behind a sequence's pages are not read, and are -1 in
+   rewritten tables; an entry outside the cache counts no page.  n_seq <=
+   EA_PAGED_MAX_SEQ; n_seq * stride, n_pages * page_size and (stride + 1) *
+   page_size < 2^31.  Asynchronous, no allocation, no plan. */
+#define EA_PAGES_OK 0
+#define EA_PAGES_NONE_FREE 1 /* fewer free pages than the call needs            */
+#define EA_PAGES_TOO_LONG 2  /* a length below 0 or above a table row's keys    */
+typedef struct ea_pages {
+  int32_t n_seq, stride, n_pages, page_size;
+  const int32_t* table;
+  const int32_t* lengths;
+  const int32_t* refs;
+  int32_t* out_table;
+  int32_t* out_lengths;
+  int32_t* out_refs;
+  int32_t* status; /* [2] */
+} ea_pages;
+/* add[s] >= 0 (negative: 0) more keys for every sequence.  out_table is table
+   itself, which gets the new pages; out_lengths and out_refs may be lengths
+   and refs.  slots, positions (NULL: not wanted): for the new tokens, sequence
+   by sequence, their slot (page * page_size + row) and position; entries
+   behind them, up to n_tokens, get -1 and 0. */
+int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, int32_t* positions, int32_t n_tokens,
+                    void* stream);
+/* Sequence i becomes a copy of sequence parent[i] (outside [0, n_seq): empty),
+   which forks, reorders and frees: whole pages are shared, a partly filled last
+   page stays with the parent's first child and its rows are copied to a new
+   page for the others, in every plane of the caches ([pages, Hkv, page_size, d]
+   or [planes, pages, Hkv, page_size, d], one block a page of a plane; at most
+   EA_MAX_INPUTS).  Pages freed by the call serve its copies.  out_ arrays must
+   not overlap the others. */
+int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages* state, const int32_t* parent,
+                    void* workspace, int64_t ws_bytes, void* stream);
+/* Moves the used pages to the first places: the k-th lowest used page behind
+   the first n_used goes to the k-th lowest free one before.  Lengths stay
+   (out_lengths is not written); out_table and out_refs may be table and refs. */
+int ea_pages_compact(int32_t n_cache, ea_relation* const* caches, const ea_pages* state, void* workspace,
+                     int64_t ws_bytes, void* stream);
+/* Workspace of select and compact: 256-byte aligned, behind its counter area
+   (which stays untouched) no initial value is needed. */
+int ea_pages_workspace(int32_t n_seq, int32_t n_pages, int64_t* ws_bytes);
+
 /* ---- plan cache --------------------------------------------------------- */
 /* Number of cached plans (all devices). */
 int64_t ea_plan_cache_size(void);

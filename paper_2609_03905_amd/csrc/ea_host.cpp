@@ -26,20 +26,6 @@
 
 using namespace ea;
 
-struct ea_relation {
-  int32_t rank = 0;
-  int32_t dtype = 0;
-  int64_t shape[kMaxRank] = {};
-  int32_t nb[kMaxRank] = {};
-  std::vector<int64_t> splits[kMaxRank];
-  std::vector<int64_t> off;  // byte offset of every block
-  int64_t nblocks = 0;
-  int64_t nbytes = 0;
-  uint64_t layout = 0;  // equal for relations of one dtype, shape and partition, distinct otherwise
-  void* data = nullptr;
-  int64_t capacity = 0;
-};
-
 // ---------------------------------------------------------------------------
 // errors (shared with the other host sources through ea_internal.h)
 // ---------------------------------------------------------------------------
@@ -62,15 +48,7 @@ int ok() {
 }
 }  // namespace ea
 
-namespace {
-
-#define EA_HIP_TRY(expr)                                                              \
-  do {                                                                                \
-    hipError_t e_ = (expr);                                                           \
-    if (e_ != hipSuccess)                                                             \
-      return fail(EA_ERR_HIP, "%s failed: %s", #expr, hipGetErrorString(e_));         \
-  } while (0)
-
+namespace ea {
 int dtype_size(int32_t dt) {
   switch (dt) {
     case EA_F32: return 4;
@@ -81,6 +59,15 @@ int dtype_size(int32_t dt) {
 }
 
 int64_t align256(int64_t x) { return (x + 255) / 256 * 256; }
+
+int check_rel(const ea_relation* r, const char* what, bool need_data) {
+  if (!r) return fail(EA_ERR_ARG, "NULL %s relation", what);
+  if (need_data && !r->data) return fail(EA_ERR_ARG, "%s relation has no data", what);
+  return EA_OK;
+}
+}  // namespace ea
+
+namespace {
 
 // ---------------------------------------------------------------------------
 // partitions and layout
@@ -2057,12 +2044,6 @@ int get_joinagg_plan(const char* spec_str, const Spec& sp, int32_t join_op, int3
                 (long long)p->ws_counters, (long long)(kWsCounterBytes / (int64_t)sizeof(int32_t)));
   *out = p.get();
   cache()[key] = std::move(p);
-  return EA_OK;
-}
-
-int check_rel(const ea_relation* r, const char* what, bool need_data) {
-  if (!r) return fail(EA_ERR_ARG, "NULL %s relation", what);
-  if (need_data && !r->data) return fail(EA_ERR_ARG, "%s relation has no data", what);
   return EA_OK;
 }
 

@@ -11,12 +11,31 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <vector>
 
 #include "ea.h"
 
 namespace ea {
-
 constexpr int kMaxRank = EA_MAX_RANK;
+}
+
+// A relation handle: host metadata over caller-owned device memory.
+struct ea_relation {
+  int32_t rank = 0;
+  int32_t dtype = 0;
+  int64_t shape[ea::kMaxRank] = {};
+  int32_t nb[ea::kMaxRank] = {};
+  std::vector<int64_t> splits[ea::kMaxRank];
+  std::vector<int64_t> off;  // byte offset of every block
+  int64_t nblocks = 0;
+  int64_t nbytes = 0;
+  uint64_t layout = 0;  // equal for relations of one dtype, shape and partition, distinct otherwise
+  void* data = nullptr;
+  int64_t capacity = 0;
+};
+
+namespace ea {
+
 constexpr int kMaxIn = EA_MAX_INPUTS;
 constexpr int kMaxOps = EA_MAX_INPUTS + 1;  // inputs, then the output
 constexpr int kMaxLetters = 16;
@@ -46,6 +65,16 @@ struct DevBlk {
 // einsum spec parser.
 int fail(int code, const char* fmt, ...);
 int ok();
+int dtype_size(int32_t dt);
+int64_t align256(int64_t x);
+int check_rel(const ea_relation* r, const char* what, bool need_data);
+
+#define EA_HIP_TRY(expr)                                                              \
+  do {                                                                                \
+    hipError_t e_ = (expr);                                                           \
+    if (e_ != hipSuccess)                                                             \
+      return ::ea::fail(EA_ERR_HIP, "%s failed: %s", #expr, hipGetErrorString(e_));   \
+  } while (0)
 
 struct Spec {
   int n_in = 0;

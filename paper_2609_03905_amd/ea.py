@@ -44,6 +44,25 @@ class _Params(ctypes.Structure):
                 ("n_seq", ctypes.c_int32), ("seq_ends", ctypes.c_void_p)]
 
 
+class _HeadsParams(ctypes.Structure):
+    _fields_ = [("d_head", ctypes.c_int32), ("eps", ctypes.c_float), ("rotary", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p)]
+
+
+class _Paged(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("n_seq", ctypes.c_int32), ("q_start", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("stride", ctypes.c_int32),
+                ("n_group", ctypes.c_int32), ("group_start", ctypes.c_void_p), ("group_shared", ctypes.c_void_p)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("stride", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("out_table", ctypes.c_void_p), ("out_lengths", ctypes.c_void_p),
+                ("out_refs", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -82,6 +101,15 @@ def lib() -> ctypes.CDLL:
                                            ctypes.c_char_p, i64, P(i64), P(ctypes.c_double)]
         L.ea_exprog_preamble.argtypes = [i32, P(i32), P(i64), i32, P(i64), P(i32), P(i32), P(i64), i32, P(i64), i32,
                                          i64, ctypes.c_char_p, i64, P(i64)]
+        L.ea_heads.argtypes = [vp] * 6 + [P(_HeadsParams), vp]
+        L.ea_heads_backward_workspace.argtypes = [i32, P(i64)]
+        L.ea_heads_backward.argtypes = [vp] * 9 + [P(_HeadsParams), vp, i64, vp]
+        L.ea_attention_paged_workspace.argtypes = [vp, vp, P(_Paged), P(i64)]
+        L.ea_attention_paged.argtypes = [vp] * 4 + [P(_Paged), vp, i64, vp]
+        L.ea_pages_workspace.argtypes = [i32, i32, P(i64)]
+        L.ea_pages_extend.argtypes = [P(_Pages), vp, vp, vp, i32, vp]
+        L.ea_pages_select.argtypes = [i32, P(vp), P(_Pages), vp, vp, i64, vp]
+        L.ea_pages_compact.argtypes = [i32, P(vp), P(_Pages), vp, i64, vp]
         L.ea_plan_cache_size.restype = i64
         L.ea_plan_cache_clear.restype = ctypes.c_int
         _lib = L
@@ -351,6 +379,208 @@ def join_tuples(spec: str, join_op: int, inputs: Sequence[Relation], out: Relati
                                 ctypes.c_void_p(tuples.data_ptr()), tuples.shape[0], ctypes.c_void_p(goff.data_ptr()),
                                 goff.numel(), ctypes.byref(n_t), ctypes.byref(n_g), _stream(stream)))
     return tuples[:n_t.value], goff
+
+
+# ---- decoding: head rows, attention over a paged cache, the page table -------
+PAGES_OK, PAGES_NONE_FREE, PAGES_TOO_LONG = 0, 1, 2  # status[0] of the page calls (EA_PAGES_*)
+PAGED_MAX_SEQ = 4096  # EA_PAGED_MAX_SEQ
+
+
+def _device_array(t, name: str, shape, dtype=torch.int32, optional: bool = False):
+    """The address of a small device array, checked: type, shape (None: any
+    extent), rows without gaps, on the current device."""
+    if t is None:
+        if optional:
+            return None
+        raise EAError(ERR_ARG, f"{name} is missing")
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise EAError(ERR_ARG, f"{name} is no {dtype} tensor")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise EAError(ERR_ARG, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_contiguous():
+        raise EAError(ERR_ARG, f"{name} is not contiguous")
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise EAError(ERR_ARG, f"{name} is on {t.device}, not on the current GPU")
+    return t.data_ptr()
+
+
+def _on_device(**rels):
+    """Relations whose data torch holds lie on the current device."""
+    for name, r in rels.items():
+        if r is not None and r.data is not None:
+            d = r.data.device
+            if d.type != "cuda" or d.index != torch.cuda.current_device():
+                raise EAError(ERR_ARG, f"{name} is on {d}, not on the current GPU")
+
+
+def _h(r):
+    return None if r is None else r._h
+
+
+def _workspace(need: int, workspace, stream):
+    """Address and size of a call's workspace: the caller's, or the stream's."""
+    if need == 0:
+        return None, 0
+    if workspace is None:
+        workspace = _stream_workspace(need, stream)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _heads_params(rows, d_head, eps, inv_freq, interleaved, positions, slots):
+    freq = _device_array(inv_freq, "inv_freq", (None,), torch.float32, optional=True)
+    return _HeadsParams(int(d_head), float(eps), 2 * inv_freq.numel() if freq else 0, int(interleaved), freq,
+                        _device_array(positions, "positions", (rows,), optional=True),
+                        _device_array(slots, "slots", (rows,), optional=True))
+
+
+def heads(qkv: Relation, q: Relation, k: Relation, v: Relation, *, d_head: int, wq: Relation | None = None,
+          wk: Relation | None = None, eps: float = 0.0, inv_freq: torch.Tensor | None = None,
+          interleaved: bool = False, positions: torch.Tensor | None = None, slots: torch.Tensor | None = None,
+          stream=None) -> None:
+    """The head rows of a QKV activation [T, (Hq + 2 Hkv) d_head] to where
+    attention reads them: queries and keys normed with ``wq`` and ``wk`` (None:
+    not), their first 2 * len(inv_freq) elements rotated by positions[t] *
+    inv_freq (``interleaved``: pairs of neighbours, else of halves; positions
+    None: the row's index), values moved along.  ``q``, ``k``, ``v``:
+    token-major [T, H d_head] or head-major [.., H, T, d_head]; with ``slots``
+    k and v are the pages [pages, Hkv, page_size, d_head] of a cache and row t
+    goes to slot slots[t] (-1: to none)."""
+    _on_device(qkv=qkv, q=q, k=k, v=v, wq=wq, wk=wk)
+    prm = _heads_params(qkv.shape[0], d_head, eps, inv_freq, interleaved, positions, slots)
+    _check(lib().ea_heads(qkv._h, _h(wq), _h(wk), q._h, k._h, v._h, ctypes.byref(prm), _stream(stream)))
+
+
+def heads_backward(qkv: Relation, dq: Relation, dk: Relation, dv: Relation, dqkv: Relation, *, d_head: int,
+                   wq: Relation | None = None, wk: Relation | None = None, dwq: Relation | None = None,
+                   dwk: Relation | None = None, eps: float = 0.0, inv_freq: torch.Tensor | None = None,
+                   interleaved: bool = False, positions: torch.Tensor | None = None, stream=None,
+                   workspace: torch.Tensor | None = None) -> None:
+    """The gradient of ``heads`` (without slots): ``dqkv`` in qkv's layout and,
+    where wanted, the norm weights' ``dwq`` and ``dwk`` ([d_head])."""
+    _on_device(qkv=qkv, dq=dq, dk=dk, dv=dv, dqkv=dqkv, wq=wq, wk=wk, dwq=dwq, dwk=dwk)
+    prm = _heads_params(qkv.shape[0], d_head, eps, inv_freq, interleaved, positions, None)
+    s = _stream(stream)
+    ws, n = None, 0
+    if dwq is not None or dwk is not None:
+        need = ctypes.c_int64()
+        _check(lib().ea_heads_backward_workspace(int(d_head), ctypes.byref(need)))
+        ws, n = _workspace(need.value, workspace, s)
+    _check(lib().ea_heads_backward(qkv._h, _h(wq), _h(wk), dq._h, dk._h, dv._h, dqkv._h, _h(dwq), _h(dwk),
+                                   ctypes.byref(prm), ws, n, s))
+
+
+def _paged(scale, table, lengths, q_start, group_start, group_shared):
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise EAError(ERR_ARG, "table is no [sequences, pages] tensor")
+    n, stride = table.shape
+    if (group_start is None) != (group_shared is None):
+        raise EAError(ERR_ARG, "group_start and group_shared: both or neither")
+    n_group = 0 if group_shared is None else group_shared.numel()
+    return _Paged(float(scale), n, _device_array(q_start, "q_start", (n + 1,), optional=True),
+                  _device_array(lengths, "lengths", (n,)), _device_array(table, "table", (n, stride)), stride, n_group,
+                  _device_array(group_start, "group_start", (n_group + 1,), optional=True),
+                  _device_array(group_shared, "group_shared", (n_group,), optional=True))
+
+
+def attention_paged_workspace(q: Relation, k: Relation, n_seq: int, n_group: int = 0) -> int:
+    """Workspace bytes of attention_paged for these operands and counts."""
+    n = ctypes.c_int64()
+    b = _Paged(1.0, int(n_seq), None, None, None, 1, int(n_group), None, None)
+    _check(lib().ea_attention_paged_workspace(q._h, k._h, ctypes.byref(b), ctypes.byref(n)))
+    return int(n.value)
+
+
+def attention_paged(q: Relation, k: Relation, v: Relation, out: Relation, *, scale: float, table: torch.Tensor,
+                    lengths: torch.Tensor, q_start: torch.Tensor | None = None,
+                    group_start: torch.Tensor | None = None, group_shared: torch.Tensor | None = None, stream=None,
+                    workspace: torch.Tensor | None = None) -> None:
+    """Attention of each sequence's newest tokens over a paged cache: ``k`` and
+    ``v`` [pages, Hkv, page_size, d], one block a page; sequence s has
+    lengths[s] keys in the pages table[s]; its query rows are q_start[s] ..
+    q_start[s + 1] - 1 of ``q`` (None: row s), the last of which sees all keys
+    and each one before it one less.  Groups of sequences group_start[g] ..
+    group_start[g + 1] - 1 share their first group_shared[g] keys, which are
+    read once.  The arrays are read when the kernels run."""
+    _on_device(q=q, k=k, v=v, out=out)
+    b = _paged(scale, table, lengths, q_start, group_start, group_shared)
+    s = _stream(stream)
+    need = ctypes.c_int64()
+    _check(lib().ea_attention_paged_workspace(q._h, k._h, ctypes.byref(b), ctypes.byref(need)))
+    ws, n = _workspace(need.value, workspace, s)
+    _check(lib().ea_attention_paged(q._h, k._h, v._h, out._h, ctypes.byref(b), ws, n, s))
+
+
+def _pages(table, lengths, refs, page_size, out_table, out_lengths, out_refs, status):
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise EAError(ERR_ARG, "table is no [sequences, pages] tensor")
+    if not isinstance(refs, torch.Tensor):
+        raise EAError(ERR_ARG, "refs is no tensor")
+    n, stride = table.shape
+    A = _device_array
+    return _Pages(n, stride, refs.numel(), int(page_size), A(table, "table", (n, stride)),
+                  A(lengths, "lengths", (n,)), A(refs, "refs", (None,)), A(out_table, "out_table", (n, stride)),
+                  A(out_lengths, "out_lengths", (n,), optional=True), A(out_refs, "out_refs", (refs.numel(),)),
+                  A(status, "status", (2,)))
+
+
+def pages_extend(table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, add: torch.Tensor, *, page_size: int,
+                 status: torch.Tensor, out_lengths: torch.Tensor | None = None, out_refs: torch.Tensor | None = None,
+                 slots: torch.Tensor | None = None, positions: torch.Tensor | None = None, stream=None) -> None:
+    """Pages for add[s] more keys of every sequence, lowest free ones first:
+    written into ``table``; ``lengths`` and ``refs`` are updated (in place
+    unless outputs are given).  ``slots`` and ``positions`` receive the new
+    tokens' places, sequence by sequence, -1 and 0 behind them.  status[0]:
+    PAGES_OK or why nothing was done; status[1]: free pages left."""
+    st = _pages(table, lengths, refs, page_size, table, lengths if out_lengths is None else out_lengths,
+                refs if out_refs is None else out_refs, status)
+    ps = _device_array(slots, "slots", (None,), optional=True)
+    pp = _device_array(positions, "positions", (None if slots is None else slots.numel(),), optional=True)
+    n = slots.numel() if ps else positions.numel() if pp else 0
+    _check(lib().ea_pages_extend(ctypes.byref(st), _device_array(add, "add", (table.shape[0],)), ps, pp, n,
+                                 _stream(stream)))
+
+
+def _page_caches(caches):
+    caches = list(caches)
+    _on_device(**{f"cache {i}": c for i, c in enumerate(caches)})
+    return len(caches), _handles(caches), caches[0].shape[-2] if caches else None
+
+
+def _pages_workspace(st, workspace, s):
+    need = ctypes.c_int64()
+    _check(lib().ea_pages_workspace(st.n_seq, st.n_pages, ctypes.byref(need)))
+    return _workspace(need.value, workspace, s)
+
+
+def pages_select(caches: Sequence[Relation], parent: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+                 refs: torch.Tensor, *, out_table: torch.Tensor, out_lengths: torch.Tensor, out_refs: torch.Tensor,
+                 status: torch.Tensor, page_size: int | None = None, stream=None,
+                 workspace: torch.Tensor | None = None) -> None:
+    """Sequence i of the new state is a copy of sequence parent[i] (-1: empty):
+    forks, reorders and frees.  Whole pages are shared; a partly filled last
+    page is copied for all children but the first, in every plane of the caches
+    ([pages, Hkv, page_size, d] or [planes, pages, Hkv, page_size, d]).
+    ``page_size`` is the caches' (needed where there are none)."""
+    n, handles, ps = _page_caches(caches)
+    st = _pages(table, lengths, refs, page_size or ps or 0, out_table, out_lengths, out_refs, status)
+    s = _stream(stream)
+    ws, nbytes = _pages_workspace(st, workspace, s)
+    _check(lib().ea_pages_select(n, handles, ctypes.byref(st), _device_array(parent, "parent", (table.shape[0],)), ws,
+                                 nbytes, s))
+
+
+def pages_compact(caches: Sequence[Relation], table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, *,
+                  status: torch.Tensor, out_table: torch.Tensor | None = None, out_refs: torch.Tensor | None = None,
+                  page_size: int | None = None, stream=None, workspace: torch.Tensor | None = None) -> None:
+    """Move the used pages to the first places of the cache (the k-th lowest
+    one behind them to the k-th lowest hole) and rewrite the table and the
+    counts, in place unless outputs are given."""
+    n, handles, ps = _page_caches(caches)
+    st = _pages(table, lengths, refs, page_size or ps or 0, table if out_table is None else out_table, None,
+                refs if out_refs is None else out_refs, status)
+    s = _stream(stream)
+    ws, nbytes = _pages_workspace(st, workspace, s)
+    _check(lib().ea_pages_compact(n, handles, ctypes.byref(st), ws, nbytes, s))
 
 
 def plan_cache_size() -> int:

@@ -1,0 +1,246 @@
+"""Attention over a paged cache, with and without shared prefixes, against the
+64-bit definition: lengths from none to several chunks, odd pages, ragged
+query rows, tables with pages outside the cache."""
+import numpy as np
+import pytest
+import torch
+
+import decode_ref as R
+from paper_2609_03905_amd import ea
+
+pytestmark = pytest.mark.gpu
+
+
+def _batch(lens, shared, groups, page, hkv, d, dtype, seed, spare=3, garbage=None):
+    """K, V, the page table and host copies: groups is a list of (first, last
+    + 1, keys shared).  Rows no sequence holds are `garbage` if given."""
+    rng = np.random.default_rng(seed)
+    n = len(lens)
+    stride = max(1, max((-(-x // page) for x in lens), default=1)) + 1
+    table = np.full((n, stride), -1, np.int64)
+    own = [-(-x // page) for x in lens]
+    total = sum(own) + spare
+    ids = list(rng.permutation(total))
+    prefix = {}
+    for first, last, keys in groups:
+        prefix[first] = [ids.pop() for _ in range(keys // page)]
+    for s in range(n):
+        g = next((f for f, e, _ in groups if f <= s < e), None)
+        mine = list(prefix.get(g, []))[: own[s]]
+        mine += [ids.pop() for _ in range(own[s] - len(mine))]
+        table[s, :own[s]] = mine
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    k, v = (torch.randn((total, hkv, page, d), generator=gen, device="cuda").to(R.TORCH[dtype]) for _ in range(2))
+    if garbage is not None:
+        seen = np.zeros((total, page), bool)
+        for s in range(n):
+            for j in range(lens[s]):
+                seen[table[s, j // page], j % page] = True
+        dead = torch.from_numpy(~seen).cuda()[:, None, :, None].expand_as(k)
+        k[dead] = garbage
+        v[dead] = garbage
+    return k, v, table
+
+
+def _run(q, k, v, table, lens, q_start, groups, scale, out=None, form="tokens"):
+    t, hq, d = q.shape
+    src = q.reshape(t, hq * d) if form == "tokens" else q.transpose(0, 1).contiguous()
+    out = torch.full_like(src, float("nan")) if out is None else out
+    kw = {}
+    if groups:
+        kw = {"group_start": R.i32([g[0] for g in groups] + [groups[-1][1]]),
+              "group_shared": R.i32([g[2] for g in groups])}
+    ea.attention_paged(R.rel(src), R.pages_rel(k), R.pages_rel(v), R.rel(out), scale=scale, table=R.i32(table),
+                       lengths=R.i32(lens), q_start=None if q_start is None else R.i32(q_start), **kw)
+    return out.view(t, hq, d) if form == "tokens" else out.transpose(0, 1)
+
+
+def _check(q, k, v, table, lens, q_start, groups, page, dtype, scale=None, form="tokens"):
+    t, hq, d = q.shape
+    scale = d ** -0.5 if scale is None else scale
+    got = _run(q, k, v, table, lens, q_start, groups, scale, form=form)
+    starts = list(range(len(lens) + 1)) if q_start is None else q_start
+    hide = lambda z: np.nan_to_num(R.f64(z), nan=0.0, posinf=0.0, neginf=0.0)
+    ref, info = R.attention(R.f64(q), hide(k), hide(v), table, lens, page, starts, scale)
+    n = starts[-1]
+    R.check(R.f64(got)[:n], ref[:n], R.attention_tol(ref, info, dtype, d)[:n])
+    return got
+
+
+CASES = [
+    # lens, groups, n_q, hq, hkv, d, page, dtype
+    ([1], [], 1, 1, 1, 64, 16, "bf16"),
+    ([0], [], 1, 4, 1, 128, 16, "f16"),
+    ([0, 3, 0, 128, 129, 1], [], 1, 4, 2, 128, 16, "bf16"),
+    ([700], [], 1, 8, 2, 128, 64, "bf16"),
+    ([333, 17, 1, 64], [], 1, 6, 2, 64, 20, "f16"),
+    ([31, 32, 33, 127], [], 1, 5, 1, 128, 1, "bf16"),
+    ([90, 45], [], 1, 40, 1, 64, 7, "f16"),             # more heads a group than a tile's columns
+    ([200, 210, 205], [(0, 3, 192)], 1, 4, 1, 128, 16, "bf16"),
+    ([128, 128], [(0, 2, 128)], 1, 4, 1, 64, 16, "f16"),  # nothing of their own
+    ([50, 300, 310, 290, 12], [(1, 4, 288)], 1, 8, 2, 128, 32, "bf16"),
+    ([130, 140, 150, 60, 70], [(0, 3, 128), (3, 5, 48)], 1, 3, 3, 64, 16, "bf16"),
+    ([40, 41, 42, 43], [(0, 2, 0), (2, 4, 40)], 1, 4, 2, 64, 8, "f16"),  # a group that shares nothing
+    ([64, 100, 64], [(0, 3, 64)], 5, 8, 2, 64, 16, "bf16"),  # drafts that end in the shared keys
+    ([3, 9, 1], [], 4, 4, 1, 128, 16, "bf16"),             # more tokens than keys: rows that see none
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=[f"n{len(c[0])}_g{len(c[1])}_q{c[2]}_h{c[3]}_{c[4]}_d{c[5]}_p{c[6]}_{c[7]}"
+                                             for c in CASES])
+def test_paged(case):
+    lens, groups, n_q, hq, hkv, d, page, dtype = case
+    k, v, table = _batch(lens, None, groups, page, hkv, d, dtype, 1)
+    q = torch.randn((len(lens) * n_q, hq, d), device="cuda").to(R.TORCH[dtype])
+    starts = None if n_q == 1 else [n_q * i for i in range(len(lens) + 1)]
+    _check(q, k, v, table, lens, starts, groups, page, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_ragged_query_rows_and_rows_behind(dtype):
+    """0, 1, 7 and 40 newest tokens a sequence; rows behind the last sequence
+    stay as they were; head-major q and out."""
+    lens, starts = [30, 5, 260, 40], [0, 0, 1, 41, 48]
+    k, v, table = _batch(lens, None, [], 16, 2, 128, dtype, 2)
+    q = torch.randn((53, 4, 128), device="cuda").to(R.TORCH[dtype])
+    got = _check(q, k, v, table, lens, starts, [], 16, dtype, form="heads")
+    assert torch.isnan(got[48:].float()).all()
+
+
+def test_many_chunks_and_repeatable():
+    """A long shared prefix split over many workgroups: against the definition
+    on a few rows, and the same bits on every run."""
+    n, shared, page, hkv, hq, d = 9, 6000, 16, 2, 8, 128
+    lens = [shared + 40 * i + 1 for i in range(n)]
+    groups = [(0, n, shared)]
+    k, v, table = _batch(lens, None, groups, page, hkv, d, "bf16", 3)
+    q = torch.randn((n, hq, d), device="cuda").to(torch.bfloat16)
+    got = _check(q, k, v, table, lens, None, groups, page, "bf16")
+    for _ in range(3):
+        assert torch.equal(_run(q, k, v, table, lens, None, groups, d ** -0.5), got)
+    # without the groups the same sequences, the same values
+    _check(q, k, v, table, lens, None, [], page, "bf16")
+
+
+@pytest.mark.parametrize("garbage", [float("nan"), float("inf"), -float("inf")])
+def test_rows_that_nobody_holds_are_never_seen(garbage):
+    lens = [70, 33, 1]
+    k, v, table = _batch(lens, None, [], 16, 1, 64, "bf16", 4, garbage=garbage)
+    q = torch.randn((3, 4, 64), device="cuda").to(torch.bfloat16)
+    _check(q, k, v, table, lens, None, [], 16, "bf16")
+
+
+def test_pages_outside_the_cache_are_invisible():
+    """Entries -1, beyond the cache and far off inside a sequence: its keys are
+    not seen, even where page 0 holds NaN; a row of them only gives zeros."""
+    lens = [64, 48, 300]
+    k, v, table = _batch(lens, None, [(0, 3, 16)], 16, 1, 64, "bf16", 5)
+    used = set(table[table >= 0].tolist())
+    table[0, 2] = -1
+    table[1, :3] = [k.shape[0], 2 ** 31 - 1, -2 ** 31]
+    table[2, 5] = k.shape[0] + 7
+    for s in (0, 2):
+        table[s, 0] = table[1, 0]
+    spare = next(p for p in range(k.shape[0]) if p not in used)
+    k[spare], v[spare] = float("nan"), float("nan")
+    # the spare page becomes page 0, what a missing row's address falls back to
+    if spare:
+        for z in (k, v):
+            z[[0, spare]] = z[[spare, 0]]
+        a, b = table == 0, table == spare
+        table[a], table[b] = spare, 0
+    q = torch.randn((3, 2, 64), device="cuda").to(torch.bfloat16)
+    got = _check(q, k, v, table, lens, None, [(0, 3, 16)], 16, "bf16")
+    assert (got[1] == 0).all()
+
+
+def test_lengths_beyond_the_table_and_below_zero():
+    lens = [64, 64]
+    k, v, table = _batch(lens, None, [], 16, 1, 64, "f16", 6)
+    table = table[:, :4]  # rows of exactly 64 keys
+    q = torch.randn((2, 1, 64), device="cuda").half()
+    got = _run(q, k, v, table, [2 ** 31 - 1, -5], None, [], 0.125)
+    ref = _run(q, k, v, table, [64, 0], None, [], 0.125)
+    assert torch.equal(got, ref) and (got[1] == 0).all()
+
+
+def test_large_scores_and_equal_values():
+    """Scores far apart and large: the largest key wins; equal values come out
+    as they are."""
+    lens = [400]
+    k, v, table = _batch(lens, None, [], 16, 1, 128, "bf16", 7)
+    q = torch.randn((1, 4, 128), device="cuda").to(torch.bfloat16)
+    _check(q, k, v, table, lens, None, [], 16, "bf16", scale=30.0)
+    v.fill_(3.0)
+    assert (_run(q, k, v, table, lens, None, [], 0.1) == 3.0).all()
+
+
+def test_a_cache_past_4_gib():
+    """Pages whose byte offsets pass 2^32."""
+    page, hkv, d = 256, 8, 128
+    n_pages = (4 << 30) // (page * hkv * d * 2) + 40
+    k = torch.empty((n_pages, hkv, page, d), device="cuda", dtype=torch.bfloat16)
+    v = torch.empty_like(k)
+    table = np.asarray([[n_pages - 1, 3, n_pages - 7], [0, n_pages - 2, -1]])
+    for p in (0, 3, n_pages - 1, n_pages - 2, n_pages - 7):
+        k[p] = torch.randn((hkv, page, d), device="cuda").to(torch.bfloat16)
+        v[p] = torch.randn((hkv, page, d), device="cuda").to(torch.bfloat16)
+    lens = [600, 300]
+    q = torch.randn((2, hkv, d), device="cuda").to(torch.bfloat16)
+    got = _run(q, k, v, table, lens, None, [], d ** -0.5)
+    small = [0, 3, n_pages - 7, n_pages - 2, n_pages - 1]
+    t2 = np.asarray([[4, 1, 2], [0, 3, -1]])
+    ref, info = R.attention(R.f64(q), R.f64(k[small]), R.f64(v[small]), t2, lens, page, [0, 1, 2], d ** -0.5)
+    R.check(R.f64(got), ref, R.attention_tol(ref, info, "bf16", d))
+
+
+def test_captured_call_follows_lengths():
+    """Captured once, replayed with other lengths and queries: every replay is
+    the eager call's, with eager work of the same stream workspace in between."""
+    page, hkv, hq, d, n = 16, 2, 8, 128, 5
+    lens = [300, 20, 170, 1, 64]
+    k, v, table = _batch([320] * n, None, [(1, 4, 64)], page, hkv, d, "bf16", 8)
+    groups = [(1, 4, 64)]
+    q = torch.randn((n, hq * d), device="cuda").to(torch.bfloat16)
+    out = torch.empty_like(q)
+    tab, ln = R.i32(table), R.i32(lens)
+    gs, gk = R.i32([1, 4]), R.i32([64])
+    ws = ea.new_workspace(ea.attention_paged_workspace(R.rel(q), R.pages_rel(k), n, 1))
+    rq, rk, rv, ro = R.rel(q), R.pages_rel(k), R.pages_rel(v), R.rel(out)
+    call = lambda: ea.attention_paged(rq, rk, rv, ro, scale=0.1, table=tab, lengths=ln, group_start=gs,
+                                      group_shared=gk, workspace=ws)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for step in range(4):
+        new = [min(320, x + 37 * step) for x in lens]
+        ln.copy_(R.i32(new))
+        q.copy_(torch.randn_like(q.float()).to(torch.bfloat16))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = _run(q.view(n, hq, d), k, v, table, new, None, groups, 0.1)
+        assert torch.equal(out.view(n, hq, d), eager)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    page, hkv, hq, d, n = 16, 2, 8, 128, 6
+    lens = [900, 800, 700, 600, 500, 400]
+    k, v, table = _batch(lens, None, [], page, hkv, d, "f16", 9)
+    qs = [torch.randn((n, hq, d), device="cuda").half() for _ in range(2)]
+    ref = [_run(q, k, v, table, lens, None, [], 0.1).clone() for q in qs]
+    tab, ln = R.i32(table), R.i32(lens)
+    rk, rv = R.pages_rel(k), R.pages_rel(v)
+    outs = [torch.empty((n, hq * d), device="cuda", dtype=torch.float16) for _ in qs]
+    rels = [(R.rel(q.view(n, hq * d)), R.rel(o)) for q, o in zip(qs, outs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(5):
+        for s, (rq, ro) in zip(streams, rels):
+            with torch.cuda.stream(s):
+                ea.attention_paged(rq, rk, rv, ro, scale=0.1, table=tab, lengths=ln)
+    torch.cuda.synchronize()
+    for o, r in zip(outs, ref):
+        assert torch.equal(o.view(n, hq, d), r)

@@ -1,0 +1,199 @@
+"""The page table's calls against their definition, page by page: exact, over
+random walks of extend, select and compact, and where they have to do nothing."""
+import numpy as np
+import pytest
+import torch
+
+import decode_ref as R
+from paper_2609_03905_amd import ea
+
+pytestmark = pytest.mark.gpu
+
+
+class Device:
+    """The same state on the device, and the calls."""
+
+    def __init__(self, ref: R.Pages, caches=()):
+        self.page = ref.page
+        self.table, self.len, self.refs = R.i32(ref.table), R.i32(ref.len), R.i32(ref.refs)
+        self.status = R.i32([9, 9])
+        self.caches = list(caches)
+
+    def extend(self, add, n_tokens, in_place=True):
+        slots, pos = R.i32([7] * n_tokens), R.i32([7] * n_tokens)
+        ol, orf = (self.len, self.refs) if in_place else (torch.empty_like(self.len), torch.empty_like(self.refs))
+        before = self.len.clone(), self.refs.clone()
+        ea.pages_extend(self.table, self.len, self.refs, R.i32(add), page_size=self.page, out_lengths=ol,
+                        out_refs=orf, status=self.status, slots=slots, positions=pos)
+        if not in_place:
+            assert torch.equal(self.len, before[0]) and torch.equal(self.refs, before[1])
+        self.len, self.refs = ol, orf
+        return tuple(self.status.tolist()), slots.cpu().numpy(), pos.cpu().numpy()
+
+    def select(self, parent):
+        new = [torch.full_like(z, 5) for z in (self.table, self.len, self.refs)]
+        ea.pages_select(self.caches, R.i32(parent), self.table, self.len, self.refs, out_table=new[0],
+                        out_lengths=new[1], out_refs=new[2], status=self.status, page_size=self.page)
+        self.table, self.len, self.refs = new
+        return tuple(self.status.tolist())
+
+    def compact(self, in_place=True):
+        t, r = (self.table, self.refs) if in_place else (torch.full_like(self.table, 5), torch.full_like(self.refs, 5))
+        ea.pages_compact(self.caches, self.table, self.len, self.refs, out_table=t, out_refs=r, status=self.status,
+                         page_size=self.page)
+        self.table, self.refs = t, r
+        return tuple(self.status.tolist())
+
+    def same(self, ref: R.Pages):
+        assert np.array_equal(self.len.cpu().numpy(), ref.len)
+        assert np.array_equal(self.refs.cpu().numpy(), ref.refs)
+        t = self.table.cpu().numpy()
+        for s, n in enumerate(ref.len):
+            k = min(ref.held(max(n, 0)), ref.stride)
+            assert np.array_equal(t[s, :k], ref.table[s, :k]), s
+
+
+@pytest.mark.parametrize("n_seq,stride,n_pages,page,seed", [(1, 3, 4, 1, 0), (1, 1, 1, 16, 1), (5, 6, 17, 4, 2),
+                                                            (40, 9, 300, 7, 3), (300, 5, 1025, 16, 4),
+                                                            (7, 40, 5000, 3, 5)])
+def test_random_walk(n_seq, stride, n_pages, page, seed):
+    rng = np.random.default_rng(seed)
+    planes = rng.integers(-30000, 30000, (2, n_pages, 2, page, 64)).astype(np.int16)
+    data = torch.from_numpy(planes.copy()).cuda().view(torch.bfloat16)
+    ref = R.Pages(n_seq, stride, n_pages, page, planes)
+    # two caches of one plane each, or one of two
+    if seed % 2:
+        dev = Device(ref, [R.pages_rel(data)])
+    else:
+        a, b = data[0].clone(), data[1].clone()
+        dev = Device(ref, [R.pages_rel(a), R.pages_rel(b)])
+    seen = set()
+    for step in range(24):
+        op = rng.choice(["extend", "extend", "select", "compact"])
+        if op == "extend":
+            add = rng.integers(-1, max(2, stride * page // 3), n_seq)
+            if rng.random() < 0.3:
+                add = rng.integers(0, 2, n_seq)
+            n_tokens = int(max(0, int(np.maximum(add, 0).sum()) + rng.integers(-2, 4)))
+            want, got = ref.extend(add, n_tokens), dev.extend(add, n_tokens, in_place=step % 2 == 0)
+            assert got[0] == want[0]
+            assert np.array_equal(got[1], want[1]) and np.array_equal(got[2], want[2])
+            code = want[0]
+        elif op == "select":
+            parent = rng.integers(-1, n_seq + 1, n_seq)
+            if rng.random() < 0.3:
+                parent = rng.permutation(n_seq)
+            code = ref.select(parent)
+            assert dev.select(parent) == code
+        else:
+            code = ref.compact()
+            assert dev.compact(in_place=step % 2 == 0) == code
+        seen.add((op, code[0]))
+        dev.same(ref)
+        # the held rows of every sequence, in every plane
+        got = data.view(torch.int16).cpu().numpy() if seed % 2 else \
+            np.stack([a.view(torch.int16).cpu().numpy(), b.view(torch.int16).cpu().numpy()])
+        assert np.array_equal(got, ref.planes), op
+    assert len(seen) > 1
+
+
+def test_nothing_is_done_without_pages():
+    """One page short: the state goes through as it came, in every output."""
+    ref = R.Pages(3, 4, 6, 8)
+    dev = Device(ref)
+    assert dev.extend([8, 9, 17], 34)[0] == ref.extend([8, 9, 17], 34)[0] == (ea.PAGES_OK, 0)
+    for add in ([0, 8, 0], [8, 7, 7]):
+        want, got = ref.extend(add, 4), dev.extend(add, 4, in_place=False)
+        assert got[0] == want[0] == (ea.PAGES_NONE_FREE, 0)
+        assert (got[1] == -1).all() and (got[2] == 0).all()
+        dev.same(ref)
+    assert dev.select([1, 1, 2]) == ref.select([1, 1, 2]) == (ea.PAGES_OK, 0)  # the freed page serves the copy
+    dev.same(ref)
+    assert dev.select([2, 2, 2]) == ref.select([2, 2, 2])
+    dev.same(ref)
+
+
+def test_a_fork_that_fits_nowhere_does_nothing():
+    ref = R.Pages(2, 3, 2, 4)
+    dev = Device(ref)
+    for add in ([3, 0], [0, 3]):
+        assert dev.extend(add, 0)[0] == ref.extend(add, 0)[0]
+    ref2 = R.Pages(3, 3, 2, 4)
+    ref2.table[:2], ref2.len[:2], ref2.refs[:] = ref.table, ref.len, ref.refs
+    dev2 = Device(ref2)
+    assert dev2.select([0, 1, 1]) == ref2.select([0, 1, 1]) == (ea.PAGES_NONE_FREE, 0)
+    dev2.same(ref2)
+
+
+def test_lengths_that_no_row_holds():
+    ref = R.Pages(2, 2, 8, 4)
+    ref.len[:] = [9, 3]
+    ref.table[1, 0], ref.refs[0] = 0, 1
+    dev = Device(ref)
+    assert dev.extend([0, 1], 1)[0] == ref.extend([0, 1], 1)[0] == (ea.PAGES_TOO_LONG, 7)
+    assert dev.select([1, 0]) == ref.select([1, 0]) == (ea.PAGES_TOO_LONG, 7)
+    dev.same(ref)
+    ref.len[:] = dev_len = np.asarray([-1, 3], np.int32)
+    dev.len = R.i32(dev_len)
+    assert dev.extend([1, 1], 1)[0] == ref.extend([1, 1], 1)[0] == (ea.PAGES_TOO_LONG, 7)
+    dev.same(ref)
+
+
+def test_entries_outside_the_cache():
+    """A table entry that names no page counts none, copies none and is kept."""
+    ref = R.Pages(3, 3, 9, 4, np.arange(9 * 4 * 32, dtype=np.int16).reshape(1, 9, 1, 4, 32))
+    ref.len[:] = [7, 4, 2]
+    ref.table[0, :2], ref.table[1, :1], ref.table[2, :1] = [-4, 100], [8], [2 ** 30]
+    ref.refs[8] = 1
+    data = torch.from_numpy(ref.planes.copy()).cuda().view(torch.bfloat16)
+    dev = Device(ref, [R.pages_rel(data)])
+    assert dev.extend([1, 0, 1], 2)[0] == ref.extend([1, 0, 1], 2)[0]
+    assert dev.select([0, 0, 2]) == ref.select([0, 0, 2])
+    dev.same(ref)
+    assert dev.compact() == ref.compact()
+    dev.same(ref)
+    assert np.array_equal(data.view(torch.int16).cpu().numpy(), ref.planes)
+
+
+def test_pages_with_padding_between_them():
+    """Pages of 48 and 80 bytes, each at a 256-byte multiple."""
+    for d, heads in ((8, 1), (40, 1)):
+        planes = np.random.default_rng(d).integers(0, 30000, (3, 11, heads, 3, d)).astype(np.int16)
+        ref = R.Pages(4, 4, 11, 3, planes)
+        cache = R.pages_rel(torch.from_numpy(planes.copy()).cuda().view(torch.bfloat16))
+        dev = Device(ref, [cache])
+        assert dev.extend([4, 2, 7, 1], 14)[0] == ref.extend([4, 2, 7, 1], 14)[0]
+        assert dev.select([0, 0, 2, -1]) == ref.select([0, 0, 2, -1])
+        assert dev.select([-1, 1, 0, 1]) == ref.select([-1, 1, 0, 1])
+        assert dev.compact() == ref.compact()
+        dev.same(ref)
+        assert np.array_equal(R.unblocked(cache).view(torch.int16).cpu().numpy(), ref.planes)
+
+
+def test_captured_step():
+    """extend and select captured into one graph and replayed: every replay is
+    the definition's."""
+    n, stride, n_pages, page = 6, 8, 60, 4
+    ref = R.Pages(n, stride, n_pages, page)
+    table, ln, refs = R.i32(ref.table), R.i32(ref.len), R.i32(ref.refs)
+    t2, l2, r2 = torch.empty_like(table), torch.empty_like(ln), torch.empty_like(refs)
+    add, parent = R.i32([1, 2, 3, 0, 1, 5]), R.i32([0, 0, 2, 3, -1, 5])
+    st, ws = R.i32([0, 0]), ea.new_workspace(1 << 20)
+
+    def step():
+        ea.pages_extend(table, ln, refs, add, page_size=page, status=st)
+        ea.pages_select([], parent, table, ln, refs, out_table=t2, out_lengths=l2, out_refs=r2, status=st,
+                        page_size=page, workspace=ws)
+        table.copy_(t2), ln.copy_(l2), refs.copy_(r2)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(5):
+        graph.replay()
+        torch.cuda.synchronize()
+        ref.extend(add.tolist(), 0)
+        code = ref.select(parent.tolist())
+        assert tuple(st.tolist()) == code
+        assert np.array_equal(table.cpu().numpy(), ref.table) and np.array_equal(refs.cpu().numpy(), ref.refs)
+        assert torch.equal(ln.cpu(), torch.from_numpy(ref.len))
