@@ -88,7 +88,7 @@ struct HeadsGradArgs {
   float eps;
   int32_t groups_per_wave, n_wg;
 };
-constexpr int kHeadsGradMaxWg = 1024;
+constexpr int kHeadsGradMaxWg = 768;
 hipError_t launch_heads_grad(const HeadsGradArgs& a, int32_t dtype, hipStream_t s);
 
 // ---- attention over pages ------------------------------------------------------

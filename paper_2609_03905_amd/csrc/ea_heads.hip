@@ -12,12 +12,15 @@
 //   du = r (s - u r mean(s u r)).
 //
 // Bound by memory: each element is read once and written once, about 10
-// operations on it.  A head row is held by d/8 lanes (16 bytes each in bf16),
-// so the mean is a few lane exchanges, and the other half of a rotated pair is
-// read again by the lane that needs it, which the L1 answers.  A wave walks
-// several groups of heads of one row, because the angles are the costly part:
-// p f_i / 2 pi is taken to its fraction in 64 bits (positions of a million
-// cost 32-bit products all of their angle) and sine and cosine follow in 32.
+// operations on it.  A lane holds 16 elements of a row (two loads of 16 bytes
+// in bf16), the two halves of 8 rotated pairs, so no element is read twice and
+// the mean takes few lane exchanges.  A wave holds 64 / LPH rows at once, heads
+// of one token, and walks the token's heads with the next rows' loads in
+// flight.  The angles are the costly part: p f_i / 2 pi is taken to its
+// fraction in 64 bits (at a position of a million a 32-bit product has lost the
+// angle), sine and cosine follow in 32; the wave's lanes share that work, each
+// pair once a token, and hand the results round through shared memory, where
+// the norm weights are kept too.
 #include "ea_decode.h"
 #include "ea_device.h"
 
@@ -81,237 +84,360 @@ __device__ __forceinline__ Raw<DT> narrow(const float (&f)[8]) {
   return r;
 }
 
-// Sum over the LPH lanes of a head row (LPH a power of two from 8 to 64).
+// Sum over the LPH lanes of a head row (LPH a power of two from 4 to 32).
 template <int LPH>
 __device__ __forceinline__ float row_sum(float v) {
   v += dpp_f<0xB1>(v);
   v += dpp_f<0x4E>(v);
-  v += dpp_f<0x141>(v);
+  if constexpr (LPH >= 8) v += dpp_f<0x141>(v);
   if constexpr (LPH >= 16) v += dpp_f<0x140>(v);
   if constexpr (LPH >= 32) v += other16(v);
-  if constexpr (LPH >= 64) v += other32(v);
   return v;
 }
 
-// How the partner of an element is reached: in the lane's own eight (pairs of
-// neighbours), as another eight (halves, rot/2 a multiple of 8), or one by one.
-enum { PAIR_NONE, PAIR_OWN, PAIR_CHUNK, PAIR_ELEM };
-__device__ __forceinline__ int pair_mode(int rot, int inter) {
-  return rot == 0 ? PAIR_NONE : inter ? PAIR_OWN : (rot / 2) % 8 == 0 ? PAIR_CHUNK : PAIR_ELEM;
+// Which 16 elements of a row lane l holds, as two eights, and how they pair:
+//   HALVES  eights (l, l + rot/16) of the rotated part, element e of one with
+//           element e of the other; then the rest of the row, eight by eight
+//   NEIGHBOURS  eights (2l, 2l + 1), pairs of neighbours
+//   APART   as NEIGHBOURS, but halves that no eight divides (rot/2 no multiple
+//           of 8): partners are read one by one
+enum { HALVES, NEIGHBOURS, APART };
+template <int MODE>
+__device__ __forceinline__ int eight_of(int l, int which, int rot) {
+  if (MODE == HALVES) return l < rot / 16 ? l + which * (rot / 16) : 2 * l + which;
+  return 2 * l + which;
 }
-// Index of element i's partner (i < rot, halves).
-__device__ __forceinline__ int partner_of(int i, int half) { return i < half ? i + half : i - half; }
 
-// cos and signed sin of the lane's eight elements at one position; elements
-// past the rotated part get (1, 0).
-__device__ __forceinline__ void angles(const float* freq, int pos, int c, int rot, int inter, bool active,
-                                       float (&cs)[8], float (&sn)[8]) {
-  const int half = rot / 2;
+// Shared memory of a workgroup: the norm weights as f32 (1 where there are
+// none) and every wave's cos and sin of its token's angles.
+template <int LPH>
+struct HeadsShared {
+  __attribute__((aligned(16))) float w[2][LPH * 16];
+  __attribute__((aligned(16))) float2 turn[kWaves][LPH * 8];
+};
+
+template <int LPH, class A>
+__device__ __forceinline__ void stage_weights(const A& a, HeadsShared<LPH>& s) {
+  for (int i = threadIdx.x; i < 2 * LPH * 16; i += kThreads) {
+    const int kind = i >= LPH * 16, col = i - kind * LPH * 16;
+    const char* w = kind ? a.wk : a.wq;
+    s.w[kind][col] = w && col < a.d ? ld_elem(w, col, kind ? a.wk_dt : a.wq_dt) : 1.0f;
+  }
+  __syncthreads();
+}
+
+// cos and sin of the token's rot/2 angles, one lane a pair.
+__device__ __forceinline__ void turn_table(const float* freq, int pos, int pairs, int lane, float2* out) {
+  for (int i = lane; i < pairs; i += 64) {
+    const double turns = (double)pos * (double)freq[i] * 0.15915494309189535;  // 1 / (2 pi)
+    const float part = (float)(turns - rint(turns));
+    float s, c;
+    sincospif(2.0f * part, &s, &c);
+    out[i] = make_float2(c, s);
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The lane's eight (cos, sin) of its pairs; (1, 0) past the rotated part.
+template <int MODE>
+__device__ __forceinline__ void my_turns(const float2* t, int l, int pairs, float (&cs)[8], float (&sn)[8]) {
+  if (MODE == APART) return;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int i = 8 * c + e;
-    cs[e] = 1.0f;
-    sn[e] = 0.0f;
-    if (active && i < rot) {
-      const int f = inter ? i >> 1 : (i < half ? i : i - half);
-      const bool first = inter ? !(i & 1) : i < half;
-      const double turns = (double)pos * (double)freq[f] * 0.15915494309189535;  // 1 / (2 pi)
-      const float part = (float)(turns - rint(turns));
-      float s, co;
-      sincospif(2.0f * part, &s, &co);
-      cs[e] = co;
-      sn[e] = first ? -s : s;
-    }
+  for (int e = 0; e < 8; e += 2) {
+    float4 v = make_float4(1.0f, 0.0f, 1.0f, 0.0f);
+    if (8 * l + e + 1 < pairs) v = *reinterpret_cast<const float4*>(t + 8 * l + e);
+    else if (8 * l + e < pairs) v.x = t[8 * l + e].x, v.y = t[8 * l + e].y;
+    cs[e] = v.x, sn[e] = v.y, cs[e + 1] = v.z, sn[e + 1] = v.w;
   }
 }
 
-// The partner values of the lane's eight elements of the row at `row`, in
-// their stored order (own: its own eight).
+// The lane's first n pairs rotated by its angles (sign -1: back); the others
+// stay, whatever their neighbours hold.  a, b: its two eights.
+template <int MODE>
+__device__ __forceinline__ void turn(float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8],
+                                     float sign, int n) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float c = cs[e], s = sign * sn[e];
+    float& x = MODE == HALVES ? a[e] : (e < 4 ? a : b)[2 * (e & 3)];
+    float& y = MODE == HALVES ? b[e] : (e < 4 ? a : b)[2 * (e & 3) + 1];
+    const float p = fmaf(x, c, -y * s), q = fmaf(y, c, x * s);
+    x = e < n ? p : x;
+    y = e < n ? q : y;
+  }
+}
+
+// APART: the eight v (elements 8 q ..) rotated with partners read one by one
+// from the stored row, scaled by r and the weights w (null: none).
 template <int DT>
-__device__ __forceinline__ void partners(const char* row, int mode, int c, int rot, const float (&own)[8],
-                                         float (&p)[8]) {
-  const int half = rot / 2;
-  if (mode == PAIR_CHUNK) {
-    if (8 * c < rot) {
-      widen<DT>(load_raw<DT>(row + (int64_t)partner_of(8 * c, half) * (DT == EA_F32 ? 4 : 2)), p);
-      return;
-    }
-  } else if (mode == PAIR_ELEM) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = 8 * c + e;
-      p[e] = i < rot ? ld_elem(row, partner_of(i, half), DT) : 0.0f;
-    }
-    return;
-  } else if (mode == PAIR_OWN) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = 8 * c + e < rot ? own[e ^ 1] : 0.0f;
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) p[e] = 0.0f;
-}
-
-// Norm weights of the lane's eight elements and of their partners.
-__device__ __forceinline__ void weights(const char* w, int dt, int mode, int c, int rot, bool active, float (&own)[8],
-                                        float (&par)[8]) {
+__device__ __forceinline__ void turn_apart(float (&v)[8], const char* row, int q, int rot, const float2* t, float r,
+                                           const float* w, float sign) {
   const int half = rot / 2;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const int i = 8 * c + e;
-    own[e] = w && active ? ld_elem(w, i, dt) : 1.0f;
-    const int j = mode == PAIR_OWN ? i ^ 1 : partner_of(i, half);
-    par[e] = w && active && i < rot ? ld_elem(w, j, dt) : 1.0f;
+    const int i = 8 * q + e;
+    if (i < rot) {
+      const bool first = i < half;
+      const int j = first ? i + half : i - half;
+      const float2 cs = t[first ? i : j];
+      const float other = ld_elem(row, j, DT) * r * (w ? w[j] : 1.0f), s = sign * cs.y;
+      v[e] = fmaf(v[e], cs.x, first ? -other * s : other * s);
+    }
   }
 }
 
-template <int LPH, int DT>
+// A lane's two eights as stored; zeros where the row has none.
+template <int DT>
+struct Pair {
+  Raw<DT> a, b;
+};
+template <int DT>
+__device__ __forceinline__ Pair<DT> load_pair(const char* row, bool ona, bool onb, int qa, int qb) {
+  constexpr int ES = DT == EA_F32 ? 4 : 2;
+  Pair<DT> p{};
+  if (ona) p.a = load_raw<DT>(row + qa * 8 * ES);
+  if (onb) p.b = load_raw<DT>(row + qb * 8 * ES);
+  return p;
+}
+
+template <int LPH, int DT, int MODE>
 __global__ __launch_bounds__(kThreads) void heads_kernel(const HeadsArgs a) {
   constexpr int RPW = 64 / LPH;  // head rows that a wave holds at once
-  const int lane = threadIdx.x & 63, sub = lane / LPH, c = lane % LPH;
-  const int heads = a.hq + 2 * a.hkv, groups = (heads + RPW - 1) / RPW;
+  constexpr int ES = DT == EA_F32 ? 4 : 2;
+  __shared__ HeadsShared<LPH> sh;
+  const int lane = threadIdx.x & 63, sub = lane / LPH, l = lane % LPH;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int heads = a.hq + 2 * a.hkv, groups = (heads + RPW - 1) / RPW, pairs = a.rot / 2;
   const int parts = (groups + a.groups_per_wave - 1) / a.groups_per_wave;
   const int64_t items = (int64_t)a.t * parts;
-  const bool active = 8 * c < a.d;
-  const int mode = pair_mode(a.rot, a.inter);
-  float wq[8], wqp[8], wk[8], wkp[8];
-  weights(a.wq, a.wq_dt, mode, c, a.rot, active, wq, wqp);
-  weights(a.wk, a.wk_dt, mode, c, a.rot, active, wk, wkp);
-  for (int64_t it = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); it < items;
-       it += (int64_t)gridDim.x * kWaves) {
-  const int t = (int)(it / parts), part = (int)(it - (int64_t)t * parts);
-  float cs[8], sn[8];
-  angles(a.freq, a.pos ? a.pos[t] : t, c, a.rot, a.inter, active, cs, sn);
-  // a row's place in the cache; none: its key and value rows go nowhere
-  int slot = 0;
-  int64_t page_off = 0;
-  int in_page = 0;
-  if (a.slots) {
-    slot = a.slots[t];
-    if (slot < 0 || slot >= a.n_slots) slot = -1;
-    const int pg = div_fast(max(slot, 0), a.page);
-    in_page = max(slot, 0) - pg * a.page_size;
-    page_off = pg * a.page_bytes;
-  }
-  const int g1 = min(groups, (part + 1) * a.groups_per_wave);
-  constexpr int ES = DT == EA_F32 ? 4 : 2;
-  for (int gi = part * a.groups_per_wave; gi < g1; ++gi) {
-    const int h = gi * RPW + sub;
-    const bool on = active && h < heads;
-    const bool is_q = h < a.hq, is_k = !is_q && h < a.hq + a.hkv, is_v = !is_q && !is_k;
-    const char* row = a.px + row_offset(a.x, t, min(h, heads - 1));
-    float u[8], p[8];
-    if (on) {
-      widen<DT>(load_raw<DT>(row + c * 8 * ES), u);
-      partners<DT>(row, mode, c, a.rot, u, p);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] = p[e] = 0.0f;
+  const int qa = eight_of<MODE>(l, 0, a.rot), qb = eight_of<MODE>(l, 1, a.rot);
+  const bool in_a = 8 * qa < a.d, in_b = 8 * qb < a.d;
+  auto row_of = [&](int t, int gi) { return a.px + row_offset(a.x, t, min(gi * RPW + sub, heads - 1)); };
+  auto load = [&](int t, int gi) {
+    const bool on = gi * RPW + sub < heads;
+    return load_pair<DT>(row_of(t, gi), on && in_a, on && in_b, qa, qb);
+  };
+  int64_t it = (int64_t)blockIdx.x * kWaves + wid;
+  // the first rows are on their way while the weights are staged
+  Pair<DT> next{};
+  int t = 0, part = 0, pos = 0;
+  auto begin = [&]() {
+    if (it >= items) return;
+    t = (int)(it / parts);
+    part = (int)(it - (int64_t)t * parts);
+    next = load(t, part * a.groups_per_wave);
+    pos = a.pos ? a.pos[t] : t;
+  };
+  begin();
+  stage_weights<LPH>(a, sh);
+  while (it < items) {
+    const int g0 = part * a.groups_per_wave, g1 = min(groups, g0 + a.groups_per_wave);
+    // the row's place in the cache; none: its keys and values go nowhere
+    int slot = 0, in_page = 0;
+    int64_t page_off = 0;
+    if (a.slots) {
+      slot = a.slots[t];
+      if (slot < 0 || slot >= a.n_slots) slot = -1;
+      const int pg = div_fast(max(slot, 0), a.page);
+      in_page = max(slot, 0) - pg * a.page_size;
+      page_off = pg * a.page_bytes;
     }
-    const char* w = is_q ? a.wq : a.wk;
-    float ss = 0.0f;
+    float cs[8], sn[8];
+    turn_table(a.freq, pos, pairs, lane, sh.turn[wid]);
+    my_turns<MODE>(sh.turn[wid], l, pairs, cs, sn);
+    for (int gi = g0; gi < g1; ++gi) {
+      const Pair<DT> cur = next;
+      if (gi + 1 < g1) next = load(t, gi + 1);
+      const int h = gi * RPW + sub;
+      const bool is_q = h < a.hq, is_v = h >= a.hq + a.hkv;
+      Pair<DT> out = cur;
+      if (__any(!is_v)) {
+        float u[8], v[8];
+        widen<DT>(cur.a, u);
+        widen<DT>(cur.b, v);
+        float r = 1.0f;
+        const float* w = sh.w[is_q ? 0 : 1];
+        if (a.wq) {
+          float ss = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fmaf(u[e], u[e], ss);
-    ss = row_sum<LPH>(ss);
-    const float r = w && !is_v ? 1.0f / sqrtf(ss / (float)a.d + a.eps) : 1.0f;
-    float y[8];
+          for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], fmaf(u[e], u[e], ss));
+          r = 1.0f / sqrtf(row_sum<LPH>(ss) / (float)a.d + a.eps);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float n = u[e] * r * (is_q ? wq[e] : wk[e]);
-      const float m = p[e] * r * (is_q ? wqp[e] : wkp[e]);
-      y[e] = is_v ? u[e] : fmaf(n, cs[e], m * sn[e]);
-    }
-    if (!on) continue;
-    char* dst;
-    if (is_q) {
-      dst = a.pq + row_offset(a.q, t, h);
-    } else {
-      const int hh = h - a.hq - (is_k ? 0 : a.hkv);
-      dst = is_k ? a.pk : a.pv;
-      if (a.slots) {
-        if (slot < 0) continue;
-        dst += page_off + ((int64_t)hh * a.page_size + in_page) * a.d * ES;
-      } else {
-        dst += row_offset(is_k ? a.k : a.v, t, hh);
+          for (int e = 0; e < 8; e += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(w + 8 * min(qa, LPH * 2 - 1) + e);
+            const float4 y = *reinterpret_cast<const float4*>(w + 8 * min(qb, LPH * 2 - 1) + e);
+            u[e] *= r * x.x, u[e + 1] *= r * x.y, u[e + 2] *= r * x.z, u[e + 3] *= r * x.w;
+            v[e] *= r * y.x, v[e + 1] *= r * y.y, v[e + 2] *= r * y.z, v[e + 3] *= r * y.w;
+          }
+        }
+        if (MODE == APART) {
+          if (h < heads && !is_v) {
+            turn_apart<DT>(u, row_of(t, gi), qa, a.rot, sh.turn[wid], r, w, 1.0f);
+            turn_apart<DT>(v, row_of(t, gi), qb, a.rot, sh.turn[wid], r, w, 1.0f);
+          }
+        } else {
+          turn<MODE>(u, v, cs, sn, 1.0f, pairs - 8 * l);
+        }
+        if (!is_v) {
+          out.a = narrow<DT>(u);
+          out.b = narrow<DT>(v);
+        }
       }
+      if (h >= heads) continue;
+      char* dst;
+      if (is_q) {
+        dst = a.pq + row_offset(a.q, t, h);
+      } else {
+        const int hh = h - a.hq - (is_v ? a.hkv : 0);
+        dst = is_v ? a.pv : a.pk;
+        if (a.slots) {
+          if (slot < 0) continue;
+          dst += page_off + ((int64_t)hh * a.page_size + in_page) * a.d * ES;
+        } else {
+          dst += row_offset(is_v ? a.v : a.k, t, hh);
+        }
+      }
+      if (in_a) store_raw<DT>(dst + qa * 8 * ES, out.a);
+      if (in_b) store_raw<DT>(dst + qb * 8 * ES, out.b);
     }
-    store_raw<DT>(dst + c * 8 * ES, narrow<DT>(y));
-  }
+    __builtin_amdgcn_wave_barrier();  // the table is the next token's from here
+    it += (int64_t)gridDim.x * kWaves;
+    begin();
   }
 }
 
-template <int LPH, int DT>
-__global__ __launch_bounds__(kThreads) void heads_grad_kernel(const HeadsGradArgs a) {
+template <int LPH, int DT, int MODE>
+__global__ __launch_bounds__(kThreads, DT == EA_F32 ? 2 : 3) void heads_grad_kernel(const HeadsGradArgs a) {
   constexpr int RPW = 64 / LPH;
   constexpr int ES = DT == EA_F32 ? 4 : 2;
-  __shared__ float s_dw[kWaves][2][LPH * 8];
-  const int lane = threadIdx.x & 63, sub = lane / LPH, c = lane % LPH;
+  __shared__ HeadsShared<LPH> sh;
+  __shared__ float s_dw[kWaves][2][LPH * 16];
+  const int lane = threadIdx.x & 63, sub = lane / LPH, l = lane % LPH;
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int heads = a.hq + 2 * a.hkv, groups = (heads + RPW - 1) / RPW;
+  const int heads = a.hq + 2 * a.hkv, groups = (heads + RPW - 1) / RPW, pairs = a.rot / 2;
   const int parts = (groups + a.groups_per_wave - 1) / a.groups_per_wave;
-  const bool active = 8 * c < a.d;
-  const int mode = pair_mode(a.rot, a.inter);
-  float wq[8], wk[8], unused[8], dwq[8] = {}, dwk[8] = {};
-  weights(a.wq, a.wq_dt, mode, c, a.rot, active, wq, unused);
-  weights(a.wk, a.wk_dt, mode, c, a.rot, active, wk, unused);
   const int64_t items = (int64_t)a.t * parts;
-  for (int64_t it = (int64_t)blockIdx.x * kWaves + wid; it < items; it += (int64_t)gridDim.x * kWaves) {
-    const int t = (int)(it / parts), part = (int)(it - (int64_t)t * parts);
+  const int qa = eight_of<MODE>(l, 0, a.rot), qb = eight_of<MODE>(l, 1, a.rot);
+  const bool in_a = 8 * qa < a.d, in_b = 8 * qb < a.d;
+  float dwq[16] = {}, dwk[16] = {};
+  auto dy_of = [&](int t, int gi) {
+    const int h = min(gi * RPW + sub, heads - 1);
+    return h < a.hq             ? a.pdq + row_offset(a.q, t, h)
+           : h < a.hq + a.hkv ? a.pdk + row_offset(a.k, t, h - a.hq)
+                              : a.pdv + row_offset(a.v, t, h - a.hq - a.hkv);
+  };
+  auto load_dy = [&](int t, int gi) {
+    const bool on = gi * RPW + sub < heads;
+    return load_pair<DT>(dy_of(t, gi), on && in_a, on && in_b, qa, qb);
+  };
+  auto load_x = [&](int t, int gi) {
+    const int h = gi * RPW + sub;
+    const bool on = h < a.hq + a.hkv && a.wq;  // the values' rows are not needed
+    return load_pair<DT>(a.px + row_offset(a.x, t, min(h, heads - 1)), on && in_a, on && in_b, qa, qb);
+  };
+  int64_t it = (int64_t)blockIdx.x * kWaves + wid;
+  Pair<DT> dy_next{}, x_next{};
+  int t = 0, part = 0, pos = 0;
+  auto begin = [&]() {
+    if (it >= items) return;
+    t = (int)(it / parts);
+    part = (int)(it - (int64_t)t * parts);
+    dy_next = load_dy(t, part * a.groups_per_wave);
+    x_next = load_x(t, part * a.groups_per_wave);
+    pos = a.pos ? a.pos[t] : t;
+  };
+  begin();
+  stage_weights<LPH>(a, sh);
+  while (it < items) {
+    const int g0 = part * a.groups_per_wave, g1 = min(groups, g0 + a.groups_per_wave);
     float cs[8], sn[8];
-    angles(a.freq, a.pos ? a.pos[t] : t, c, a.rot, a.inter, active, cs, sn);
-    const int g1 = min(groups, (part + 1) * a.groups_per_wave);
-    for (int gi = part * a.groups_per_wave; gi < g1; ++gi) {
+    turn_table(a.freq, pos, pairs, lane, sh.turn[wid]);
+    my_turns<MODE>(sh.turn[wid], l, pairs, cs, sn);
+    for (int gi = g0; gi < g1; ++gi) {
+      const Pair<DT> dy = dy_next, x = x_next;
+      if (gi + 1 < g1) {
+        dy_next = load_dy(t, gi + 1);
+        x_next = load_x(t, gi + 1);
+      }
       const int h = gi * RPW + sub;
-      const bool on = active && h < heads;
-      const bool is_q = h < a.hq, is_k = !is_q && h < a.hq + a.hkv, is_v = !is_q && !is_k;
-      const int hh = is_q ? h : h - a.hq - (is_k ? 0 : a.hkv);
-      const int64_t xoff = row_offset(a.x, t, min(h, heads - 1));
-      float u[8] = {}, dy[8] = {}, p[8] = {};
-      const char* w = is_q ? a.wq : a.wk;
-      if (on) {
-        const char* row = is_q ? a.pdq + row_offset(a.q, t, hh)
-                               : is_k ? a.pdk + row_offset(a.k, t, hh) : a.pdv + row_offset(a.v, t, hh);
-        widen<DT>(load_raw<DT>(row + c * 8 * ES), dy);
+      const bool is_q = h < a.hq, is_v = h >= a.hq + a.hkv;
+      Pair<DT> out = dy;
+      if (__any(!is_v)) {
+        float g[8], k[8];
+        widen<DT>(dy.a, g);
+        widen<DT>(dy.b, k);
+        if (MODE == APART) {
+          if (!is_v) {
+            turn_apart<DT>(g, dy_of(t, gi), qa, a.rot, sh.turn[wid], 1.0f, nullptr, -1.0f);
+            turn_apart<DT>(k, dy_of(t, gi), qb, a.rot, sh.turn[wid], 1.0f, nullptr, -1.0f);
+          }
+        } else {
+          turn<MODE>(g, k, cs, sn, -1.0f, pairs - 8 * l);
+        }
+        if (a.wq) {
+          float u[8], v[8];
+          widen<DT>(x.a, u);
+          widen<DT>(x.b, v);
+          float ss = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], fmaf(u[e], u[e], ss));
+          const float r = 1.0f / sqrtf(row_sum<LPH>(ss) / (float)a.d + a.eps);
+          const float* w = sh.w[is_q ? 0 : 1];
+          const bool is_k = !is_q && !is_v;
+          float dot = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            u[e] *= r;
+            v[e] *= r;
+            const float gu = g[e] * u[e], kv = k[e] * v[e];
+            dwq[e] = is_q ? dwq[e] + gu : dwq[e];
+            dwq[8 + e] = is_q ? dwq[8 + e] + kv : dwq[8 + e];
+            dwk[e] = is_k ? dwk[e] + gu : dwk[e];
+            dwk[8 + e] = is_k ? dwk[8 + e] + kv : dwk[8 + e];
+          }
+#pragma unroll
+          for (int e = 0; e < 8; e += 4) {
+            const float4 p = *reinterpret_cast<const float4*>(w + 8 * min(qa, LPH * 2 - 1) + e);
+            const float4 q = *reinterpret_cast<const float4*>(w + 8 * min(qb, LPH * 2 - 1) + e);
+            g[e] *= p.x, g[e + 1] *= p.y, g[e + 2] *= p.z, g[e + 3] *= p.w;
+            k[e] *= q.x, k[e + 1] *= q.y, k[e + 2] *= q.z, k[e + 3] *= q.w;
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dot = fmaf(k[e], v[e], fmaf(g[e], u[e], dot));
+          const float mean = row_sum<LPH>(dot) / (float)a.d;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            g[e] = r * fmaf(-u[e], mean, g[e]);
+            k[e] = r * fmaf(-v[e], mean, k[e]);
+          }
+        }
         if (!is_v) {
-          partners<DT>(row, mode, c, a.rot, dy, p);
-          if (w) widen<DT>(load_raw<DT>(a.px + xoff + c * 8 * ES), u);
+          out.a = narrow<DT>(g);
+          out.b = narrow<DT>(k);
         }
       }
-      float ss = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(u[e], u[e], ss);
-      ss = row_sum<LPH>(ss);
-      const bool normed = w && !is_v;
-      const float r = normed ? 1.0f / sqrtf(ss / (float)a.d + a.eps) : 1.0f;
-      float g[8], n[8], dot = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        g[e] = is_v ? dy[e] : fmaf(dy[e], cs[e], -p[e] * sn[e]);  // rotated by -a
-        n[e] = u[e] * r;
-        const float gn = g[e] * n[e];
-        dwq[e] += is_q && on ? gn : 0.0f;
-        dwk[e] += is_k && on ? gn : 0.0f;
-        g[e] *= normed ? (is_q ? wq[e] : wk[e]) : 1.0f;
-        dot = fmaf(g[e], n[e], dot);
-      }
-      const float mean = row_sum<LPH>(dot) / (float)a.d;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] = normed ? r * fmaf(-n[e], mean, g[e]) : g[e];
-      if (on) store_raw<DT>(a.pdx + xoff + c * 8 * ES, narrow<DT>(g));
+      if (h >= heads) continue;
+      char* dst = a.pdx + row_offset(a.x, t, h);
+      if (in_a) store_raw<DT>(dst + qa * 8 * ES, out.a);
+      if (in_b) store_raw<DT>(dst + qb * 8 * ES, out.b);
     }
+    __builtin_amdgcn_wave_barrier();
+    it += (int64_t)gridDim.x * kWaves;
+    begin();
   }
   if (!a.part) return;
   // over the wave's head rows, then over the workgroup's waves, in a fixed order
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < 16; ++e) {
 #pragma unroll
     for (int o = LPH; o < 64; o *= 2) {
       dwq[e] += __shfl_xor(dwq[e], o);
       dwk[e] += __shfl_xor(dwk[e], o);
     }
-    if (sub == 0) {
-      s_dw[wid][0][8 * c + e] = dwq[e];
-      s_dw[wid][1][8 * c + e] = dwk[e];
+    const int q = e < 8 ? qa : qb;
+    if (sub == 0 && 8 * q < a.d) {
+      s_dw[wid][0][8 * q + (e & 7)] = dwq[e];
+      s_dw[wid][1][8 * q + (e & 7)] = dwk[e];
     }
   }
   __syncthreads();
@@ -324,87 +450,99 @@ __global__ __launch_bounds__(kThreads) void heads_grad_kernel(const HeadsGradArg
   }
 }
 
-// Sums of the workgroups' parts: 16 columns and 16 strips of workgroups each.
+// Sums of the workgroups' parts: 8 columns and 32 strips of workgroups each.
 __global__ __launch_bounds__(kThreads) void heads_dw_kernel(const HeadsGradArgs a) {
-  __shared__ float s[16][16];
-  const int per = (a.d + 15) / 16;
-  const int kind = blockIdx.x / per, col = (blockIdx.x % per) * 16 + (threadIdx.x & 15);
-  const int strip = threadIdx.x >> 4;
+  __shared__ float s[32][8];
+  const int per = a.d / 8;
+  const int kind = blockIdx.x / per, col = (blockIdx.x % per) * 8 + (threadIdx.x & 7);
+  const int strip = threadIdx.x >> 3;
   float v = 0.0f;
-  if (col < a.d)
-#pragma unroll 4
-    for (int w = strip; w < a.n_wg; w += 16) v += a.part[((int64_t)w * 2 + kind) * a.d + col];
-  s[strip][threadIdx.x & 15] = v;
+  for (int w0 = strip; w0 < a.n_wg; w0 += 32 * 8) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = w0 + 32 * i < a.n_wg ? a.part[((int64_t)(w0 + 32 * i) * 2 + kind) * a.d + col] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += x[i];
+  }
+  s[strip][threadIdx.x & 7] = v;
   __syncthreads();
   char* out = kind ? a.dwk : a.dwq;
-  if (strip == 0 && col < a.d && out) {
-    for (int i = 1; i < 16; ++i) v += s[i][threadIdx.x];
+  if (strip == 0 && out) {
+    for (int i = 1; i < 32; ++i) v += s[i][threadIdx.x];
     st_elem(out, col, kind ? a.dwk_dt : a.dwq_dt, v);
   }
 }
 
-template <int LPH>
+template <int LPH, int MODE>
 hipError_t run_heads(const HeadsArgs& a, int32_t dt, int64_t grid, hipStream_t s) {
   const dim3 g((uint32_t)grid), b(kThreads);
-  if (dt == EA_F32) heads_kernel<LPH, EA_F32><<<g, b, 0, s>>>(a);
-  else if (dt == EA_BF16) heads_kernel<LPH, EA_BF16><<<g, b, 0, s>>>(a);
-  else heads_kernel<LPH, EA_F16><<<g, b, 0, s>>>(a);
+  if (dt == EA_F32) heads_kernel<LPH, EA_F32, MODE><<<g, b, 0, s>>>(a);
+  else if (dt == EA_BF16) heads_kernel<LPH, EA_BF16, MODE><<<g, b, 0, s>>>(a);
+  else heads_kernel<LPH, EA_F16, MODE><<<g, b, 0, s>>>(a);
   return hipGetLastError();
 }
-template <int LPH>
-hipError_t run_heads_grad(const HeadsGradArgs& a, int32_t dt, hipStream_t s) {
-  const dim3 g((uint32_t)a.n_wg), b(kThreads);
-  if (dt == EA_F32) heads_grad_kernel<LPH, EA_F32><<<g, b, 0, s>>>(a);
-  else if (dt == EA_BF16) heads_grad_kernel<LPH, EA_BF16><<<g, b, 0, s>>>(a);
-  else heads_grad_kernel<LPH, EA_F16><<<g, b, 0, s>>>(a);
+template <int LPH, int MODE>
+hipError_t run_heads(const HeadsGradArgs& a, int32_t dt, int64_t grid, hipStream_t s) {
+  const dim3 g((uint32_t)grid), b(kThreads);
+  if (dt == EA_F32) heads_grad_kernel<LPH, EA_F32, MODE><<<g, b, 0, s>>>(a);
+  else if (dt == EA_BF16) heads_grad_kernel<LPH, EA_BF16, MODE><<<g, b, 0, s>>>(a);
+  else heads_grad_kernel<LPH, EA_F16, MODE><<<g, b, 0, s>>>(a);
   return hipGetLastError();
 }
 
-// Lanes of a head row: 8 elements each, a power of two from 8 up.
+// Lanes of a head row: 16 elements each, a power of two from 4 up.
 int lanes_of(int d) {
-  int n = 8;
-  while (n * 8 < d) n *= 2;
+  int n = 4;
+  while (n * 16 < d) n *= 2;
   return n;
+}
+
+// Workgroups of a launch, and the groups of heads that a wave walks for one
+// token: so many that the launch is one round of the `waves` a CU that its
+// registers admit, up to all of a token's.
+template <class A>
+int64_t split(A* a, int waves) {
+  const int rpw = 64 / lanes_of(a->d), groups = (a->hq + 2 * a->hkv + rpw - 1) / rpw;
+  const int64_t gpw = ((int64_t)a->t * groups + waves * 256 - 1) / (waves * 256);
+  a->groups_per_wave = (int32_t)(gpw > groups ? groups : gpw);
+  const int64_t parts = (groups + a->groups_per_wave - 1) / a->groups_per_wave;
+  return ((int64_t)a->t * parts + kWaves - 1) / kWaves;
+}
+
+template <int LPH, class A>
+hipError_t run_mode(const A& a, int32_t dt, int64_t grid, hipStream_t s) {
+  if (a.inter || a.rot == 0) return run_heads<LPH, NEIGHBOURS>(a, dt, grid, s);
+  if ((a.rot / 2) % 8) return run_heads<LPH, APART>(a, dt, grid, s);
+  return run_heads<LPH, HALVES>(a, dt, grid, s);
+}
+template <class A>
+hipError_t run_any(const A& a, int32_t dt, int64_t grid, hipStream_t s) {
+  switch (lanes_of(a.d)) {
+    case 4: return run_mode<4>(a, dt, grid, s);
+    case 8: return run_mode<8>(a, dt, grid, s);
+    case 16: return run_mode<16>(a, dt, grid, s);
+    default: return run_mode<32>(a, dt, grid, s);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_heads(const HeadsArgs& a0, int32_t dt, hipStream_t s) {
   HeadsArgs a = a0;
-  const int lph = lanes_of(a.d), rpw = 64 / lph;
-  const int groups = (a.hq + 2 * a.hkv + rpw - 1) / rpw;
-  // As many groups a wave as leave eight waves a CU to hide the loads.
-  int64_t gpw = (int64_t)a.t * groups / (8 * 256);
-  a.groups_per_wave = (int32_t)(gpw < 1 ? 1 : gpw > groups ? groups : gpw);
-  const int64_t parts = (groups + a.groups_per_wave - 1) / a.groups_per_wave;
-  const int64_t wgs = ((int64_t)a.t * parts + kWaves - 1) / kWaves;
-  const int64_t grid = wgs < kHeadsMaxWg ? wgs : kHeadsMaxWg;
-  switch (lph) {
-    case 8: return run_heads<8>(a, dt, grid, s);
-    case 16: return run_heads<16>(a, dt, grid, s);
-    case 32: return run_heads<32>(a, dt, grid, s);
-    default: return run_heads<64>(a, dt, grid, s);
-  }
+  const int64_t wgs = split(&a, 16);
+  return run_any(a, dt, wgs < kHeadsMaxWg ? wgs : kHeadsMaxWg, s);
 }
 
 hipError_t launch_heads_grad(const HeadsGradArgs& a0, int32_t dt, hipStream_t s) {
   HeadsGradArgs a = a0;
-  const int lph = lanes_of(a.d), rpw = 64 / lph;
-  const int groups = (a.hq + 2 * a.hkv + rpw - 1) / rpw;
-  int64_t gpw = (int64_t)a.t * groups / (8 * 256);
-  a.groups_per_wave = (int32_t)(gpw < 1 ? 1 : gpw > groups ? groups : gpw);
-  const int64_t parts = (groups + a.groups_per_wave - 1) / a.groups_per_wave;
-  const int64_t wgs = ((int64_t)a.t * parts + kWaves - 1) / kWaves;
-  a.n_wg = (int32_t)(wgs < kHeadsGradMaxWg ? wgs : kHeadsGradMaxWg);
-  hipError_t e;
-  switch (lph) {
-    case 8: e = run_heads_grad<8>(a, dt, s); break;
-    case 16: e = run_heads_grad<16>(a, dt, s); break;
-    case 32: e = run_heads_grad<32>(a, dt, s); break;
-    default: e = run_heads_grad<64>(a, dt, s); break;
-  }
+  // its registers admit three workgroups a CU (two in f32): more would wait
+  // for a second round and leave the chip half empty
+  const int64_t most = dt == EA_F32 ? 512 : kHeadsGradMaxWg;
+  const int64_t wgs = split(&a, dt == EA_F32 ? 8 : 12);
+  a.n_wg = (int32_t)(wgs < most ? wgs : most);
+  const hipError_t e = run_any(a, dt, a.n_wg, s);
   if (e != hipSuccess || !a.part) return e;
-  heads_dw_kernel<<<dim3(2 * ((a.d + 15) / 16)), dim3(kThreads), 0, s>>>(a);
+  heads_dw_kernel<<<dim3(2 * (a.d / 8)), dim3(kThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -196,6 +196,7 @@ class Relation:
             ptr = data.data_ptr() + self._byte_offset
             cap = data.numel() * data.element_size() - self._byte_offset
         nb, sp = _partition_args(self.partition)
+        self._device = -1 if data is None else data.get_device()
         h = ctypes.c_void_p()
         _check(lib().ea_relation_create(len(self.shape), _arr(ctypes.c_int64, self.shape), DTYPES[dtype], nb, sp,
                                         ctypes.c_void_p(ptr) if ptr else None, cap, ctypes.byref(h)))
@@ -386,6 +387,9 @@ PAGES_OK, PAGES_NONE_FREE, PAGES_TOO_LONG = 0, 1, 2  # status[0] of the page cal
 PAGED_MAX_SEQ = 4096  # EA_PAGED_MAX_SEQ
 
 
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _device_array(t, name: str, shape, dtype=torch.int32, optional: bool = False):
     """The address of a small device array, checked: type, shape (None: any
     extent), rows without gaps, on the current device."""
@@ -393,24 +397,26 @@ def _device_array(t, name: str, shape, dtype=torch.int32, optional: bool = False
         if optional:
             return None
         raise EAError(ERR_ARG, f"{name} is missing")
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
         raise EAError(ERR_ARG, f"{name} is no {dtype} tensor")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+    if t.shape != shape and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
         raise EAError(ERR_ARG, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if not t.is_contiguous():
         raise EAError(ERR_ARG, f"{name} is not contiguous")
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.get_device() != _get_device():
         raise EAError(ERR_ARG, f"{name} is on {t.device}, not on the current GPU")
     return t.data_ptr()
 
 
-def _on_device(**rels):
+def _on_device(*rels):
     """Relations whose data torch holds lie on the current device."""
-    for name, r in rels.items():
+    dev = None
+    for r in rels:
         if r is not None and r.data is not None:
-            d = r.data.device
-            if d.type != "cuda" or d.index != torch.cuda.current_device():
-                raise EAError(ERR_ARG, f"{name} is on {d}, not on the current GPU")
+            if dev is None:
+                dev = _get_device() if r._device >= 0 else -2
+            if r._device != dev:
+                raise EAError(ERR_ARG, f"a relation is on {r.data.device}, not on the current GPU")
 
 
 def _h(r):
@@ -445,7 +451,7 @@ def heads(qkv: Relation, q: Relation, k: Relation, v: Relation, *, d_head: int, 
     token-major [T, H d_head] or head-major [.., H, T, d_head]; with ``slots``
     k and v are the pages [pages, Hkv, page_size, d_head] of a cache and row t
     goes to slot slots[t] (-1: to none)."""
-    _on_device(qkv=qkv, q=q, k=k, v=v, wq=wq, wk=wk)
+    _on_device(qkv, q, k, v, wq, wk)
     prm = _heads_params(qkv.shape[0], d_head, eps, inv_freq, interleaved, positions, slots)
     _check(lib().ea_heads(qkv._h, _h(wq), _h(wk), q._h, k._h, v._h, ctypes.byref(prm), _stream(stream)))
 
@@ -457,7 +463,7 @@ def heads_backward(qkv: Relation, dq: Relation, dk: Relation, dv: Relation, dqkv
                    workspace: torch.Tensor | None = None) -> None:
     """The gradient of ``heads`` (without slots): ``dqkv`` in qkv's layout and,
     where wanted, the norm weights' ``dwq`` and ``dwk`` ([d_head])."""
-    _on_device(qkv=qkv, dq=dq, dk=dk, dv=dv, dqkv=dqkv, wq=wq, wk=wk, dwq=dwq, dwk=dwk)
+    _on_device(qkv, dq, dk, dv, dqkv, wq, wk, dwq, dwk)
     prm = _heads_params(qkv.shape[0], d_head, eps, inv_freq, interleaved, positions, None)
     s = _stream(stream)
     ws, n = None, 0
@@ -501,7 +507,7 @@ def attention_paged(q: Relation, k: Relation, v: Relation, out: Relation, *, sca
     and each one before it one less.  Groups of sequences group_start[g] ..
     group_start[g + 1] - 1 share their first group_shared[g] keys, which are
     read once.  The arrays are read when the kernels run."""
-    _on_device(q=q, k=k, v=v, out=out)
+    _on_device(q, k, v, out)
     b = _paged(scale, table, lengths, q_start, group_start, group_shared)
     s = _stream(stream)
     need = ctypes.c_int64()
@@ -542,7 +548,7 @@ def pages_extend(table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor,
 
 def _page_caches(caches):
     caches = list(caches)
-    _on_device(**{f"cache {i}": c for i, c in enumerate(caches)})
+    _on_device(*caches)
     return len(caches), _handles(caches), caches[0].shape[-2] if caches else None
 
 

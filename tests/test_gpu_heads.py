@@ -134,6 +134,18 @@ def test_heads_rows_are_independent():
     assert torch.equal(bad[1], clean[1]) and torch.equal(bad[2], clean[2])
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rotary", [16, 18])
+def test_elements_past_the_rotated_part_stay(rotary, interleaved):
+    """Without a norm an infinity among them reaches no other element."""
+    t, d = 3, 64
+    x, _, _, freq, _ = _inputs(t, 1, 1, d, rotary, "f32", False, 0, 12)
+    x[1, 40], x[1, rotary] = float("inf"), float("nan")
+    out = [torch.empty((t, d), device="cuda") for _ in range(3)]
+    ea.heads(R.rel(x), *[R.rel(o) for o in out], d_head=d, inv_freq=freq, interleaved=interleaved)
+    assert torch.equal(out[0][1, rotary + 1:], x[1, rotary + 1:d]) and torch.isfinite(out[0][1, :rotary]).all()
+
+
 GRAD = [
     (1, 1, 1, 8, 8, False, True, "f32", 0),
     (50, 4, 2, 128, 128, False, True, "bf16", 5000),
