@@ -247,12 +247,31 @@ int ea_heads_backward(const ea_relation* qkv, const ea_relation* wq, const ea_re
 
 namespace {
 
-// Checks what a paged call's workspace depends on; *cap: the units it holds.
-// Their number is at most the target, one more unit of every (tile, key-value
-// head) for its last chunk and seven paddings a tile; tiles of sequences and of
-// groups each cover the rows once.
-int paged_units(const ea_relation* q, const ea_relation* k, const ea_paged* b, bool need_data, RowMap* mq,
-                int64_t* cap) {
+// How a paged call walks its keys, and its workspace.
+struct PagedPlan {
+  PagedPass shared{}, own{};
+  int64_t bytes = 0;
+  int64_t seg = 0, ml[2] = {}, o[2] = {};  // offsets
+};
+
+// A pass over n segments of `cols` query columns in all.  Columns of a tile: as
+// many as a segment has on the average, up to 64 (each doubling reads the keys
+// half as often and computes as much); the registers then admit one workgroup
+// a CU, else two.  A segment's tiles are at most its columns / tile + 1, and a
+// walk's parts number the tiles and the workgroups.
+void plan_pass(PagedPass* p, int first, int n, int64_t cols, int64_t hkv) {
+  p->first = first;
+  p->n = n;
+  const int64_t avg = n ? cols / n : 0;
+  p->cols = avg > 32 ? 64 : avg > 16 ? 32 : 16;
+  p->grid = p->cols == 16 ? 512 : 256;
+  const int64_t slots = n ? (cols / p->cols + n) * hkv + p->grid : 0;
+  p->slots = (int32_t)(slots < INT32_MAX ? slots : INT32_MAX);
+}
+
+// Checks what a paged call's workspace depends on, and lays it out.
+int plan_paged(const ea_relation* q, const ea_relation* k, const ea_paged* b, bool need_data, RowMap* mq,
+               PagedPlan* p) {
   if (!b) return fail(EA_ERR_ARG, "NULL batch");
   int e;
   if ((e = check_rel(q, "q", need_data)) || (e = check_cache(k, "k", need_data, 0))) return e;
@@ -267,17 +286,19 @@ int paged_units(const ea_relation* q, const ea_relation* k, const ea_paged* b, b
     return fail(EA_ERR_UNSUPPORTED, "%d sequences and %d groups, at most %d", b->n_seq, b->n_group, EA_PAGED_MAX_SEQ);
   if ((int64_t)mq->t * mq->h > INT32_MAX) return fail(EA_ERR_UNSUPPORTED, "2^31 query rows and heads or more");
   const int64_t cols = (int64_t)mq->t * (mq->h / hkv);
-  const int64_t tiles = (b->n_group ? 2 : 1) * (cols / kPagedCols) + b->n_seq + b->n_group;
-  *cap = kPagedTarget + 64 + tiles * (hkv + 7);
-  if (*cap > INT32_MAX / kPagedCols) return fail(EA_ERR_UNSUPPORTED, "too many query rows in one call");
+  plan_pass(&p->shared, 0, b->n_group, cols, hkv);
+  plan_pass(&p->own, b->n_group, b->n_seq, cols, hkv);
+  p->seg = kWsCounterBytes;
+  int64_t at = p->seg + align256((b->n_seq + b->n_group) * (int64_t)sizeof(PagedSeg));
+  int i = 0;
+  for (const PagedPass* s : {&p->shared, &p->own}) {
+    p->ml[i] = at;
+    at += align256((int64_t)s->slots * s->cols * 2 * 4);
+    p->o[i++] = at;
+    at += align256((int64_t)s->slots * s->cols * d * 4);
+  }
+  p->bytes = at;
   return EA_OK;
-}
-
-int64_t paged_header(const ea_paged* b) {
-  return align256(b->n_seq * (int64_t)sizeof(PagedSeq)) + align256(b->n_group * (int64_t)sizeof(PagedGroup));
-}
-int64_t paged_bytes(const ea_paged* b, int64_t cap, int64_t d) {
-  return kWsCounterBytes + paged_header(b) + align256(cap * kPagedCols * 2 * 4) + cap * kPagedCols * d * 4;
 }
 
 }  // namespace
@@ -288,18 +309,18 @@ int ea_attention_paged_workspace(const ea_relation* q, const ea_relation* k, con
                                  int64_t* ws_bytes) {
   if (!ws_bytes) return fail(EA_ERR_ARG, "NULL ws_bytes");
   RowMap mq;
-  int64_t cap;
-  const int e = paged_units(q, k, batch, false, &mq, &cap);
+  PagedPlan p;
+  const int e = plan_paged(q, k, batch, false, &mq, &p);
   if (e) return e;
-  *ws_bytes = paged_bytes(batch, cap, k->shape[3]);
+  *ws_bytes = p.bytes;
   return ok();
 }
 
 int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_relation* v, ea_relation* out,
                        const ea_paged* batch, void* workspace, int64_t ws_bytes, void* stream) {
   PagedArgs a{};
-  int64_t cap;
-  int e = paged_units(q, k, batch, true, &a.q, &cap);
+  PagedPlan p;
+  int e = plan_paged(q, k, batch, true, &a.q, &p);
   if (e) return e;
   if ((e = check_cache(v, "v", true, 0)) || (e = check_rel(out, "out", true))) return e;
   if (v->dtype != k->dtype || out->dtype != k->dtype)
@@ -318,7 +339,7 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
   if (!b.q_start && a.q.t < b.n_seq) return fail(EA_ERR_ARG, "%d query rows for %d sequences", a.q.t, b.n_seq);
   for (const ea_relation* r : {q, k, v})
     if (overlap(out, r)) return fail(EA_ERR_ARG, "out overlaps an input");
-  const int64_t need = paged_bytes(batch, cap, d);
+  const int64_t need = p.bytes;
   if (!workspace || (uintptr_t)workspace % 256) return fail(EA_ERR_ARG, "workspace missing or not 256-byte aligned");
   if (ws_bytes < need)
     return fail(EA_ERR_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
@@ -343,14 +364,14 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
   a.gdiv = fast_div((uint32_t)a.g);
   a.page_bytes = page_bytes(k);
   a.scale = b.scale * 1.4426950408889634f;
-  a.cap = (int32_t)cap;
-  char* ws = (char*)workspace + kWsCounterBytes;
-  a.seq = (PagedSeq*)ws;
-  a.group = (PagedGroup*)(ws + align256(b.n_seq * (int64_t)sizeof(PagedSeq)));
-  ws += paged_header(batch);
-  a.part_ml = (float*)ws;
-  a.part_o = (float*)(ws + align256(cap * kPagedCols * 2 * 4));
-  EA_HIP_TRY(launch_paged(a, d, k->dtype, (hipStream_t)stream));
+  char* ws = (char*)workspace;
+  a.seg = (PagedSeg*)(ws + p.seg);
+  int i = 0;
+  for (PagedPass* s : {&p.shared, &p.own}) {
+    s->part_ml = (float*)(ws + p.ml[i]);
+    s->part_o = (float*)(ws + p.o[i++]);
+  }
+  EA_HIP_TRY(launch_paged(a, p.shared, p.own, d, k->dtype, (hipStream_t)stream));
   return ok();
 }
 

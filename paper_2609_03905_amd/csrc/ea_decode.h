@@ -93,19 +93,25 @@ hipError_t launch_heads_grad(const HeadsGradArgs& a, int32_t dtype, hipStream_t 
 
 // ---- attention over pages ------------------------------------------------------
 constexpr int kPagedMaxSeg = EA_PAGED_MAX_SEQ;  // sequences and groups of one call
-constexpr int kPagedCols = 16;                  // query columns of a tile
+constexpr int kPagedCols = 16;                  // query columns of a matrix tile
 constexpr int kPagedStep = 128;                 // keys that a workgroup takes at a time
-constexpr int kPagedTarget = 4096;              // units that the key split aims at
 
-struct PagedSeq {   // what the merge needs of a sequence
-  int32_t r0, r1;   // query rows
-  int32_t base;     // first unit of its own keys
-  int32_t chunks;   // key chunks of them
-  int32_t group;    // its group or -1
-  int32_t pad[3];
+struct PagedSeg {  // what the join needs of a segment
+  int32_t r0, r1;       // query rows
+  int32_t step, steps;  // first step of its first tile's walk; steps of a walk
+  int32_t tile, tiles;  // first tile; tiles of a head
+  int32_t group;        // own keys: the sequence's group or -1
+  int32_t total;        // steps of the launch
 };
-struct PagedGroup {
-  int32_t r0, base, chunks, tiles;
+
+// One launch of the walk: the groups' shared keys, or the sequences' own.
+struct PagedPass {
+  int32_t first, n;  // segments
+  int32_t grid;      // workgroups
+  int32_t cols;      // query columns of a tile: 16, 32 or 64
+  int32_t slots;     // partial results that the workspace holds
+  float* part_ml;    // [slots][cols][2]
+  float* part_o;     // [slots][cols][D]
 };
 
 struct PagedArgs {
@@ -117,13 +123,10 @@ struct PagedArgs {
   FastDiv page, gdiv;
   int64_t page_bytes;
   float scale;       // of the scores, log2 domain
-  int32_t cap;       // units that the workspace holds
-  PagedSeq* seq;
-  PagedGroup* group;
-  float* part_ml;    // [cap][16][2]
-  float* part_o;     // [cap][16][D]
+  PagedSeg* seg;     // groups, then sequences
 };
-hipError_t launch_paged(const PagedArgs& a, int32_t d, int32_t dtype, hipStream_t s);
+hipError_t launch_paged(const PagedArgs& a, const PagedPass& shared, const PagedPass& own, int32_t d, int32_t dtype,
+                        hipStream_t s);
 
 // ---- the page table -------------------------------------------------------------
 struct PagesArgs {
