@@ -503,7 +503,7 @@ int ea_heads_backward(const ea_relation* qkv, const ea_relation* wq, const ea_re
    keys; a key whose page lies outside the cache is invisible.  Rows behind the
    last sequence's stay as they were.  Keys and values that a row does not see
    must be finite where the same call sees them in another row. */
-#define EA_PAGED_MAX_SEQ 4096
+#define EA_PAGED_MAX_SEQ 2048
 typedef struct ea_paged {
   float scale;                 /* of the scores: positive, finite                  */
   int32_t n_seq;
@@ -519,9 +519,9 @@ typedef struct ea_paged {
 /* q, out: [rows, Hq d] or [.., Hq, rows, d] (forms as ea_heads' q).  bf16 or
    f16, d 64 or 128; scores and sums in f32, weights rounded to the dtype for
    the product with V.  n_seq + n_group <= EA_PAGED_MAX_SEQ, rows * Hq < 2^31.
-   workspace: as ea_joinagg's, of at least ea_attention_paged_workspace's bytes
-   for these operands (its counter area stays untouched); asynchronous, never
-   allocates, deterministic.  Errors: EA_ERR_ARG, EA_ERR_DTYPE,
+   workspace: as ea_joinagg's (a zeroed counter area, left zero; the rest needs
+   no initial value), of at least ea_attention_paged_workspace's bytes for these
+   operands; asynchronous, never allocates, deterministic.  Errors: EA_ERR_ARG, EA_ERR_DTYPE,
    EA_ERR_UNSUPPORTED, EA_ERR_CAPACITY, EA_ERR_HIP. */
 int ea_attention_paged_workspace(const ea_relation* q, const ea_relation* k, const ea_paged* batch, int64_t* ws_bytes);
 int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_relation* v, ea_relation* out,

@@ -251,22 +251,24 @@ namespace {
 struct PagedPlan {
   PagedPass shared{}, own{};
   int64_t bytes = 0;
-  int64_t seg = 0, ml[2] = {}, o[2] = {};  // offsets
+  int64_t seg = 0, lim = 0, ml[2] = {}, o[2] = {};  // offsets
 };
 
-// A pass over n segments of `cols` query columns in all.  Columns of a tile: as
-// many as a segment has on the average, up to 64 (each doubling reads the keys
-// half as often and computes as much); the registers then admit one workgroup
-// a CU, else two.  A segment's tiles are at most its columns / tile + 1, and a
-// walk's parts number the tiles and the workgroups.
-void plan_pass(PagedPass* p, int first, int n, int64_t cols, int64_t hkv) {
+// A pass over n segments of `cols` query columns in all, by the columns that a
+// segment has on the average: up to 16 or 32, the walk that loads keys into
+// registers (at 32 columns of width 128 its registers admit one workgroup a
+// CU); beyond, the walk through shared memory, on tiles of 64 or 128 columns,
+// a step on the narrower costing about 0.55 of one on the wider.
+void plan_pass(PagedPass* p, bool shared, int first, int n, int64_t cols, int64_t hkv, int64_t d) {
+  p->shared = shared;
   p->first = first;
   p->n = n;
-  const int64_t avg = n ? cols / n : 0;
-  p->cols = avg > 32 ? 64 : avg > 16 ? 32 : 16;
-  p->grid = p->cols == 16 ? 512 : 256;
-  const int64_t slots = n ? (cols / p->cols + n) * hkv + p->grid : 0;
-  p->slots = (int32_t)(slots < INT32_MAX ? slots : INT32_MAX);
+  const int64_t avg = n ? (cols + n - 1) / n : 0;
+  if (avg <= 32) p->cols = avg > 16 ? 32 : 16;
+  else p->cols = 0.55 * (double)((avg + 63) / 64) < (double)((avg + 127) / 128) ? 64 : 128;
+  p->grid = p->cols == 32 && d == 128 ? 256 : 512;
+  const int64_t tiles = (cols / p->cols + n) * hkv;
+  p->tiles = (int32_t)(tiles < INT32_MAX ? tiles : INT32_MAX);
 }
 
 // Checks what a paged call's workspace depends on, and lays it out.
@@ -286,16 +288,21 @@ int plan_paged(const ea_relation* q, const ea_relation* k, const ea_paged* b, bo
     return fail(EA_ERR_UNSUPPORTED, "%d sequences and %d groups, at most %d", b->n_seq, b->n_group, EA_PAGED_MAX_SEQ);
   if ((int64_t)mq->t * mq->h > INT32_MAX) return fail(EA_ERR_UNSUPPORTED, "2^31 query rows and heads or more");
   const int64_t cols = (int64_t)mq->t * (mq->h / hkv);
-  plan_pass(&p->shared, 0, b->n_group, cols, hkv);
-  plan_pass(&p->own, b->n_group, b->n_seq, cols, hkv);
+  plan_pass(&p->shared, true, 0, b->n_group, cols, hkv, d);
+  plan_pass(&p->own, false, b->n_group, b->n_seq, cols, hkv, d);
+  // without groups, and few tiles enough for the arrival counters, the last
+  // part of a tile joins them and no second launch follows
+  p->own.fused = b->n_group == 0 && p->own.cols <= 32 && p->own.tiles <= kWsCounterBytes / 4;
   p->seg = kWsCounterBytes;
-  int64_t at = p->seg + align256((b->n_seq + b->n_group) * (int64_t)sizeof(PagedSeg));
+  p->lim = p->seg + align256((b->n_seq + b->n_group) * (int64_t)sizeof(PagedSeg));
+  int64_t at = p->lim + (b->n_group ? align256((int64_t)mq->t * 4) : 0);
   int i = 0;
   for (const PagedPass* s : {&p->shared, &p->own}) {
+    const int64_t slots = s->n ? (int64_t)s->tiles + s->grid : 0;
     p->ml[i] = at;
-    at += align256((int64_t)s->slots * s->cols * 2 * 4);
+    at += align256(slots * s->cols * 2 * 4);
     p->o[i++] = at;
-    at += align256((int64_t)s->slots * s->cols * d * 4);
+    at += align256(slots * s->cols * d * 4);
   }
   p->bytes = at;
   return EA_OK;
@@ -366,6 +373,8 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
   a.scale = b.scale * 1.4426950408889634f;
   char* ws = (char*)workspace;
   a.seg = (PagedSeg*)(ws + p.seg);
+  a.row_lim = (int32_t*)(ws + p.lim);
+  p.own.counters = (int32_t*)ws;
   int i = 0;
   for (PagedPass* s : {&p.shared, &p.own}) {
     s->part_ml = (float*)(ws + p.ml[i]);

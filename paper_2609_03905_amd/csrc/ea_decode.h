@@ -95,6 +95,7 @@ hipError_t launch_heads_grad(const HeadsGradArgs& a, int32_t dtype, hipStream_t 
 constexpr int kPagedMaxSeg = EA_PAGED_MAX_SEQ;  // sequences and groups of one call
 constexpr int kPagedCols = 16;                  // query columns of a matrix tile
 constexpr int kPagedStep = 128;                 // keys that a workgroup takes at a time
+constexpr int kPagedWideStep = 64;              // and with many columns
 
 struct PagedSeg {  // what the join needs of a segment
   int32_t r0, r1;       // query rows
@@ -107,11 +108,14 @@ struct PagedSeg {  // what the join needs of a segment
 // One launch of the walk: the groups' shared keys, or the sequences' own.
 struct PagedPass {
   int32_t first, n;  // segments
+  int32_t shared;    // the groups' pass
   int32_t grid;      // workgroups
-  int32_t cols;      // query columns of a tile: 16, 32 or 64
-  int32_t slots;     // partial results that the workspace holds
-  float* part_ml;    // [slots][cols][2]
-  float* part_o;     // [slots][cols][D]
+  int32_t cols;      // query columns of a tile: 16, 32, 64 or 128
+  int32_t fused;     // the walk joins its results itself (no groups)
+  int32_t* counters; // fused: arrivals at every tile, zero between calls
+  int32_t tiles;     // the most that ascending query rows can have
+  float* part_ml;    // [tiles + grid][cols][2]
+  float* part_o;     // [tiles + grid][cols][D]
 };
 
 struct PagedArgs {
@@ -124,6 +128,7 @@ struct PagedArgs {
   int64_t page_bytes;
   float scale;       // of the scores, log2 domain
   PagedSeg* seg;     // groups, then sequences
+  int32_t* row_lim;  // keys that a query row sees
 };
 hipError_t launch_paged(const PagedArgs& a, const PagedPass& shared, const PagedPass& own, int32_t d, int32_t dtype,
                         hipStream_t s);

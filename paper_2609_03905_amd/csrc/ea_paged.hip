@@ -87,8 +87,6 @@ __device__ __forceinline__ int xcd_part(int b, int n) {
   return x * per + min(x, more) + (b >> 3);
 }
 
-constexpr int64_t kMost = 0x7fffffff;
-
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
 // First query row of sequence s (0 <= s <= n_seq).
@@ -99,9 +97,12 @@ __device__ __forceinline__ int first_row(const PagedArgs& a, int s) {
 struct Segment {
   int r0, r1;  // query rows
   int k0, k1;  // keys
-  int seq;     // whose table row lists the pages
-  int group;   // own keys: the sequence's group or -1
 };
+
+// The sequence whose table row lists a segment's pages.
+__device__ __forceinline__ int table_row(const PagedArgs& a, const PagedPass& ps, int i) {
+  return ps.shared ? clampi(a.group_start[i], 0, a.n_seq - 1) : i;
+}
 
 // Keys that group g shares (no more than a table row holds).
 __device__ __forceinline__ int shared_keys(const PagedArgs& a, int g) {
@@ -121,95 +122,162 @@ __device__ __forceinline__ int group_of(const PagedArgs& a, int s) {
   return lo;
 }
 
+// Segment i: the groups, then the sequences.
 __device__ __forceinline__ Segment segment(const PagedArgs& a, int i) {
   Segment s;
   if (i < a.n_group) {
     const int s0 = clampi(a.group_start[i], 0, a.n_seq), s1 = clampi(a.group_start[i + 1], s0, a.n_seq);
-    s.seq = min(s0, a.n_seq - 1);
     s.r0 = first_row(a, s0);
     s.r1 = max(first_row(a, s1), s.r0);
     s.k0 = 0;
     s.k1 = shared_keys(a, i);
-    s.group = -1;
   } else {
-    s.seq = i - a.n_group;
-    s.r0 = first_row(a, s.seq);
-    s.r1 = max(first_row(a, s.seq + 1), s.r0);
-    s.k1 = clampi(a.len[s.seq], 0, a.stride * a.page_size);
-    s.group = group_of(a, s.seq);
-    s.k0 = s.group >= 0 ? min(shared_keys(a, s.group), s.k1) : 0;
+    const int seq = i - a.n_group, g = group_of(a, seq);
+    s.r0 = first_row(a, seq);
+    s.r1 = max(first_row(a, seq + 1), s.r0);
+    s.k1 = clampi(a.len[seq], 0, a.stride * a.page_size);
+    s.k0 = g >= 0 ? min(shared_keys(a, g), s.k1) : 0;
   }
   return s;
 }
 
-__device__ __forceinline__ int tiles_of(const PagedArgs& a, const Segment& s, int cols) {
-  return (int)(((int64_t)(s.r1 - s.r0) * a.g + cols - 1) / cols);
+// A segment as the walk needs it, kept in shared memory (one more at the end
+// holds the totals).
+struct Seg {
+  int r0, rows;    // query rows
+  int k0, k1;      // keys
+  int step, tile;  // first step and first tile
+};
+
+__device__ __forceinline__ int add_most(int a, int b) { return (int)min((int64_t)a + b, (int64_t)0x7fffffff); }
+
+// Inclusive sums over a wave's lanes, no larger than 2^31 - 1.
+__device__ __forceinline__ int wave_scan(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int u = __shfl_up(v, o);
+    if (lane >= o) v = add_most(v, u);
+  }
+  return v;
 }
-__device__ __forceinline__ int steps_of(const Segment& s) { return (s.k1 - s.k0 + kPagedStep - 1) / kPagedStep; }
+
+__device__ __forceinline__ int steps_of(int k0, int k1, int keys) {
+  return (int)(((int64_t)k1 - k0 + keys - 1) / keys);
+}
+__device__ __forceinline__ int tiles_of(int rows, int g, int cols) {
+  return (int)(((int64_t)rows * g + cols - 1) / cols);
+}
+
+// Every segment's first step and tile, by the whole workgroup.  Also hands the
+// join what it needs and, from the sequences' pass, the shared pass every
+// query row's limit (the number of keys it sees).  Returns the steps of all.
+template <int D, int COLS, int KEYS>
+__device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps, Seg* seg) {
+  __shared__ int s_wave[kWaves][2];
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int per = (ps.n + kThreads - 1) / kThreads;
+  const int i0 = min(ps.n, tid * per), i1 = min(ps.n, i0 + per);
+  int steps = 0, ntile = 0;
+  for (int i = i0; i < i1; ++i) {
+    const Segment s = segment(a, ps.first + i);
+    const int n = steps_of(s.k0, s.k1, KEYS);
+    const int64_t t = n ? (int64_t)tiles_of(s.r1 - s.r0, a.g, COLS) * a.hkv : 0;
+    Seg x;
+    x.r0 = s.r0, x.rows = s.r1 - s.r0, x.k0 = s.k0, x.k1 = s.k1, x.step = steps, x.tile = ntile;
+    seg[i] = x;
+    steps = (int)min((int64_t)steps + n * t, (int64_t)0x7fffffff);
+    ntile = (int)min((int64_t)ntile + t, (int64_t)0x7fffffff);
+  }
+  int st = wave_scan(steps), ti = wave_scan(ntile);
+  if (lane == 63) {
+    s_wave[wid][0] = st;
+    s_wave[wid][1] = ti;
+  }
+  __syncthreads();
+  for (int w = 0; w < wid; ++w) {
+    st = add_most(st, s_wave[w][0]);
+    ti = add_most(ti, s_wave[w][1]);
+  }
+  if (tid == kThreads - 1) {
+    seg[ps.n].step = st;
+    seg[ps.n].tile = ti;
+  }
+  for (int i = i0; i < i1; ++i) {
+    seg[i].step = add_most(seg[i].step, st - steps);
+    seg[i].tile = add_most(seg[i].tile, ti - ntile);
+  }
+  __syncthreads();
+  // more tiles than the rows can have: the sequences' rows overlap, no walk
+  const bool off = seg[ps.n].tile > ps.tiles;
+  const int total = off ? 0 : seg[ps.n].step;
+  for (int i = blockIdx.x; i < ps.n; i += gridDim.x) {
+    const Seg s = seg[i];
+    if (ps.fused) {  // rows of a sequence without keys: no walk reaches them
+      if (s.k1 > 0) continue;
+      const int n = a.hkv * a.g * (D / 8);
+      for (int j = tid; j < s.rows * n; j += kThreads) {
+        const int r = j / n, x = j - r * n;
+        *reinterpret_cast<uint4*>(a.po + row_offset(a.o, s.r0 + r, x / (D / 8)) + x % (D / 8) * 16) =
+            make_uint4(0, 0, 0, 0);
+      }
+      continue;
+    }
+    if (tid == 0) {
+      PagedSeg g;
+      g.r0 = s.r0, g.r1 = s.r0 + s.rows, g.step = s.step, g.steps = off ? 0 : steps_of(s.k0, s.k1, KEYS);
+      g.tile = s.tile, g.tiles = tiles_of(s.rows, a.g, COLS), g.group = ps.shared ? -1 : group_of(a, i);
+      g.total = total;
+      a.seg[ps.first + i] = g;
+    }
+    if (a.n_group && !ps.shared)
+      for (int r = tid; r < s.rows; r += kThreads) a.row_lim[s.r0 + r] = s.k1 - s.rows + r + 1;
+  }
+  return total;
+}
+
+// The segment that step `at` belongs to (empty ones share a step).
+__device__ __forceinline__ int find_segment(const Seg* seg, int n, int at) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (seg[mid].step <= at) lo = mid;
+    else hi = mid;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Keys that query row `row`, the rr-th of segment s, sees.
+__device__ __forceinline__ int limit_of(const PagedArgs& a, const PagedPass& ps, const Seg& s, int row, int rr) {
+  return ps.shared ? a.row_lim[row] : s.k1 - s.rows + rr + 1;
+}
+
+// VE neighbouring elements of an output row, scaled.
+template <int VE, bool BF>
+__device__ __forceinline__ void store_row(char* dst, const float (&o)[VE], float scale) {
+  uint32_t x[VE / 2];
+#pragma unroll
+  for (int j = 0; j < VE; j += 2) x[j / 2] = pack2<BF>(o[j] * scale, o[j + 1] * scale);
+  if constexpr (VE == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
+  else *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
+}
 
 template <int D, bool BF, int NC>
-__global__ __launch_bounds__(kThreads, NC > 1 ? 1 : 2) void paged_kernel(const PagedArgs a, const PagedPass ps) {
+__global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kernel(const PagedArgs a, const PagedPass ps) {
   constexpr int VE = D / 16;          // d elements a lane holds of a V row
   constexpr int KS = D / 32;          // k steps of the score product
   constexpr int PITCH = D + 4;        // of a column in the waves' join (banks)
   constexpr int COLS = kPagedCols * NC;
-  __shared__ int s_step[kPagedMaxSeg + 1];  // first step of every segment
-  __shared__ int s_tile[kPagedMaxSeg + 1];  // and its first tile
+  extern __shared__ __attribute__((aligned(16))) char dyn[];
+  Seg* seg = reinterpret_cast<Seg*>(dyn);
   __shared__ int64_t s_off[kWaves][2][32];
   __shared__ __attribute__((aligned(16))) float s_o[kWaves][kPagedCols][PITCH];
   __shared__ float s_ml[kWaves][kPagedCols][2];
-  __shared__ int64_t s_sum[kThreads][2];
+  __shared__ int s_last;
 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int nseg = ps.n;
-  const int per = (nseg + kThreads - 1) / kThreads;
-
-  // ---- the schedule: every segment's first step and tile
-  int64_t steps = 0, ntile = 0;
-  for (int i = tid * per; i < min(nseg, (tid + 1) * per); ++i) {
-    const Segment s = segment(a, ps.first + i);
-    const int n = steps_of(s), t = n ? tiles_of(a, s, COLS) * a.hkv : 0;
-    s_step[i] = (int)min(steps, kMost);
-    s_tile[i] = (int)min(ntile, kMost);
-    steps = min(steps + (int64_t)n * t, kMost);
-    ntile = min(ntile + t, kMost);
-  }
-  s_sum[tid][0] = steps;
-  s_sum[tid][1] = ntile;
-  __syncthreads();
-  for (int o = 1; o < kThreads && o < nseg; o *= 2) {
-    const int64_t x = tid >= o ? s_sum[tid - o][0] : 0, y = tid >= o ? s_sum[tid - o][1] : 0;
-    __syncthreads();
-    s_sum[tid][0] = min(s_sum[tid][0] + x, kMost);
-    s_sum[tid][1] = min(s_sum[tid][1] + y, kMost);
-    __syncthreads();
-  }
-  const int64_t step0 = tid ? s_sum[tid - 1][0] : 0, tile0 = tid ? s_sum[tid - 1][1] : 0;
-  for (int i = tid * per; i < min(nseg, (tid + 1) * per); ++i) {
-    s_step[i] = (int)min(s_step[i] + step0, kMost);
-    s_tile[i] = (int)min(s_tile[i] + tile0, kMost);
-  }
-  // with fewer segments than threads the scan stops early: the last one has all
-  const int last = min(kThreads, (nseg + per - 1) / per) - 1;
-  if (tid == 0) {
-    s_step[nseg] = (int)s_sum[last][0];
-    s_tile[nseg] = (int)s_sum[last][1];
-  }
-  __syncthreads();
-  const int total = s_step[nseg];
-  const int parts = min((int)gridDim.x, total);
-  if (blockIdx.x == 0) {  // for the join
-    for (int i = tid; i < nseg; i += kThreads) {
-      const Segment s = segment(a, ps.first + i);
-      PagedSeg g;
-      g.r0 = s.r0, g.r1 = s.r1, g.step = s_step[i], g.steps = steps_of(s), g.tile = s_tile[i];
-      g.tiles = tiles_of(a, s, COLS), g.group = s.group, g.total = total;
-      a.seg[ps.first + i] = g;
-    }
-  }
-  // part w of `parts` for this workgroup: neighbours on one XCD (workgroup b
-  // runs on XCD b mod 8)
+  const int total = schedule<D, COLS, kPagedStep>(a, ps, seg), parts = min((int)gridDim.x, total);
   if ((int)blockIdx.x >= parts) return;
   const int w = xcd_part(blockIdx.x, parts);
   int at = (int)((int64_t)total * w / parts);
@@ -217,28 +285,21 @@ __global__ __launch_bounds__(kThreads, NC > 1 ? 1 : 2) void paged_kernel(const P
 
   while (at < end) {
     // ---- which tile, and how far this part walks it
-    int lo = 0, hi = nseg;  // s_step[lo] <= at < s_step[hi]; empty segments share a step
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (s_step[mid] <= at) lo = mid;
-      else hi = mid;
-    }
-    const int si = __builtin_amdgcn_readfirstlane(lo);
-    const Segment s = segment(a, ps.first + si);
-    const bool shared = ps.first + si < a.n_group;
-    const int n = steps_of(s), tiles = tiles_of(a, s, COLS);
-    const int local = at - s_step[si], it = local / n, step = local - it * n;
+    const int si = find_segment(seg, ps.n, at);
+    const Seg s = seg[si];
+    const int n = steps_of(s.k0, s.k1, kPagedStep), tiles = tiles_of(s.rows, a.g, COLS);
+    const int local = at - s.step, it = local / n, step = local - it * n;
     const int h = it / tiles, tile = it - h * tiles;
     const int walk = min(n - step, end - at);
-    const int slot_out = s_tile[si] + it + w;
+    const int slot_out = s.tile + it + w;
     // the only result of these columns: no join
-    const bool whole = !shared && walk == n && (s.group < 0 || s.k0 == 0);
+    const bool whole = !ps.shared && walk == n && s.k0 == 0;
     const int ka = s.k0 + step * kPagedStep;
     const int kb = (int)min((int64_t)s.k1, (int64_t)ka + (int64_t)walk * kPagedStep);
     at += walk;
 
     // ---- this lane's columns: query rows and heads, and the keys they see
-    const int ncol = (s.r1 - s.r0) * a.g;
+    const int ncol = s.rows * a.g;
     int lim[NC], lim_min = 0x7fffffff;
     uint4 q[NC][KS];
 #pragma unroll
@@ -246,20 +307,7 @@ __global__ __launch_bounds__(kThreads, NC > 1 ? 1 : 2) void paged_kernel(const P
       const int col = tile * COLS + t * kPagedCols + c;
       const int cc = min(col, ncol - 1);
       const int rr = div_fast(cc, a.gdiv), row = s.r0 + rr, head = h * a.g + cc - rr * a.g;
-      if (!shared) {
-        lim[t] = s.k1 - (s.r1 - s.r0) + rr + 1;
-      } else {  // the row's own sequence says how far it sees
-        int l2 = clampi(a.group_start[si], 0, a.n_seq), h2 = clampi(a.group_start[si + 1], l2, a.n_seq);
-        while (h2 - l2 > 1) {
-          const int mid = (l2 + h2) >> 1;
-          if (first_row(a, mid) <= row) l2 = mid;
-          else h2 = mid;
-        }
-        l2 = min(l2, a.n_seq - 1);
-        const int ln = clampi(a.len[l2], 0, a.stride * a.page_size);
-        lim[t] = ln - (first_row(a, l2 + 1) - row) + 1;
-      }
-      if (col >= ncol) lim[t] = 0x7fffffff;  // never stored: no mask
+      lim[t] = col < ncol ? limit_of(a, ps, s, row, rr) : 0x7fffffff;  // (never stored: no mask)
       lim_min = min(lim_min, lim[t]);
       const char* p = a.pq + row_offset(a.q, row, head) + g4 * 16;
 #pragma unroll
@@ -270,7 +318,7 @@ __global__ __launch_bounds__(kThreads, NC > 1 ? 1 : 2) void paged_kernel(const P
     lim_min = min(lim_min, __shfl_xor(lim_min, 4));
     lim_min = __builtin_amdgcn_readfirstlane(min(lim_min, __shfl_xor(lim_min, 8)));
 
-    const int32_t* pages = a.table + (int64_t)s.seq * a.stride;
+    const int32_t* pages = a.table + (int64_t)table_row(a, ps, si) * a.stride;
     const int64_t head_off = (int64_t)h * a.page_size * D * 2;
     const char* kbase = a.pk + head_off + g4 * 16;
     const char* vbase = a.pv + head_off + c * VE * 2;
@@ -446,25 +494,382 @@ __global__ __launch_bounds__(kThreads, NC > 1 ? 1 : 2) void paged_kernel(const P
         if (col < ncol) {
           const int rr = div_fast(col, a.gdiv);
           const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-          char* dst = a.po + row_offset(a.o, s.r0 + rr, h * a.g + col - rr * a.g) + part * VE * 2;
-          uint32_t x[VE / 2];
-#pragma unroll
-          for (int j = 0; j < VE; j += 2) x[j / 2] = pack2<BF>(o[j] * inv, o[j + 1] * inv);
-          if constexpr (VE == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
-          else *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
+          store_row<VE, BF>(a.po + row_offset(a.o, s.r0 + rr, h * a.g + col - rr * a.g) + part * VE * 2, o, inv);
         }
-      } else if (slot_out < ps.slots) {
+      } else if (tile * COLS + t * kPagedCols + jc < ncol) {
         const int64_t to = (int64_t)slot_out * COLS + t * kPagedCols + jc;
-        if (part == 0) {
-          ps.part_ml[2 * to] = top;
-          ps.part_ml[2 * to + 1] = lt;
-        }
+        if (ps.fused) {  // read by another workgroup of this launch
+          if (part == 0) store_agent2(ps.part_ml + 2 * to, top, lt);
 #pragma unroll
-        for (int j = 0; j < VE; j += 4)
-          *reinterpret_cast<float4*>(ps.part_o + to * D + part * VE + j) =
-              make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+          for (int j = 0; j < VE; j += 2) store_agent2(ps.part_o + to * D + part * VE + j, o[j], o[j + 1]);
+        } else {
+          if (part == 0) {
+            ps.part_ml[2 * to] = top;
+            ps.part_ml[2 * to + 1] = lt;
+          }
+#pragma unroll
+          for (int j = 0; j < VE; j += 4)
+            *reinterpret_cast<float4*>(ps.part_o + to * D + part * VE + j) =
+                make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+        }
       }
       __syncthreads();
+    }
+    if (!ps.fused || whole) continue;
+
+    // ---- the last part of the tile to arrive joins them, in part order
+    const int64_t from = s.step + (int64_t)it * n;
+    const int w0 = (int)(((from + 1) * parts - 1) / total), w1 = (int)(((from + n) * parts - 1) / total);
+    drain_vmem();
+    __syncthreads();
+    int32_t* counter = ps.counters + s.tile + it;
+    if (tid == 0) {
+      const bool last = arrive_agent(counter) == w1 - w0;
+      if (last) reset_agent(counter);  // ready for the next call (stream-ordered)
+      s_last = last;
+    }
+    __syncthreads();
+    if (s_last) {
+      const int jc = tid >> 4, part = tid & 15;
+#pragma unroll
+      for (int t = 0; t < NC; ++t) {
+        const int col = tile * COLS + t * kPagedCols + jc;
+        if (col >= ncol) continue;
+        const int64_t first = (int64_t)(s.tile + it + w0) * COLS + t * kPagedCols + jc;
+        float m_all = -INFINITY, l_all = 0.0f, o[VE] = {};
+        for (int p0 = 0; p0 <= w1 - w0; p0 += 4) {  // four parts' loads at a time
+          float2 ml[4], x[4][VE / 2];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int64_t to = first + (int64_t)min(p0 + i, w1 - w0) * COLS;
+            ml[i] = load_agent2(ps.part_ml + 2 * to);
+#pragma unroll
+            for (int j = 0; j < VE; j += 2) x[i][j / 2] = load_agent2(ps.part_o + to * D + part * VE + j);
+          }
+          float top = m_all;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i].x);
+          const float use = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m_all - use);
+          m_all = top;
+          l_all *= keep;
+#pragma unroll
+          for (int j = 0; j < VE; ++j) o[j] *= keep;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (p0 + i > w1 - w0) break;
+            const float f = __builtin_amdgcn_exp2f(ml[i].x - use);
+            l_all = fmaf(ml[i].y, f, l_all);
+#pragma unroll
+            for (int j = 0; j < VE; j += 2) {
+              o[j] = fmaf(x[i][j / 2].x, f, o[j]);
+              o[j + 1] = fmaf(x[i][j / 2].y, f, o[j + 1]);
+            }
+          }
+        }
+        const int rr = div_fast(col, a.gdiv);
+        store_row<VE, BF>(a.po + row_offset(a.o, s.r0 + rr, h * a.g + col - rr * a.g) + part * VE * 2, o,
+                          l_all == 0.0f ? 0.0f : 1.0f / l_all);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---- the walk for many columns --------------------------------------------------
+// A workgroup's tile is 32 CW columns, 32 a wave (CW 4), or, for up to 64, two
+// waves of columns and two halves of every step's keys (CW 2).  With 64 columns
+// and more the keys' bytes arrive faster than the matrix cores use them, so a
+// step of 64 keys is fetched once for the workgroup, straight into shared
+// memory (one instruction 1 KiB, a lane 16 bytes, each from its own key row),
+// while the step before is computed; two workgroups share a CU, so that one's
+// softmax runs beside the other's products.
+//   S^T = K Q^T on 32x32x16: a lane holds one column's scores of 16 keys in 32
+//   O^T += V^T P^T: V^T through transposing reads; the product's k index 8 g + e
+//   stands for key 16 hh + 4 g + e (e < 4) or 16 hh + 8 + 4 g + e - 4, as the
+//   accumulators of S^T lie
+// 16-byte pieces of a row are XOR-swizzled so that the 16 rows of a K read, and
+// the 4 rows of a transposing V read, take different banks.
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+
+template <bool BF>
+__device__ __forceinline__ f32x16_t mfma32(const uint4& a, const uint4& b, const f32x16_t& c) {
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b),
+                                                   c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c,
+                                                  0, 0, 0);
+}
+
+template <int D>
+__device__ __forceinline__ int swz_k(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int swz_v(int r) { return D == 128 ? (2 * (r & 3)) ^ (8 * (r & 1)) : 4 * ((r >> 1) & 1); }
+
+// 16 bytes a lane from its own address to 1 KiB of shared memory at lds (wave
+// uniform).  Written as asm, so that the compiler does not wait for it at every
+// shared read; the kernel waits itself (vmcnt 0, then a barrier).
+__device__ __forceinline__ void load_to_lds(const char* p, uint32_t lds) {
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds);
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(to) : "memory", "m0");
+#pragma clang diagnostic pop
+}
+
+template <int D, bool BF, int CW>
+__global__ __launch_bounds__(kThreads, 2) void paged_wide_kernel(const PagedArgs a, const PagedPass ps) {
+  constexpr int COLS = 32 * CW, KEYS = kPagedWideStep;
+  constexpr int KT = CW / 2;          // 32-key tiles that a wave computes of a step
+  constexpr int NS = D / 16, ND = D / 32;
+  constexpr int CPR = D / 8;          // 16-byte pieces of a row
+  constexpr int RPI = 64 / CPR;       // rows of one load
+  constexpr int LPW = 16 / RPI;       // loads of a wave (16 rows) for K, and for V
+  constexpr int BUF = 2 * KEYS * D;   // elements of a step: K, then V
+  __shared__ __attribute__((aligned(1024))) uint16_t sKV[2 * BUF];
+  __shared__ int64_t s_off[2][KEYS];
+  extern __shared__ __attribute__((aligned(16))) char dyn[];
+  Seg* seg = reinterpret_cast<Seg*>(dyn);
+
+  const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, g = lane >> 5;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wc = wid % CW, wk = wid / CW;  // the wave's columns, and its part of a step's keys
+  const int total = schedule<D, COLS, KEYS>(a, ps, seg), parts = min((int)gridDim.x, total);
+  if ((int)blockIdx.x >= parts) return;
+  const int w = xcd_part(blockIdx.x, parts);
+  int at = (int)((int64_t)total * w / parts);
+  const int end = (int)((int64_t)total * (w + 1) / parts);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)sKV;
+
+  while (at < end) {
+    const int si = find_segment(seg, ps.n, at);
+    const Seg s = seg[si];
+    const int n = steps_of(s.k0, s.k1, KEYS), tiles = tiles_of(s.rows, a.g, COLS);
+    const int local = at - s.step, it = local / n, step = local - it * n;
+    const int h = it / tiles, tile = it - h * tiles;
+    const int walk = min(n - step, end - at);
+    const int slot_out = s.tile + it + w;
+    const bool whole = !ps.shared && walk == n && s.k0 == 0;
+    const int ka = s.k0 + step * KEYS;
+    const int kb = (int)min((int64_t)s.k1, (int64_t)ka + (int64_t)walk * KEYS);
+    at += walk;
+
+    const int32_t* pages = a.table + (int64_t)table_row(a, ps, si) * a.stride;
+    const int64_t head_off = (int64_t)h * a.page_size * D * 2;
+    const char* kbase = a.pk + head_off;
+    const char* vbase = a.pv + head_off;
+    // a wave fetches 16 of a step's rows; lane i (and i + 16, ...) looks after row i
+    const int my = wid * 16 + (lane & 15);
+    auto entry = [&](int k) { return k + my < kb ? pages[div_fast(k + my, a.page)] : -1; };
+    auto place = [&](int b, int k, int pg) {  // the rows' offsets; -1: no such row
+      const int key = k + my, in = key - div_fast(key, a.page) * a.page_size;
+      const int64_t off = (uint32_t)pg < (uint32_t)a.n_pages ? pg * a.page_bytes + (int64_t)in * (D * 2) : -1;
+      if (lane < 16) s_off[b][my] = off;
+      __builtin_amdgcn_wave_barrier();
+    };
+    // one of a step's 2 LPW loads of this wave: i < LPW a K piece, else a V piece
+    auto issue = [&](int b, int i) {
+      const int inst = wid * LPW + i % LPW, r = inst * RPI + lane / CPR;
+      const int64_t off = s_off[b][r];
+      const int sw = i < LPW ? swz_k<D>(r) : swz_v<D>(r);
+      const char* p = (i < LPW ? kbase : vbase) + (off < 0 ? 0 : off) + 16 * ((lane % CPR) ^ sw);
+      load_to_lds(p, lds0 + (b * BUF + (i < LPW ? 0 : KEYS * D)) * 2 + inst * 1024);
+    };
+    auto landed = [&](int b) {  // this wave's loads are there; rows that do not exist hold no value
+      asm volatile("" ::: "memory");
+      drain_vmem();
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < LPW; ++i) {
+        const int inst = wid * LPW + i, r = inst * RPI + lane / CPR;
+        if (s_off[b][r] < 0)
+          *reinterpret_cast<uint4*>(sKV + b * BUF + KEYS * D + inst * 512 + lane * 8) = make_uint4(0, 0, 0, 0);
+      }
+    };
+    int next_pg = entry(ka);
+    place(0, ka, next_pg);
+#pragma unroll
+    for (int i = 0; i < 2 * LPW; ++i) issue(0, i);
+    next_pg = entry(ka + KEYS);
+
+    // ---- this lane's column
+    const int ncol = s.rows * a.g, col = tile * COLS + wc * 32 + lq, cc = min(col, ncol - 1);
+    const int rr = div_fast(cc, a.gdiv), row = s.r0 + rr, head = h * a.g + cc - rr * a.g;
+    const int lim = col < ncol ? limit_of(a, ps, s, row, rr) : 0x7fffffff;  // (never stored: no mask)
+    const bool idle = tile * COLS + wc * 32 >= ncol;  // a wave without columns only fetches
+    uint4 q[NS];
+    {
+      const char* p = a.pq + row_offset(a.q, row, head) + g * 16;
+#pragma unroll
+      for (int i = 0; i < NS; ++i) q[i] = *reinterpret_cast<const uint4*>(p + i * 32);
+    }
+    int lim_min = lim;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) lim_min = min(lim_min, __shfl_xor(lim_min, o));
+    lim_min = __builtin_amdgcn_readfirstlane(lim_min);
+
+    f32x16_t acc[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i) acc[i] = f32x16_t{};
+    float m = -INFINITY, l = 0.0f;
+
+    auto compute = [&](int b, int k, bool full, auto&& load) {
+      const uint16_t* sK = sKV + b * BUF;
+      const uint16_t* sV = sK + KEYS * D;
+      f32x16_t sc[KT];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) sc[t] = f32x16_t{};
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        uint4 x[KT];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          const int r = 32 * (wk * KT + t) + lq;
+          x[t] = *reinterpret_cast<const uint4*>(sK + r * D + 8 * ((2 * i + g) ^ swz_k<D>(r)));
+        }
+        load(i);
+#pragma unroll
+        for (int t = 0; t < KT; ++t) sc[t] = mfma32<BF>(x[t], q[i], sc[t]);
+      }
+      __builtin_amdgcn_s_setprio(0);
+      if (!full) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int kk = 32 * (wk * KT + t) + 8 * (r >> 2) + 4 * g + (r & 3);
+            sc[t][r] = s_off[b][kk] >= 0 && k + kk < lim ? sc[t][r] : -INFINITY;
+          }
+      }
+      float mx = sc[0][0];
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[t][r]);
+      mx = fmaxf(mx, other32(mx)) * a.scale;
+      const float m_new = mx > m + kLazyMax || m == -INFINITY ? fmaxf(mx, m) : m;
+      const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+      if (__any(m_new != m)) {
+        const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) acc[i] *= alpha;
+      }
+      m = m_new;
+      const int gq = lane >> 4, li = lane & 15;
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[t][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][r], a.scale, -m_use));
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          uint4 p;
+          p.x = pack_p<BF>(sc[t][8 * hh], sc[t][8 * hh + 1], l);
+          p.y = pack_p<BF>(sc[t][8 * hh + 2], sc[t][8 * hh + 3], l);
+          p.z = pack_p<BF>(sc[t][8 * hh + 4], sc[t][8 * hh + 5], l);
+          p.w = pack_p<BF>(sc[t][8 * hh + 6], sc[t][8 * hh + 7], l);
+          const int k0 = 32 * (wk * KT + t) + 16 * hh + 4 * (gq >> 1) + (li >> 2);
+#pragma unroll
+          for (int i = 0; i < ND; ++i) {
+            const int d = 32 * i + 16 * (gq & 1) + 4 * (li & 3);
+            auto tr = [&](int r) {
+              return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(
+                  sV + r * D + 8 * ((d >> 3) ^ swz_v<D>(r)) + (d & 4)));
+            };
+            const s16x8_t v = __builtin_shufflevector(tr(k0), tr(k0 + 8), 0, 1, 2, 3, 4, 5, 6, 7);
+            acc[i] = mfma32<BF>(__builtin_bit_cast(uint4, v), p, acc[i]);
+          }
+        }
+      __builtin_amdgcn_s_setprio(0);
+    };
+
+    landed(0);
+    __syncthreads();
+    int b = 0;
+    for (int k = ka; k < kb; k += KEYS, b ^= 1) {
+      const bool more = k + KEYS < kb;
+      if (more) {
+        place(b ^ 1, k + KEYS, next_pg);
+        next_pg = entry(k + 2 * KEYS);
+      }
+      if (idle) {
+#pragma unroll
+        for (int i = 0; i < 2 * LPW; ++i)
+          if (more) issue(b ^ 1, i);
+      } else {
+        const bool full = k + KEYS <= lim_min && __all(s_off[b][lane] >= 0);
+        compute(b, k, full, [&](int i) {
+          if (more) issue(b ^ 1, i);
+        });
+      }
+      if (more) landed(b ^ 1);
+      __syncthreads();
+    }
+    l += other32(l);
+
+    // ---- CW 2: the halves of the keys meet in shared memory
+    if (CW == 2) {
+      float4* box = reinterpret_cast<float4*>(sKV) + wc * (ND * 4 + 1) * 64;
+      if (wk == 1) {
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            box[(4 * i + r) * 64 + lane] =
+                make_float4(acc[i][4 * r], acc[i][4 * r + 1], acc[i][4 * r + 2], acc[i][4 * r + 3]);
+        box[ND * 4 * 64 + lane] = make_float4(m, l, 0.0f, 0.0f);
+      }
+      __syncthreads();
+      if (wk == 0) {
+        const float4 o = box[ND * 4 * 64 + lane];
+        const float top = fmaxf(m, o.x), use = top == -INFINITY ? 0.0f : top;
+        const float f0 = __builtin_amdgcn_exp2f(m - use), f1 = __builtin_amdgcn_exp2f(o.x - use);
+        m = top;
+        l = l * f0 + o.y * f1;
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float4 v = box[(4 * i + r) * 64 + lane];
+            acc[i][4 * r] = acc[i][4 * r] * f0 + v.x * f1;
+            acc[i][4 * r + 1] = acc[i][4 * r + 1] * f0 + v.y * f1;
+            acc[i][4 * r + 2] = acc[i][4 * r + 2] * f0 + v.z * f1;
+            acc[i][4 * r + 3] = acc[i][4 * r + 3] * f0 + v.w * f1;
+          }
+      }
+      __syncthreads();
+    }
+    // acc[i][4 r + e] is d = 32 i + 8 r + 4 g + e of this lane's column
+    if (col >= ncol || wk != 0) continue;
+    if (whole) {
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      char* dst = a.po + row_offset(a.o, row, head) + g * 8;
+#pragma unroll
+      for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *reinterpret_cast<uint2*>(dst + (32 * i + 8 * r) * 2) =
+              make_uint2(pack2<BF>(acc[i][4 * r] * inv, acc[i][4 * r + 1] * inv),
+                         pack2<BF>(acc[i][4 * r + 2] * inv, acc[i][4 * r + 3] * inv));
+    } else {
+      const int64_t to = (int64_t)slot_out * COLS + wc * 32 + lq;
+      if (g == 0) {
+        ps.part_ml[2 * to] = m;
+        ps.part_ml[2 * to + 1] = l;
+      }
+      float* dst = ps.part_o + to * D + 4 * g;
+#pragma unroll
+      for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *reinterpret_cast<float4*>(dst + 32 * i + 8 * r) =
+              make_float4(acc[i][4 * r], acc[i][4 * r + 1], acc[i][4 * r + 2], acc[i][4 * r + 3]);
     }
   }
 }
@@ -491,7 +896,7 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
       const int64_t n = min(p.grid, s.total), from = s.step + (int64_t)it * s.steps;
       const int w0 = (int)(((from + 1) * n - 1) / s.total), w1 = (int)(((from + s.steps) * n - 1) / s.total);
       *at = ((int64_t)s.tile + it + w0) * p.cols + (col - tile * p.cols);
-      return min(w1 - w0 + 1, max(0, p.slots - (s.tile + it + w0)));
+      return w1 - w0 + 1;
     };
     int64_t at_g = 0, at_q = 0;
     const int n_g = range(g, sh, &at_g), n_q = range(q, own, &at_q);
@@ -540,20 +945,26 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
   }
 }
 
+template <class K>
+hipError_t run_walk(K kernel, const PagedArgs& a, const PagedPass& p, hipStream_t s) {
+  kernel<<<dim3(p.grid), dim3(kThreads), (p.n + 1) * sizeof(Seg), s>>>(a, p);
+  return hipGetLastError();
+}
 template <int D, bool BF>
 hipError_t run_pass(const PagedArgs& a, const PagedPass& p, hipStream_t s) {
-  const dim3 g(p.grid), b(kThreads);
-  if (p.cols == 16) paged_kernel<D, BF, 1><<<g, b, 0, s>>>(a, p);
-  else if (p.cols == 32) paged_kernel<D, BF, 2><<<g, b, 0, s>>>(a, p);
-  else paged_kernel<D, BF, 4><<<g, b, 0, s>>>(a, p);
-  return hipGetLastError();
+  if (p.cols == 16) return run_walk(paged_kernel<D, BF, 1>, a, p, s);
+  if (p.cols == 32) return run_walk(paged_kernel<D, BF, 2>, a, p, s);
+  if (p.cols == 64) return run_walk(paged_wide_kernel<D, BF, 2>, a, p, s);
+  return run_walk(paged_wide_kernel<D, BF, 4>, a, p, s);
 }
 
 template <int D, bool BF>
 hipError_t run_paged(const PagedArgs& a, const PagedPass& sh, const PagedPass& own, hipStream_t s) {
   hipError_t e;
-  if (sh.n && (e = run_pass<D, BF>(a, sh, s)) != hipSuccess) return e;
+  // the sequences first: their pass says how far every row sees
   if ((e = run_pass<D, BF>(a, own, s)) != hipSuccess) return e;
+  if (own.fused) return e;
+  if (sh.n && (e = run_pass<D, BF>(a, sh, s)) != hipSuccess) return e;
   const int64_t avg = (a.rows + (int64_t)a.n_seq - 1) / a.n_seq;
   const dim3 jg(a.n_seq, (a.hkv * a.g + kWaves - 1) / kWaves, (uint32_t)(avg < 64 ? avg : 64));
   paged_join_kernel<D, BF><<<jg, dim3(kThreads), 0, s>>>(a, sh, own);

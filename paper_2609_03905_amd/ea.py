@@ -384,7 +384,7 @@ def join_tuples(spec: str, join_op: int, inputs: Sequence[Relation], out: Relati
 
 # ---- decoding: head rows, attention over a paged cache, the page table -------
 PAGES_OK, PAGES_NONE_FREE, PAGES_TOO_LONG = 0, 1, 2  # status[0] of the page calls (EA_PAGES_*)
-PAGED_MAX_SEQ = 4096  # EA_PAGED_MAX_SEQ
+PAGED_MAX_SEQ = 2048  # EA_PAGED_MAX_SEQ
 
 
 _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device

@@ -143,8 +143,8 @@ def paged(ws=256, n=None, **change):
 @pytest.mark.parametrize("code,change", [
     (ARG, dict(no_batch=True)), (ARG, dict(q=None)), (ARG, dict(k=None)), (ARG, dict(v=None)), (ARG, dict(out=None)),
     (ARG, dict(scale=0.0)), (ARG, dict(scale=-1.0)), (ARG, dict(scale=float("nan"))), (ARG, dict(scale=float("inf"))),
-    (ARG, dict(n_seq=0)), (ARG, dict(n_group=-1)), (UNSUPPORTED, dict(n_seq=4097)),
-    (UNSUPPORTED, dict(n_seq=4000, n_group=97)),
+    (ARG, dict(n_seq=0)), (ARG, dict(n_group=-1)), (UNSUPPORTED, dict(n_seq=2049)),
+    (UNSUPPORTED, dict(n_seq=2000, n_group=49)),
     (ARG, dict(lengths=None)), (ARG, dict(table=None)), (ARG, dict(stride=0)), (UNSUPPORTED, dict(stride=2 ** 27)),
     (ARG, dict(n_group=1)), (ARG, dict(n_group=1, gs=256)),
     (ARG, dict(n_seq=6)),                               # fewer rows than sequences, one row each
@@ -207,7 +207,7 @@ def compact(caches=(), ws=256, n=None, **change):
 @pytest.mark.parametrize("call", [extend, select, compact])
 @pytest.mark.parametrize("code,change", [
     (ARG, dict(n_seq=0)), (ARG, dict(stride=0)), (ARG, dict(n_pages=0)), (ARG, dict(page_size=0)),
-    (ARG, dict(n_pages=-5)), (UNSUPPORTED, dict(n_seq=4097)), (UNSUPPORTED, dict(n_seq=4096, stride=1 << 20)),
+    (ARG, dict(n_pages=-5)), (UNSUPPORTED, dict(n_seq=2049)), (UNSUPPORTED, dict(n_seq=2048, stride=1 << 20)),
     (UNSUPPORTED, dict(n_pages=1 << 28)), (UNSUPPORTED, dict(stride=1 << 27, n_seq=1)),
     (ARG, dict(table=None)), (ARG, dict(lengths=None)), (ARG, dict(refs=None)), (ARG, dict(out_refs=None)),
     (ARG, dict(status=None)), (ARG, dict(out_refs=A + 4)), (ARG, dict(status=A + (2 << 20))),

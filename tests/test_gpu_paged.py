@@ -244,3 +244,60 @@ def test_two_streams_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     for o, r in zip(outs, ref):
         assert torch.equal(o.view(n, hq, d), r)
+
+
+WIDE = [
+    # lens, groups, n_q, hq, hkv, d, page, dtype: more than 32 columns a tile
+    ([200] * 9, [(0, 9, 160)], 1, 8, 2, 128, 16, "bf16"),            # 36 columns
+    ([130] * 17, [(0, 17, 128)], 1, 4, 1, 64, 64, "f16"),            # 68
+    ([300, 310, 320], [], 40, 4, 1, 128, 16, "bf16"),                # long drafts, 160 columns each
+    ([33, 1, 64, 65], [], 20, 4, 2, 64, 7, "f16"),                   # rows that see none, odd pages
+    ([700 + 3 * i for i in range(40)], [(0, 40, 640)], 1, 8, 1, 128, 20, "bf16"),  # 320 columns
+    ([90 + i for i in range(30)], [(0, 15, 64), (15, 30, 80)], 2, 6, 1, 64, 8, "bf16"),
+]
+
+
+@pytest.mark.parametrize("case", WIDE, ids=[f"n{len(c[0])}_g{len(c[1])}_q{c[2]}_h{c[3]}_{c[4]}_d{c[5]}_p{c[6]}_{c[7]}"
+                                            for c in WIDE])
+def test_many_columns(case):
+    lens, groups, n_q, hq, hkv, d, page, dtype = case
+    k, v, table = _batch(lens, None, groups, page, hkv, d, dtype, 21, garbage=float("nan"))
+    q = torch.randn((len(lens) * n_q, hq, d), device="cuda").to(R.TORCH[dtype])
+    starts = None if n_q == 1 else [n_q * i for i in range(len(lens) + 1)]
+    got = _check(q, k, v, table, lens, starts, groups, page, dtype)
+    assert torch.equal(got, _run(q, k, v, table, lens, starts, groups, d ** -0.5))
+
+
+def test_many_columns_with_pages_outside_the_cache():
+    lens, groups = [210] * 12, [(0, 12, 128)]
+    k, v, table = _batch(lens, None, groups, 16, 1, 128, "bf16", 22, garbage=float("nan"))
+    for s in range(12):
+        table[s, 3] = -1          # inside the shared keys
+        table[s, 10] = k.shape[0]  # and inside the own ones
+    q = torch.randn((12, 4, 128), device="cuda").to(torch.bfloat16)
+    _check(q, k, v, table, lens, None, groups, 16, "bf16")
+
+
+def test_the_largest_batch():
+    """As many sequences as a call takes: lengths 0 to 6, some with none."""
+    n = ea.PAGED_MAX_SEQ - 1
+    lens = [i % 7 for i in range(n)]
+    k, v, table = _batch(lens, None, [], 4, 1, 64, "bf16", 23)
+    q = torch.randn((n, 1, 64), device="cuda").to(torch.bfloat16)
+    _check(q, k, v, table, lens, None, [], 4, "bf16")
+    groups = [(100, 900, 0)]
+    _check(q, k, v, table, lens, None, groups, 4, "bf16")
+
+
+def test_query_rows_that_do_not_ascend_stay_inside():
+    """A bad q_start gives no defined values; the call ends, writes no row
+    behind the last and leaves the workspace usable."""
+    lens = [100, 200, 300]
+    k, v, table = _batch(lens, None, [], 16, 1, 64, "bf16", 24)
+    q = torch.randn((8, 4, 64), device="cuda").to(torch.bfloat16)
+    good = _run(q, k, v, table, lens, [0, 2, 5, 8], [], 0.1).clone()
+    for bad in ([0, 8, 0, 8], [8, 0, 8, 0], [-5, 2 ** 31 - 1, -2 ** 31, 8], [3, 3, 3, 3]):
+        out = torch.full((9, 4 * 64), 7.0, device="cuda", dtype=torch.bfloat16)
+        _run(q, k, v, table, lens, bad, [], 0.1, out=out[:8])
+        assert (out[8] == 7.0).all()
+        assert torch.equal(_run(q, k, v, table, lens, [0, 2, 5, 8], [], 0.1), good)
