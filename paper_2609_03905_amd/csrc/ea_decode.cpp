@@ -342,7 +342,7 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
   if (!b.lengths || !b.table) return fail(EA_ERR_ARG, "NULL lengths or table");
   if (b.n_group && (!b.group_start || !b.group_shared)) return fail(EA_ERR_ARG, "NULL group_start or group_shared");
   if (b.stride < 1) return fail(EA_ERR_ARG, "table stride %d", b.stride);
-  if ((b.stride + 1) * k->shape[2] > INT32_MAX) return fail(EA_ERR_UNSUPPORTED, "a table row of 2^31 keys or more");
+  if ((b.stride + (int64_t)1) * k->shape[2] > INT32_MAX - 1024) return fail(EA_ERR_UNSUPPORTED, "a table row of 2^31 keys or more");
   if (!b.q_start && a.q.t < b.n_seq) return fail(EA_ERR_ARG, "%d query rows for %d sequences", a.q.t, b.n_seq);
   for (const ea_relation* r : {q, k, v})
     if (overlap(out, r)) return fail(EA_ERR_ARG, "out overlaps an input");

@@ -262,6 +262,16 @@ __device__ __forceinline__ void store_row(char* dst, const float (&o)[VE], float
   else *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
 }
 
+// A stretch of one tile's walk.
+struct Piece {
+  Seg s;
+  const int32_t* pages;
+  int64_t head_off;
+  int si, h, tile, it, n;  // segment, key-value head, tile of the head, tile of the segment, steps of its walk
+  int ka, kb;              // keys
+  bool whole;
+};
+
 template <int D, bool BF, int NC>
 __global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kernel(const PagedArgs a, const PagedPass ps) {
   constexpr int VE = D / 16;          // d elements a lane holds of a V row
@@ -283,45 +293,106 @@ __global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kern
   int at = (int)((int64_t)total * w / parts);
   const int end = (int)((int64_t)total * (w + 1) / parts);
 
-  while (at < end) {
-    // ---- which tile, and how far this part walks it
-    const int si = find_segment(seg, ps.n, at);
-    const Seg s = seg[si];
-    const int n = steps_of(s.k0, s.k1, kPagedStep), tiles = tiles_of(s.rows, a.g, COLS);
-    const int local = at - s.step, it = local / n, step = local - it * n;
-    const int h = it / tiles, tile = it - h * tiles;
-    const int walk = min(n - step, end - at);
-    const int slot_out = s.tile + it + w;
+  // ---- the tile that step `at` belongs to, and how far this part walks it
+  auto next_piece = [&]() {
+    Piece p;
+    p.si = find_segment(seg, ps.n, at);
+    p.s = seg[p.si];
+    p.n = steps_of(p.s.k0, p.s.k1, kPagedStep);
+    const int tiles = tiles_of(p.s.rows, a.g, COLS);
+    const int local = at - p.s.step, step = local % p.n;
+    p.it = local / p.n;
+    p.h = p.it / tiles;
+    p.tile = p.it - p.h * tiles;
+    const int walk = min(p.n - step, end - at);
     // the only result of these columns: no join
-    const bool whole = !ps.shared && walk == n && s.k0 == 0;
-    const int ka = s.k0 + step * kPagedStep;
-    const int kb = (int)min((int64_t)s.k1, (int64_t)ka + (int64_t)walk * kPagedStep);
+    p.whole = !ps.shared && walk == p.n && p.s.k0 == 0;
+    p.ka = p.s.k0 + step * kPagedStep;
+    p.kb = (int)min((int64_t)p.s.k1, (int64_t)p.ka + (int64_t)walk * kPagedStep);
+    p.pages = a.table + (int64_t)table_row(a, ps, p.si) * a.stride;
+    p.head_off = (int64_t)p.h * a.page_size * D * 2;
     at += walk;
-
-    // ---- this lane's columns: query rows and heads, and the keys they see
-    const int ncol = s.rows * a.g;
-    int lim[NC], lim_min = 0x7fffffff;
-    uint4 q[NC][KS];
+    return p;
+  };
+  // a wave's step is 32 keys; lane i (and i + 32) looks after key i
+  const int kl = lane & 31;
+  auto entry = [&](const Piece& p, int k) { return k + kl < p.kb ? p.pages[div_fast(k + kl, a.page)] : -1; };
+  auto place = [&](const Piece& p, int slot, int k, int pg) {  // the rows' offsets, -1: no such row
+    const int key = k + kl, in = key - div_fast(key, a.page) * a.page_size;
+    const int64_t off = (uint32_t)pg < (uint32_t)a.n_pages ? pg * a.page_bytes + (int64_t)in * (D * 2) : -1;
+    if (lane < 32) s_off[wid][slot][kl] = off;
+    __builtin_amdgcn_wave_barrier();
+  };
+  uint4 kr[2][KS];
+  uint32_t vr[8][VE / 2];
+  auto load_k = [&](const Piece& pc, int slot) {
+    const char* base = a.pk + pc.head_off + g4 * 16;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int64_t off = s_off[wid][slot][16 * t + c];
+      const char* p = base + (off < 0 ? 0 : off);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) kr[t][i] = *reinterpret_cast<const uint4*>(p + i * 64);
+    }
+  };
+  auto load_v = [&](const Piece& pc, int slot) {
+    const char* base = a.pv + pc.head_off + c * VE * 2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t off = s_off[wid][slot][16 * (i >> 2) + 4 * g4 + (i & 3)];
+      const char* p = base + (off < 0 ? 0 : off);
+      if constexpr (VE == 8) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        vr[i][0] = x.x, vr[i][1] = x.y, vr[i][2] = x.z, vr[i][3] = x.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        vr[i][0] = x.x, vr[i][1] = x.y;
+      }
+    }
+  };
+  uint4 q[NC][KS];
+  auto load_q = [&](const Piece& pc) {  // this lane's columns: query rows and heads
 #pragma unroll
     for (int t = 0; t < NC; ++t) {
-      const int col = tile * COLS + t * kPagedCols + c;
-      const int cc = min(col, ncol - 1);
-      const int rr = div_fast(cc, a.gdiv), row = s.r0 + rr, head = h * a.g + cc - rr * a.g;
-      lim[t] = col < ncol ? limit_of(a, ps, s, row, rr) : 0x7fffffff;  // (never stored: no mask)
-      lim_min = min(lim_min, lim[t]);
-      const char* p = a.pq + row_offset(a.q, row, head) + g4 * 16;
+      const int cc = min(pc.tile * COLS + t * kPagedCols + c, pc.s.rows * a.g - 1);
+      const int rr = div_fast(cc, a.gdiv);
+      const char* p = a.pq + row_offset(a.q, pc.s.r0 + rr, pc.h * a.g + cc - rr * a.g) + g4 * 16;
 #pragma unroll
       for (int i = 0; i < KS; ++i) q[t][i] = *reinterpret_cast<const uint4*>(p + i * 64);
+    }
+  };
+
+  // The loads of a step are on their way while the step before is computed,
+  // also from one piece to the next: `next` is known before the last step of
+  // `cur`, and its first rows are fetched behind that step's products.
+  Piece next = next_piece();
+  int slot = 0, next_pg = entry(next, next.ka + wid * 32);
+  load_q(next);
+  place(next, 0, next.ka + wid * 32, next_pg);
+  load_k(next, 0);
+  load_v(next, 0);
+  bool have = true;
+  while (have) {
+    const Piece cur = next;
+    have = at < end;
+    if (have) next = next_piece();
+    const Seg s = cur.s;
+    const int h = cur.h, tile = cur.tile, it = cur.it, n = cur.n, kb = cur.kb, slot_out = s.tile + it + w;
+    const bool whole = cur.whole;
+
+    // ---- the keys that this lane's columns see
+    const int ncol = s.rows * a.g;
+    int lim[NC], lim_min = 0x7fffffff;
+#pragma unroll
+    for (int t = 0; t < NC; ++t) {
+      const int col = tile * COLS + t * kPagedCols + c, rr = div_fast(min(col, ncol - 1), a.gdiv);
+      lim[t] = col < ncol ? limit_of(a, ps, s, s.r0 + rr, rr) : 0x7fffffff;  // (never stored: no mask)
+      lim_min = min(lim_min, lim[t]);
     }
     lim_min = min(lim_min, __shfl_xor(lim_min, 1));
     lim_min = min(lim_min, __shfl_xor(lim_min, 2));
     lim_min = min(lim_min, __shfl_xor(lim_min, 4));
     lim_min = __builtin_amdgcn_readfirstlane(min(lim_min, __shfl_xor(lim_min, 8)));
-
-    const int32_t* pages = a.table + (int64_t)table_row(a, ps, si) * a.stride;
-    const int64_t head_off = (int64_t)h * a.page_size * D * 2;
-    const char* kbase = a.pk + head_off + g4 * 16;
-    const char* vbase = a.pv + head_off + c * VE * 2;
 
     f32x4_t acc[NC][VE];
     float m[NC], l[NC];
@@ -332,62 +403,19 @@ __global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kern
 #pragma unroll
       for (int j = 0; j < VE; ++j) acc[t][j] = f32x4_t{};
     }
-
-    // a wave's step is 32 keys; lane i (and i + 32) looks after key i
-    const int kl = lane & 31;
-    auto entry = [&](int k) { return k + kl < kb ? pages[div_fast(k + kl, a.page)] : -1; };
-    auto offset = [&](int k, int pg) -> int64_t {  // of the key's row, -1: no such row
-      if ((uint32_t)pg >= (uint32_t)a.n_pages) return -1;
-      const int key = k + kl, in = key - div_fast(key, a.page) * a.page_size;
-      return pg * a.page_bytes + (int64_t)in * (D * 2);
-    };
-    uint4 kr[2][KS];
-    uint32_t vr[8][VE / 2];
-    auto load_k = [&](int slot) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int64_t off = s_off[wid][slot][16 * t + c];
-        const char* p = kbase + (off < 0 ? 0 : off);
-#pragma unroll
-        for (int i = 0; i < KS; ++i) kr[t][i] = *reinterpret_cast<const uint4*>(p + i * 64);
-      }
-    };
-    auto load_v = [&](int slot) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int64_t off = s_off[wid][slot][16 * (i >> 2) + 4 * g4 + (i & 3)];
-        const char* p = vbase + (off < 0 ? 0 : off);
-        if constexpr (VE == 8) {
-          const uint4 x = *reinterpret_cast<const uint4*>(p);
-          vr[i][0] = x.x, vr[i][1] = x.y, vr[i][2] = x.z, vr[i][3] = x.w;
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(p);
-          vr[i][0] = x.x, vr[i][1] = x.y;
-        }
-      }
-    };
-    int k = ka + wid * 32;
-    bool full = false;  // every key of the step has a row and is seen by every column
-    int next_pg = 0;
-    if (k < kb) {
-      const int64_t off = offset(k, entry(k));
-      if (lane < 32) s_off[wid][0][kl] = off;
-      full = __all(off >= 0) && k + 32 <= lim_min;
-      next_pg = entry(k + kPagedStep);
-      __builtin_amdgcn_wave_barrier();
-      load_k(0);
-      load_v(0);
-    }
-    int slot = 0;
-    for (; k < kb; k += kPagedStep) {
-      const bool more = k + kPagedStep < kb;
-      bool full_next = false;
-      if (more) {
-        const int64_t off = offset(k + kPagedStep, next_pg);
-        if (lane < 32) s_off[wid][slot ^ 1][kl] = off;
-        full_next = __all(off >= 0) && k + kPagedStep + 32 <= lim_min;
-        next_pg = entry(k + 2 * kPagedStep);
-        __builtin_amdgcn_wave_barrier();
+    // (a piece shorter than the waves before this one's rows: the step is
+    // empty, its rows are masked, and the next piece's loads follow it)
+    int k = cur.ka + wid * 32;
+    next_pg = entry(cur, k + kPagedStep);
+    for (bool again = true; again; k += kPagedStep) {
+      again = k + kPagedStep < kb;
+      // every key of the step has a row and is seen by every column
+      const bool full = __all(s_off[wid][slot][kl] >= 0) && k + 32 <= lim_min;
+      if (again) {
+        place(cur, slot ^ 1, k + kPagedStep, next_pg);
+        next_pg = entry(cur, k + 2 * kPagedStep);
+      } else if (have) {
+        place(next, slot ^ 1, next.ka + wid * 32, entry(next, next.ka + wid * 32));
       }
       f32x4_t sc[NC][2];
 #pragma unroll
@@ -399,7 +427,8 @@ __global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kern
           sc[t][1] = mfma16<BF>(kr[1][i], q[t][i], sc[t][1]);
         }
       }
-      if (more) load_k(slot ^ 1);
+      if (again) load_k(cur, slot ^ 1);
+      else if (have) load_k(next, slot ^ 1);
       if (!full) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -452,10 +481,11 @@ __global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kern
 #pragma unroll
         for (int t = 0; t < NC; ++t) acc[t][j] = mfma16<BF>(v, p[t], acc[t][j]);
       }
-      if (more) load_v(slot ^ 1);
+      if (again) load_v(cur, slot ^ 1);
+      else if (have) load_v(next, slot ^ 1);
       slot ^= 1;
-      full = full_next;
     }
+    if (have) load_q(next);
     // ---- join the four waves, 16 columns at a time.  Lane (g4, c) holds
     // d = (4 g4 + i) VE + j of its column: 4 VE neighbours.
 #pragma unroll
@@ -874,21 +904,22 @@ __global__ __launch_bounds__(kThreads, 2) void paged_wide_kernel(const PagedArgs
   }
 }
 
-// Join of a row's partial results: one wave a (row, query head), its parts in
-// order (shared keys, then own).
+// Join of a row's partial results, shared keys first: one wave a (row, query
+// head), D / 4 lanes a part, several parts at a time and eight loads of each in
+// flight; what the lane groups hold is joined at the end.
 template <int D, bool BF>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a, const PagedPass sh,
                                                               const PagedPass own) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int hq = blockIdx.y * kWaves + wid;
+  constexpr int LPP = D / 4, PPW = 64 / LPP;
+  const int lane = threadIdx.x & 63, sub = lane / LPP, e4 = lane % LPP;
+  const int hq = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (hq >= a.hkv * a.g) return;
   const int h = div_fast(hq, a.gdiv), hg = hq - h * a.g;
   const PagedSeg q = a.seg[a.n_group + blockIdx.x];
   PagedSeg g = {};
   if (q.group >= 0) g = a.seg[q.group];
   for (int row = q.r0 + blockIdx.z; row < q.r1; row += gridDim.z) {
-    // parts [first, first + n) of a walk, and the column of slot `first`
+    // parts of a walk, and the column of the first one's slot
     auto range = [&](const PagedSeg& s, const PagedPass& p, int64_t* at) {
       if (s.steps == 0) return 0;
       const int col = (row - s.r0) * a.g + hg, tile = col / p.cols;
@@ -901,47 +932,50 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
     int64_t at_g = 0, at_q = 0;
     const int n_g = range(g, sh, &at_g), n_q = range(q, own, &at_q);
     if (n_g == 0 && n_q == 1) continue;  // stored by the walk itself
-    auto ml_of = [&](int p) {
-      return p < n_g ? sh.part_ml + 2 * (at_g + (int64_t)p * sh.cols)
-                     : own.part_ml + 2 * (at_q + (int64_t)(p - n_g) * own.cols);
-    };
     const int parts = n_g + n_q;
-    float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, *ml_of(p));
-    top = wave_max(top);
-    const float use = top == -INFINITY ? 0.0f : top;
-    float l = 0.0f, o[E] = {};
-    for (int p0 = 0; p0 < parts; p0 += 64) {
-      const int n = min(64, parts - p0);
-      float f = 0.0f, lp = 0.0f;
-      if (lane < n) {
-        const float* ml = ml_of(p0 + lane);
-        f = __builtin_amdgcn_exp2f(ml[0] - use);
-        lp = ml[1] * f;
+    float m = -INFINITY, l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int p0 = sub; p0 < parts; p0 += 8 * PPW) {
+      float2 ml[8];
+      float4 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int p = min(p0 + i * PPW, parts - 1);
+        const bool in_g = p < n_g;
+        const int64_t at = in_g ? at_g + (int64_t)p * sh.cols : at_q + (int64_t)(p - n_g) * own.cols;
+        ml[i] = *reinterpret_cast<const float2*>((in_g ? sh.part_ml : own.part_ml) + 2 * at);
+        x[i] = *reinterpret_cast<const float4*>((in_g ? sh.part_o : own.part_o) + at * D + 4 * e4);
+        if (p0 + i * PPW >= parts) ml[i] = make_float2(-INFINITY, 0.0f);
       }
-      l += wave_sum(lp);
-      for (int i0 = 0; i0 < n; i0 += 8) {  // eight parts' loads at a time
-        float x[8][E];
+      float top = m;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int p = p0 + min(i0 + i, n - 1);
-          const float* src = (p < n_g ? sh.part_o + (at_g + (int64_t)p * sh.cols) * D
-                                      : own.part_o + (at_q + (int64_t)(p - n_g) * own.cols) * D) + lane * E;
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
+      const float use = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - use);
+      m = top;
+      l *= keep;
+      o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
 #pragma unroll
-          for (int e = 0; e < E; ++e) x[i][e] = src[e];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float fi = __shfl(f, min(i0 + i, n - 1));
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = i0 + i < n ? fmaf(x[i][e], fi, o[e]) : o[e];
+      for (int i = 0; i < 8; ++i) {
+        if (p0 + i * PPW < parts) {
+          const float f = __builtin_amdgcn_exp2f(ml[i].x - use);
+          l = fmaf(ml[i].y, f, l);
+          o.x = fmaf(x[i].x, f, o.x), o.y = fmaf(x[i].y, f, o.y);
+          o.z = fmaf(x[i].z, f, o.z), o.w = fmaf(x[i].w, f, o.w);
         }
       }
     }
+    float top = fmaxf(m, other32(m));
+    if (PPW == 4) top = fmaxf(top, other16(top));
+    const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+    auto sum = [&](float v) {
+      v *= f;
+      v += other32(v);
+      return PPW == 4 ? v + other16(v) : v;
+    };
+    l = sum(l);
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    char* dst = a.po + row_offset(a.o, row, hq) + lane * E * 2;
-    if constexpr (E == 2) *reinterpret_cast<uint32_t*>(dst) = pack2<BF>(o[0] * inv, o[1] * inv);
-    else *reinterpret_cast<uint16_t*>(dst) = BF ? f32_to_bf16(o[0] * inv) : f32_to_f16(o[0] * inv);
+    const uint2 y = make_uint2(pack2<BF>(sum(o.x) * inv, sum(o.y) * inv), pack2<BF>(sum(o.z) * inv, sum(o.w) * inv));
+    if (sub == 0) *reinterpret_cast<uint2*>(a.po + row_offset(a.o, row, hq) + e4 * 8) = y;
   }
 }
 
