@@ -251,20 +251,21 @@ namespace {
 struct PagedPlan {
   PagedPass shared{}, own{};
   int64_t bytes = 0;
-  int64_t seg = 0, lim = 0, ml[2] = {}, o[2] = {};  // offsets
+  int64_t seg = 0, ml[2] = {}, o[2] = {};  // offsets
 };
 
 // A pass over n segments of `cols` query columns in all, by the columns that a
 // segment has on the average: up to 16 or 32, the walk that loads keys into
 // registers (at 32 columns of width 128 its registers admit one workgroup a
-// CU); beyond, the walk through shared memory, on tiles of 64 or 128 columns,
-// a step on the narrower costing about 0.55 of one on the wider.
+// CU); beyond, and for shared keys, the walk through shared memory, on tiles of
+// 64 or 128 columns, a step on the narrower costing about 0.55 of one on the
+// wider.
 void plan_pass(PagedPass* p, bool shared, int first, int n, int64_t cols, int64_t hkv, int64_t d) {
   p->shared = shared;
   p->first = first;
   p->n = n;
   const int64_t avg = n ? (cols + n - 1) / n : 0;
-  if (avg <= 32) p->cols = avg > 16 ? 32 : 16;
+  if (avg <= 32 && !shared) p->cols = avg > 16 ? 32 : 16;
   else p->cols = 0.55 * (double)((avg + 63) / 64) < (double)((avg + 127) / 128) ? 64 : 128;
   p->grid = p->cols == 32 && d == 128 ? 256 : 512;
   const int64_t tiles = (cols / p->cols + n) * hkv;
@@ -294,8 +295,7 @@ int plan_paged(const ea_relation* q, const ea_relation* k, const ea_paged* b, bo
   // part of a tile joins them and no second launch follows
   p->own.fused = b->n_group == 0 && p->own.cols <= 32 && p->own.tiles <= kWsCounterBytes / 4;
   p->seg = kWsCounterBytes;
-  p->lim = p->seg + align256((b->n_seq + b->n_group) * (int64_t)sizeof(PagedSeg));
-  int64_t at = p->lim + (b->n_group ? align256((int64_t)mq->t * 4) : 0);
+  int64_t at = p->seg + align256((b->n_seq + b->n_group) * (int64_t)sizeof(PagedSeg));
   int i = 0;
   for (const PagedPass* s : {&p->shared, &p->own}) {
     const int64_t slots = s->n ? (int64_t)s->tiles + s->grid : 0;
@@ -373,7 +373,6 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
   a.scale = b.scale * 1.4426950408889634f;
   char* ws = (char*)workspace;
   a.seg = (PagedSeg*)(ws + p.seg);
-  a.row_lim = (int32_t*)(ws + p.lim);
   p.own.counters = (int32_t*)ws;
   int i = 0;
   for (PagedPass* s : {&p.shared, &p.own}) {

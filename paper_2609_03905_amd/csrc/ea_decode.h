@@ -128,7 +128,6 @@ struct PagedArgs {
   int64_t page_bytes;
   float scale;       // of the scores, log2 domain
   PagedSeg* seg;     // groups, then sequences
-  int32_t* row_lim;  // keys that a query row sees
 };
 hipError_t launch_paged(const PagedArgs& a, const PagedPass& shared, const PagedPass& own, int32_t d, int32_t dtype,
                         hipStream_t s);

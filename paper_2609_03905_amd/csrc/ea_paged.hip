@@ -170,10 +170,9 @@ __device__ __forceinline__ int tiles_of(int rows, int g, int cols) {
 }
 
 // Every segment's first step and tile, by the whole workgroup.  Also hands the
-// join what it needs and, from the sequences' pass, the shared pass every
-// query row's limit (the number of keys it sees).  Returns the steps of all.
+// join what it needs.  Returns the steps of all.
 template <int D, int COLS, int KEYS>
-__device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps, Seg* seg) {
+__device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps, Seg* seg, int block) {
   __shared__ int s_wave[kWaves][2];
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int per = (ps.n + kThreads - 1) / kThreads;
@@ -211,7 +210,7 @@ __device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps,
   // more tiles than the rows can have: the sequences' rows overlap, no walk
   const bool off = seg[ps.n].tile > ps.tiles;
   const int total = off ? 0 : seg[ps.n].step;
-  for (int i = blockIdx.x; i < ps.n; i += gridDim.x) {
+  for (int i = block; i < ps.n; i += ps.grid) {
     const Seg s = seg[i];
     if (ps.fused) {  // rows of a sequence without keys: no walk reaches them
       if (s.k1 > 0) continue;
@@ -230,8 +229,6 @@ __device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps,
       g.total = total;
       a.seg[ps.first + i] = g;
     }
-    if (a.n_group && !ps.shared)
-      for (int r = tid; r < s.rows; r += kThreads) a.row_lim[s.r0 + r] = s.k1 - s.rows + r + 1;
   }
   return total;
 }
@@ -247,9 +244,28 @@ __device__ __forceinline__ int find_segment(const Seg* seg, int n, int at) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Keys that query row `row`, the rr-th of segment s, sees.
-__device__ __forceinline__ int limit_of(const PagedArgs& a, const PagedPass& ps, const Seg& s, int row, int rr) {
-  return ps.shared ? a.row_lim[row] : s.k1 - s.rows + rr + 1;
+// Keys that query row `row`, the rr-th of segment i, sees.  In a group the
+// row's own sequence says so.
+__device__ __forceinline__ int limit_of(const PagedArgs& a, const PagedPass& ps, const Seg& s, int i, int row, int rr) {
+  if (!ps.shared) return s.k1 - s.rows + rr + 1;
+  int lo = clampi(a.group_start[i], 0, a.n_seq), hi = clampi(a.group_start[i + 1], lo, a.n_seq);
+  if (!a.q_start) lo = clampi(row, lo, hi);
+  else
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first_row(a, mid) <= row) lo = mid;
+      else hi = mid;
+    }
+  lo = min(lo, a.n_seq - 1);
+  return clampi(a.len[lo], 0, a.stride * a.page_size) - (first_row(a, lo + 1) - row) + 1;
+}
+
+// Workgroups that share a walk of `total` steps: all of them, but at least
+// eight steps each of a walk over many columns while half of them remain (a
+// part leaves D floats a column behind, which the join reads again).
+__device__ __forceinline__ int parts_of(const PagedPass& p, int total) {
+  if (p.cols <= 32) return min(p.grid, total);
+  return min(max(total / 8, min(total, p.grid / 2)), p.grid);
 }
 
 // VE neighbouring elements of an output row, scaled.
@@ -272,24 +288,43 @@ struct Piece {
   bool whole;
 };
 
-template <int D, bool BF, int NC>
-__global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kernel(const PagedArgs a, const PagedPass ps) {
+// The part of n that takes step `at` of `total`: the last w with total w / n,
+// rounded down, at or before it.  The quotient is below 2^10 and at least
+// 2^-31 below the next whole number unless it is one, so that 53 bits do.
+__device__ __forceinline__ int part_of(int64_t at, int64_t n, int total) {
+  return (int)((double)((at + 1) * n - 1) / (double)total);
+}
+
+// Shared memory of the two walks.
+template <int D>
+struct __attribute__((aligned(16))) FewShared {
+  int64_t off[kWaves][2][32];
+  float o[kWaves][kPagedCols][D + 4];  // (four more: banks)
+  float ml[kWaves][kPagedCols][2];
+  int last;
+};
+template <int D>
+struct __attribute__((aligned(1024))) ManyShared {
+  uint16_t kv[2][2 * kPagedWideStep * D];  // two steps' buffers: K, then V
+  int64_t off[2][kPagedWideStep];
+};
+
+template <int D, bool BF, int COLS>
+__device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps, Seg* seg, FewShared<D>& sh,
+                                         int block) {
+  constexpr int NC = COLS / kPagedCols;
   constexpr int VE = D / 16;          // d elements a lane holds of a V row
   constexpr int KS = D / 32;          // k steps of the score product
-  constexpr int PITCH = D + 4;        // of a column in the waves' join (banks)
-  constexpr int COLS = kPagedCols * NC;
-  extern __shared__ __attribute__((aligned(16))) char dyn[];
-  Seg* seg = reinterpret_cast<Seg*>(dyn);
-  __shared__ int64_t s_off[kWaves][2][32];
-  __shared__ __attribute__((aligned(16))) float s_o[kWaves][kPagedCols][PITCH];
-  __shared__ float s_ml[kWaves][kPagedCols][2];
-  __shared__ int s_last;
+  auto& s_off = sh.off;
+  auto& s_o = sh.o;
+  auto& s_ml = sh.ml;
+  int& s_last = sh.last;
 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int total = schedule<D, COLS, kPagedStep>(a, ps, seg), parts = min((int)gridDim.x, total);
-  if ((int)blockIdx.x >= parts) return;
-  const int w = xcd_part(blockIdx.x, parts);
+  const int total = schedule<D, COLS, kPagedStep>(a, ps, seg, block), parts = parts_of(ps, total);
+  if (block >= parts) return;
+  const int w = xcd_part(block, parts);
   int at = (int)((int64_t)total * w / parts);
   const int end = (int)((int64_t)total * (w + 1) / parts);
 
@@ -386,7 +421,7 @@ __global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kern
 #pragma unroll
     for (int t = 0; t < NC; ++t) {
       const int col = tile * COLS + t * kPagedCols + c, rr = div_fast(min(col, ncol - 1), a.gdiv);
-      lim[t] = col < ncol ? limit_of(a, ps, s, s.r0 + rr, rr) : 0x7fffffff;  // (never stored: no mask)
+      lim[t] = col < ncol ? limit_of(a, ps, s, cur.si, s.r0 + rr, rr) : 0x7fffffff;  // (never stored: no mask)
       lim_min = min(lim_min, lim[t]);
     }
     lim_min = min(lim_min, __shfl_xor(lim_min, 1));
@@ -549,7 +584,7 @@ __global__ __launch_bounds__(kThreads, NC > 1 && D > 64 ? 1 : 2) void paged_kern
 
     // ---- the last part of the tile to arrive joins them, in part order
     const int64_t from = s.step + (int64_t)it * n;
-    const int w0 = (int)(((from + 1) * parts - 1) / total), w1 = (int)(((from + n) * parts - 1) / total);
+    const int w0 = part_of(from, parts, total), w1 = part_of(from + n - 1, parts, total);
     drain_vmem();
     __syncthreads();
     int32_t* counter = ps.counters + s.tile + it;
@@ -649,26 +684,25 @@ __device__ __forceinline__ void load_to_lds(const char* p, uint32_t lds) {
 #pragma clang diagnostic pop
 }
 
-template <int D, bool BF, int CW>
-__global__ __launch_bounds__(kThreads, 2) void paged_wide_kernel(const PagedArgs a, const PagedPass ps) {
-  constexpr int COLS = 32 * CW, KEYS = kPagedWideStep;
+template <int D, bool BF, int COLS>
+__device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& ps, Seg* seg, ManyShared<D>& sh,
+                                          int block) {
+  constexpr int CW = COLS / 32, KEYS = kPagedWideStep;
   constexpr int KT = CW / 2;          // 32-key tiles that a wave computes of a step
   constexpr int NS = D / 16, ND = D / 32;
   constexpr int CPR = D / 8;          // 16-byte pieces of a row
   constexpr int RPI = 64 / CPR;       // rows of one load
   constexpr int LPW = 16 / RPI;       // loads of a wave (16 rows) for K, and for V
   constexpr int BUF = 2 * KEYS * D;   // elements of a step: K, then V
-  __shared__ __attribute__((aligned(1024))) uint16_t sKV[2 * BUF];
-  __shared__ int64_t s_off[2][KEYS];
-  extern __shared__ __attribute__((aligned(16))) char dyn[];
-  Seg* seg = reinterpret_cast<Seg*>(dyn);
+  uint16_t* sKV = sh.kv[0];
+  auto& s_off = sh.off;
 
   const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, g = lane >> 5;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wc = wid % CW, wk = wid / CW;  // the wave's columns, and its part of a step's keys
-  const int total = schedule<D, COLS, KEYS>(a, ps, seg), parts = min((int)gridDim.x, total);
-  if ((int)blockIdx.x >= parts) return;
-  const int w = xcd_part(blockIdx.x, parts);
+  const int total = schedule<D, COLS, KEYS>(a, ps, seg, block), parts = parts_of(ps, total);
+  if (block >= parts) return;
+  const int w = xcd_part(block, parts);
   int at = (int)((int64_t)total * w / parts);
   const int end = (int)((int64_t)total * (w + 1) / parts);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)sKV;
@@ -727,7 +761,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_wide_kernel(const PagedArgs
     // ---- this lane's column
     const int ncol = s.rows * a.g, col = tile * COLS + wc * 32 + lq, cc = min(col, ncol - 1);
     const int rr = div_fast(cc, a.gdiv), row = s.r0 + rr, head = h * a.g + cc - rr * a.g;
-    const int lim = col < ncol ? limit_of(a, ps, s, row, rr) : 0x7fffffff;  // (never stored: no mask)
+    const int lim = col < ncol ? limit_of(a, ps, s, si, row, rr) : 0x7fffffff;  // (never stored: no mask)
     const bool idle = tile * COLS + wc * 32 >= ncol;  // a wave without columns only fetches
     uint4 q[NS];
     {
@@ -904,15 +938,18 @@ __global__ __launch_bounds__(kThreads, 2) void paged_wide_kernel(const PagedArgs
   }
 }
 
-// Join of a row's partial results, shared keys first: one wave a (row, query
+// Join of a row's partial results, shared keys first: W waves a (row, query
 // head), D / 4 lanes a part, several parts at a time and eight loads of each in
-// flight; what the lane groups hold is joined at the end.
-template <int D, bool BF>
+// flight; what the lane groups (and waves) hold is joined at the end.
+template <int D, bool BF, int W>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a, const PagedPass sh,
                                                               const PagedPass own) {
-  constexpr int LPP = D / 4, PPW = 64 / LPP;
-  const int lane = threadIdx.x & 63, sub = lane / LPP, e4 = lane % LPP;
-  const int hq = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int LPP = D / 4, PPW = 64 / LPP, STRIDE = PPW * W;
+  __shared__ float4 s_o[W][LPP];
+  __shared__ float2 s_ml[W];
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, e4 = lane % LPP, sub = lane / LPP + (W > 1 ? wid * PPW : 0);
+  const int hq = W > 1 ? blockIdx.y : blockIdx.y * kWaves + wid;
   if (hq >= a.hkv * a.g) return;
   const int h = div_fast(hq, a.gdiv), hg = hq - h * a.g;
   const PagedSeg q = a.seg[a.n_group + blockIdx.x];
@@ -924,8 +961,8 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
       if (s.steps == 0) return 0;
       const int col = (row - s.r0) * a.g + hg, tile = col / p.cols;
       const int it = h * s.tiles + tile;
-      const int64_t n = min(p.grid, s.total), from = s.step + (int64_t)it * s.steps;
-      const int w0 = (int)(((from + 1) * n - 1) / s.total), w1 = (int)(((from + s.steps) * n - 1) / s.total);
+      const int64_t n = parts_of(p, s.total), from = s.step + (int64_t)it * s.steps;
+      const int w0 = part_of(from, n, s.total), w1 = part_of(from + s.steps - 1, n, s.total);
       *at = ((int64_t)s.tile + it + w0) * p.cols + (col - tile * p.cols);
       return w1 - w0 + 1;
     };
@@ -935,17 +972,20 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
     const int parts = n_g + n_q;
     float m = -INFINITY, l = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int p0 = sub; p0 < parts; p0 += 8 * PPW) {
+    for (int p0 = sub; p0 < parts; p0 += 8 * STRIDE) {
       float2 ml[8];
       float4 x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int p = min(p0 + i * PPW, parts - 1);
-        const bool in_g = p < n_g;
-        const int64_t at = in_g ? at_g + (int64_t)p * sh.cols : at_q + (int64_t)(p - n_g) * own.cols;
-        ml[i] = *reinterpret_cast<const float2*>((in_g ? sh.part_ml : own.part_ml) + 2 * at);
-        x[i] = *reinterpret_cast<const float4*>((in_g ? sh.part_o : own.part_o) + at * D + 4 * e4);
-        if (p0 + i * PPW >= parts) ml[i] = make_float2(-INFINITY, 0.0f);
+        const int p = p0 + i * STRIDE;
+        ml[i] = make_float2(-INFINITY, 0.0f);
+        x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (p < parts) {
+          const bool in_g = p < n_g;
+          const int64_t at = in_g ? at_g + (int64_t)p * sh.cols : at_q + (int64_t)(p - n_g) * own.cols;
+          ml[i] = *reinterpret_cast<const float2*>((in_g ? sh.part_ml : own.part_ml) + 2 * at);
+          x[i] = *reinterpret_cast<const float4*>((in_g ? sh.part_o : own.part_o) + at * D + 4 * e4);
+        }
       }
       float top = m;
 #pragma unroll
@@ -956,12 +996,10 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
       o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (p0 + i * PPW < parts) {
-          const float f = __builtin_amdgcn_exp2f(ml[i].x - use);
-          l = fmaf(ml[i].y, f, l);
-          o.x = fmaf(x[i].x, f, o.x), o.y = fmaf(x[i].y, f, o.y);
-          o.z = fmaf(x[i].z, f, o.z), o.w = fmaf(x[i].w, f, o.w);
-        }
+        const float f = __builtin_amdgcn_exp2f(ml[i].x - use);
+        l = fmaf(ml[i].y, f, l);
+        o.x = fmaf(x[i].x, f, o.x), o.y = fmaf(x[i].y, f, o.y);
+        o.z = fmaf(x[i].z, f, o.z), o.w = fmaf(x[i].w, f, o.w);
       }
     }
     float top = fmaxf(m, other32(m));
@@ -973,35 +1011,105 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
       return PPW == 4 ? v + other16(v) : v;
     };
     l = sum(l);
+    o = make_float4(sum(o.x), sum(o.y), sum(o.z), sum(o.w));
+    if constexpr (W > 1) {
+      if (lane < LPP) s_o[wid][lane] = o;
+      if (lane == 0) s_ml[wid] = make_float2(top, l);
+      __syncthreads();
+      if (wid == 0) {
+        float t2 = top;
+#pragma unroll
+        for (int i = 1; i < W; ++i) t2 = fmaxf(t2, s_ml[i].x);
+        const float use = t2 == -INFINITY ? 0.0f : t2;
+        l = 0.0f;
+        o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const float2 ml = s_ml[i];
+          const float4 x = s_o[i][e4];
+          const float fi = __builtin_amdgcn_exp2f(ml.x - use);
+          l = fmaf(ml.y, fi, l);
+          o.x = fmaf(x.x, fi, o.x), o.y = fmaf(x.y, fi, o.y), o.z = fmaf(x.z, fi, o.z), o.w = fmaf(x.w, fi, o.w);
+        }
+      }
+    }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const uint2 y = make_uint2(pack2<BF>(sum(o.x) * inv, sum(o.y) * inv), pack2<BF>(sum(o.z) * inv, sum(o.w) * inv));
-    if (sub == 0) *reinterpret_cast<uint2*>(a.po + row_offset(a.o, row, hq) + e4 * 8) = y;
+    if (sub == 0)
+      *reinterpret_cast<uint2*>(a.po + row_offset(a.o, row, hq) + e4 * 8) =
+          make_uint2(pack2<BF>(o.x * inv, o.y * inv), pack2<BF>(o.z * inv, o.w * inv));
+    if (W > 1) __syncthreads();  // the boxes are the next row's
   }
 }
 
-template <class K>
-hipError_t run_walk(K kernel, const PagedArgs& a, const PagedPass& p, hipStream_t s) {
-  kernel<<<dim3(p.grid), dim3(kThreads), (p.n + 1) * sizeof(Seg), s>>>(a, p);
+// One pass alone, and both passes of a call with groups in one launch: the
+// first workgroups walk the shared keys, the others the sequences' own, which
+// then fill the CUs as the first ones end.
+template <int D, bool BF, int COLS>
+__global__ __launch_bounds__(kThreads, COLS == 32 && D > 64 ? 1 : 2) void paged_kernel(const PagedArgs a,
+                                                                                      const PagedPass ps) {
+  extern __shared__ __attribute__((aligned(16))) char dyn[];
+  Seg* seg = reinterpret_cast<Seg*>(dyn);
+  if constexpr (COLS <= 32) {
+    __shared__ FewShared<D> sh;
+    walk_few<D, BF, COLS>(a, ps, seg, sh, blockIdx.x);
+  } else {
+    __shared__ ManyShared<D> sh;
+    walk_many<D, BF, COLS>(a, ps, seg, sh, blockIdx.x);
+  }
+}
+template <int D, bool BF, int OWN, int SHARED>
+__global__ __launch_bounds__(kThreads, OWN == 32 && D > 64 ? 1 : 2) void paged_both_kernel(const PagedArgs a,
+                                                                                          const PagedPass own,
+                                                                                          const PagedPass shared) {
+  extern __shared__ __attribute__((aligned(16))) char dyn[];
+  Seg* seg = reinterpret_cast<Seg*>(dyn);
+  __shared__ union Both {
+    __device__ Both() {}
+    FewShared<D> few;
+    ManyShared<D> many;
+  } sh;
+  if ((int)blockIdx.x < shared.grid) walk_many<D, BF, SHARED>(a, shared, seg, sh.many, blockIdx.x);
+  else walk_few<D, BF, OWN>(a, own, seg, sh.few, blockIdx.x - shared.grid);
+}
+
+template <int D, bool BF>
+hipError_t run_pass(const PagedArgs& a, const PagedPass& p, hipStream_t s) {
+  const dim3 g(p.grid), b(kThreads);
+  const size_t lds = (p.n + 1) * sizeof(Seg);
+  if (p.cols == 16) paged_kernel<D, BF, 16><<<g, b, lds, s>>>(a, p);
+  else if (p.cols == 32) paged_kernel<D, BF, 32><<<g, b, lds, s>>>(a, p);
+  else if (p.cols == 64) paged_kernel<D, BF, 64><<<g, b, lds, s>>>(a, p);
+  else paged_kernel<D, BF, 128><<<g, b, lds, s>>>(a, p);
   return hipGetLastError();
 }
 template <int D, bool BF>
-hipError_t run_pass(const PagedArgs& a, const PagedPass& p, hipStream_t s) {
-  if (p.cols == 16) return run_walk(paged_kernel<D, BF, 1>, a, p, s);
-  if (p.cols == 32) return run_walk(paged_kernel<D, BF, 2>, a, p, s);
-  if (p.cols == 64) return run_walk(paged_wide_kernel<D, BF, 2>, a, p, s);
-  return run_walk(paged_wide_kernel<D, BF, 4>, a, p, s);
+hipError_t run_both(const PagedArgs& a, const PagedPass& own, const PagedPass& sh, hipStream_t s) {
+  const dim3 g(sh.grid + own.grid), b(kThreads);
+  const size_t lds = ((own.n > sh.n ? own.n : sh.n) + 1) * sizeof(Seg);
+  if (own.cols == 16 && sh.cols == 64) paged_both_kernel<D, BF, 16, 64><<<g, b, lds, s>>>(a, own, sh);
+  else if (own.cols == 16) paged_both_kernel<D, BF, 16, 128><<<g, b, lds, s>>>(a, own, sh);
+  else if (sh.cols == 64) paged_both_kernel<D, BF, 32, 64><<<g, b, lds, s>>>(a, own, sh);
+  else paged_both_kernel<D, BF, 32, 128><<<g, b, lds, s>>>(a, own, sh);
+  return hipGetLastError();
 }
 
 template <int D, bool BF>
 hipError_t run_paged(const PagedArgs& a, const PagedPass& sh, const PagedPass& own, hipStream_t s) {
   hipError_t e;
-  // the sequences first: their pass says how far every row sees
-  if ((e = run_pass<D, BF>(a, own, s)) != hipSuccess) return e;
-  if (own.fused) return e;
-  if (sh.n && (e = run_pass<D, BF>(a, sh, s)) != hipSuccess) return e;
+  if (sh.n && own.cols <= 32) {
+    if ((e = run_both<D, BF>(a, own, sh, s)) != hipSuccess) return e;
+  } else {
+    if ((e = run_pass<D, BF>(a, own, s)) != hipSuccess || own.fused) return e;
+    if (sh.n && (e = run_pass<D, BF>(a, sh, s)) != hipSuccess) return e;
+  }
   const int64_t avg = (a.rows + (int64_t)a.n_seq - 1) / a.n_seq;
-  const dim3 jg(a.n_seq, (a.hkv * a.g + kWaves - 1) / kWaves, (uint32_t)(avg < 64 ? avg : 64));
-  paged_join_kernel<D, BF><<<jg, dim3(kThreads), 0, s>>>(a, sh, own);
+  const int heads = a.hkv * a.g;
+  const uint32_t z = (uint32_t)(avg < 64 ? avg : 64);
+  // many parts a row: all the waves of a workgroup join them
+  if (sh.n && sh.grid / (2 * sh.tiles) >= 8)
+    paged_join_kernel<D, BF, kWaves><<<dim3(a.n_seq, heads, z), dim3(kThreads), 0, s>>>(a, sh, own);
+  else
+    paged_join_kernel<D, BF, 1><<<dim3(a.n_seq, (heads + kWaves - 1) / kWaves, z), dim3(kThreads), 0, s>>>(a, sh, own);
   return hipGetLastError();
 }
 
