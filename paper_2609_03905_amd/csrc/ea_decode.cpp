@@ -401,6 +401,7 @@ int check_pages(const ea_pages* p, PagesArgs* a) {
     return fail(EA_ERR_ARG, "NULL array");
   a->n_seq = p->n_seq;
   a->stride = p->stride;
+  a->row = fast_div((uint32_t)p->stride);
   a->n_pages = p->n_pages;
   a->page_size = p->page_size;
   a->table = p->table;

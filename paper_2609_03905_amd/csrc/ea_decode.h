@@ -135,6 +135,7 @@ hipError_t launch_paged(const PagedArgs& a, const PagedPass& shared, const Paged
 // ---- the page table -------------------------------------------------------------
 struct PagesArgs {
   int32_t n_seq, stride, n_pages, page_size;
+  FastDiv row;  // by stride
   const int32_t *table, *len, *refs;
   int32_t *out_table, *out_len, *out_refs, *status;
   // extend
