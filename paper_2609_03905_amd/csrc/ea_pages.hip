@@ -30,6 +30,8 @@ constexpr int kCopyThreads = 256, kCopyWgs = 2048;
 constexpr int kWorkCount = 0;   // pages to move
 constexpr int kWorkLists = 16;  // then source pages, destinations and rows
 
+constexpr int kList = 4096;     // pages that extend hands out at a time
+
 __device__ __forceinline__ int held(int len, int page) { return (len + page - 1) / page; }
 
 // A barrier after which every wave of the workgroup sees the others' writes and
@@ -90,7 +92,7 @@ __device__ __forceinline__ i32x4_t load_refs(const int32_t* refs, int p, int n_p
   return s;
 }
 
-constexpr int kBatch = 8;  // loads of a wave in flight: 8 * 256 pages
+constexpr int kBatch = 16;  // loads of a wave in flight: 16 * 256 pages
 
 // Free pages before each wave's range, and in all (s: kMetaWaves ints).
 __device__ __forceinline__ int free_before(const int32_t* refs, int n_pages, int* s, int* total) {
@@ -103,9 +105,9 @@ __device__ __forceinline__ int free_before(const int32_t* refs, int n_pages, int
     for (int i = 0; i < kBatch; ++i) r[i] = load_refs(refs, p0 + 256 * i + 4 * lane, n_pages);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int p = p0 + 256 * i + 4 * lane;
+      const int left = end - (p0 + 256 * i + 4 * lane);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) n += p + e < end && r[i][e] <= 0;
+      for (int e = 0; e < 4; ++e) n += e < left && r[i][e] <= 0;
     }
   }
 #pragma unroll
@@ -122,22 +124,27 @@ __device__ __forceinline__ int free_before(const int32_t* refs, int n_pages, int
   return before;
 }
 
-// Walk of a wave's pages in order: out[page] = f(page, refs, rank among the
-// free pages), stored where it may differ (out null: nowhere).
+// Walk of a wave's pages in order: f(page, refs, rank among the free pages),
+// until the rank `limit`; copies the counts to `copy` (null: no copy) on the
+// way, to the end.
 template <class F>
-__device__ __forceinline__ void each_page(const int32_t* refs, int32_t* out, int n_pages, int before, F f) {
+__device__ __forceinline__ void each_page(const int32_t* refs, int32_t* copy, int n_pages, int before, int limit, F f) {
+  constexpr int kAhead = 4;
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   int begin, end;
   wave_range(n_pages, wid, &begin, &end);
-  int run = before;
-  for (int p0 = begin; p0 < end; p0 += 256 * kBatch) {
-    i32x4_t batch[kBatch];
+  int run = __builtin_amdgcn_readfirstlane(before);
+  i32x4_t ahead[kAhead];
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) batch[i] = load_refs(refs, p0 + 256 * i + 4 * lane, n_pages);
+  for (int i = 0; i < kAhead; ++i) ahead[i] = load_refs(refs, begin + 256 * i + 4 * lane, n_pages);
+  for (int p0 = begin; p0 < end; p0 += 256) {
+    if (run >= limit && !copy) return;
+    const int p = p0 + 4 * lane;
+    const i32x4_t v = ahead[0];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int p = p0 + 256 * k + 4 * lane;
-      const i32x4_t v = batch[k];
+    for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+    ahead[kAhead - 1] = load_refs(refs, p + 256 * kAhead, n_pages);
+    if (run < limit) {
       int rank = run, all = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -146,22 +153,20 @@ __device__ __forceinline__ void each_page(const int32_t* refs, int32_t* out, int
         all += __popcll(b);
       }
       run += all;
-      if (p >= end) continue;
-      i32x4_t y = v;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (p + i < end) {
-          y[i] = f(p + i, v[i], rank);
+          f(p + i, v[i], rank);
           rank += v[i] <= 0;
         }
-      if (!out || (out == refs && y[0] == v[0] && y[1] == v[1] && y[2] == v[2] && y[3] == v[3])) continue;
-      if (p + 3 < end) {
-        *reinterpret_cast<i32x4_t*>(out + p) = y;
-      } else {
+    }
+    if (!copy) continue;
+    if (p + 3 < end) {
+      *reinterpret_cast<i32x4_t*>(copy + p) = v;
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (p + i < end) out[p + i] = y[i];
-      }
+      for (int i = 0; i < 4; ++i)
+        if (p + i < end) copy[p + i] = v[i];
     }
   }
 }
@@ -188,6 +193,7 @@ __device__ __forceinline__ void set_status(const PagesArgs& a, int code, int lef
 // new tokens, sequence by sequence.
 __global__ __launch_bounds__(kMetaThreads) void extend_kernel(const PagesArgs a) {
   __shared__ int s_need[kMaxSeq], s_tok[kMaxSeq], s_len[kMaxSeq];  // exclusive sums over sequences
+  __shared__ int s_list[kList];
   __shared__ int s_wave[kMetaWaves];
   const int tid = threadIdx.x;
   const int per = (a.n_seq + kMetaThreads - 1) / kMetaThreads;
@@ -214,17 +220,31 @@ __global__ __launch_bounds__(kMetaThreads) void extend_kernel(const PagesArgs a)
   }
   bad = __syncthreads_or(bad);
   int all_free;
-  const int before = free_before(a.refs, a.n_pages, s_wave, &all_free);
+  int before = free_before(a.refs, a.n_pages, s_wave, &all_free);
   const int code = bad ? EA_PAGES_TOO_LONG : all_need > all_free ? EA_PAGES_NONE_FREE : 0;
-  if (code) need = all_need = all_tok = 0;
-  each_page(a.refs, a.out_refs, a.n_pages, before, [&](int p, int refs, int rank) {
-    const bool take = refs <= 0 && rank < all_need;
-    if (take) {
-      const int s = last_at_most(s_need, a.n_seq, rank);
-      a.out_table[(int64_t)s * a.stride + held(s_len[s], a.page_size) + rank - s_need[s]] = p;
+  if (code) all_need = all_tok = 0;
+  // the lowest free pages into a list, as many as it holds at a time; then a
+  // thread each to hand them out
+  const int32_t* from = a.refs;
+  int32_t* copy = a.out_refs == a.refs ? nullptr : a.out_refs;
+  for (int base = 0; base == 0 || base < all_need; base += kList) {
+    const int n = min(kList, all_need - base);
+    each_page(from, copy, a.n_pages, before, n, [&](int p, int refs, int rank) {
+      if (refs <= 0 && rank < n) s_list[rank] = p;
+    });
+    settle();
+    for (int i = tid; i < n; i += kMetaThreads) {
+      const int s = last_at_most(s_need, a.n_seq, base + i), p = s_list[i];
+      a.out_table[(int64_t)s * a.stride + held(s_len[s], a.page_size) + base + i - s_need[s]] = p;
+      a.out_refs[p] = 1;
     }
-    return take ? 1 : refs;
-  });
+    if (base + n >= all_need) break;
+    settle();  // the pages handed out are no longer free
+    from = a.out_refs;
+    copy = nullptr;
+    int left;
+    before = free_before(from, a.n_pages, s_wave, &left);
+  }
   set_status(a, code, all_free - all_need);
   settle();
   for (int t = tid; t < a.n_tokens; t += kMetaThreads) {
@@ -331,13 +351,15 @@ __global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a)
   const int before = free_before(a.out_refs, a.n_pages, s_wave, &all_free);
   const int code = bad ? EA_PAGES_TOO_LONG : count > all_free ? EA_PAGES_NONE_FREE : 0;
   if (!code) {
-    each_page(a.out_refs, a.out_refs, a.n_pages, before, [&](int p, int refs, int r) {
-      if (refs > 0 || r >= count) return refs;
-      const int i = who[r], at = s_len[s_parent[i]] / a.page_size;
-      dst[r] = p;
-      a.out_table[(int64_t)i * a.stride + at] = p;
-      return 1;
+    each_page(a.out_refs, nullptr, a.n_pages, before, count, [&](int p, int refs, int r) {
+      if (refs <= 0 && r < count) dst[r] = p;
     });
+    settle();
+    for (int r = tid; r < count; r += kMetaThreads) {
+      const int i = who[r], at = s_len[s_parent[i]] / a.page_size, p = dst[r];
+      a.out_refs[p] = 1;
+      a.out_table[(int64_t)i * a.stride + at] = p;
+    }
     if (tid == 0) a.work[kWorkCount] = count;
     set_status(a, 0, all_free - count);
     return;
@@ -371,20 +393,18 @@ __global__ __launch_bounds__(kMetaThreads) void compact_kernel(const PagesArgs a
   const int n_used = a.n_pages - all_free;
   if (tid == 0) s_moves = 0;
   __syncthreads();
-  each_page(a.refs, nullptr, a.n_pages, before, [&](int p, int refs, int free_rank) {
+  each_page(a.refs, nullptr, a.n_pages, before, 0x7fffffff, [&](int p, int refs, int free_rank) {
     to[p] = p;
     if (p < n_used && refs <= 0) dst[free_rank] = p;
     // the free pages before n_used are as many as the used ones behind it:
     // a used page's rank among the latter is its rank among the used ones
     // less those before n_used
     if (p == n_used - 1) s_moves = free_rank + (refs <= 0);
-    return refs;
   });
   settle();
   const int moves = s_moves;
-  each_page(a.refs, nullptr, a.n_pages, before, [&](int p, int refs, int free_rank) {
+  each_page(a.refs, nullptr, a.n_pages, before, 0x7fffffff, [&](int p, int refs, int free_rank) {
     if (p >= n_used && refs > 0) src[p - free_rank - (n_used - moves)] = p;
-    return refs;
   });
   settle();
   // every count is read before a thread writes another's (they may be updated

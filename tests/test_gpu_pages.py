@@ -113,6 +113,21 @@ def test_nothing_is_done_without_pages():
     dev.same(ref)
 
 
+@pytest.mark.parametrize("in_place", [True, False])
+def test_more_pages_than_one_round_hands_out(in_place):
+    """9000 new pages in one call, the cache a third full of holes, page counts
+    that no four divides."""
+    n, stride, n_pages, page = 3, 4000, 13001, 2
+    ref = R.Pages(n, stride, n_pages, page)
+    ref.refs[1::3] = 1  # held by somebody else
+    ref.len[1], ref.table[1, 0], ref.refs[5] = 1, 5, 1
+    dev = Device(ref)
+    for add in ([6000, 3999, 3001], [0, 0, 4300], [1, 1, 1]):
+        want, got = ref.extend(add, sum(add) + 5), dev.extend(add, sum(add) + 5, in_place)
+        assert got[0] == want[0] and np.array_equal(got[1], want[1]) and np.array_equal(got[2], want[2])
+        dev.same(ref)
+
+
 def test_a_fork_that_fits_nowhere_does_nothing():
     ref = R.Pages(2, 3, 2, 4)
     dev = Device(ref)
