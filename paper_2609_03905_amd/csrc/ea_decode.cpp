@@ -83,6 +83,14 @@ bool overlap(const ea_relation* a, const ea_relation* b) {
   return a && b && overlap(a->data, a->nbytes, b->data, b->nbytes);
 }
 
+// Equal dtype, shape and partition (layout ids may differ where these do not).
+bool same_layout(const ea_relation* a, const ea_relation* b) {
+  if (a->dtype != b->dtype || a->rank != b->rank) return false;
+  for (int d = 0; d < a->rank; ++d)
+    if (a->splits[d] != b->splits[d]) return false;
+  return true;
+}
+
 int check_weights(const ea_relation* w, int32_t d, const char* what) {
   const int e = check_rel(w, what, true);
   if (e) return e;
@@ -197,7 +205,7 @@ int ea_heads_backward(const ea_relation* qkv, const ea_relation* wq, const ea_re
   if (e) return e;
   if (params->slots) return fail(EA_ERR_ARG, "the gradient takes no slots");
   if ((e = check_rel(dqkv, "dqkv", true))) return e;
-  if (dqkv->layout != qkv->layout) return fail(EA_ERR_ARG, "dqkv and qkv differ in dtype, shape or partition");
+  if (!same_layout(dqkv, qkv)) return fail(EA_ERR_ARG, "dqkv and qkv differ in dtype, shape or partition");
   if ((dwq || dwk) && !wq) return fail(EA_ERR_ARG, "gradients of norm weights that are not given");
   if (dwq && (e = check_weights(dwq, params->d_head, "dwq"))) return e;
   if (dwk && (e = check_weights(dwk, params->d_head, "dwk"))) return e;

@@ -7,6 +7,7 @@ compute function raises: there is no fallback path.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import Sequence
@@ -128,8 +129,20 @@ def _arr(ctype, values):
 
 def _partition_args(partition):
     nb = _arr(ctypes.c_int32, [len(s) - 1 for s in partition])
-    sp = _arr(ctypes.c_int64, [int(p) for s in partition for p in s])
-    return nb, sp
+    flat = array.array("q")
+    for s in partition:
+        flat += _points(s)
+    if not flat:
+        return nb, _arr(ctypes.c_int64, [])
+    return nb, (ctypes.c_int64 * len(flat)).from_buffer(flat)
+
+
+def _points(s) -> array.array:
+    """Split points as 64-bit integers (a cache has one a page: tens of thousands)."""
+    try:
+        return array.array("q", s)
+    except TypeError:
+        return array.array("q", map(int, s))
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -185,8 +198,11 @@ class Relation:
                  device: str | torch.device = "cuda", allocate: bool = True, byte_offset: int = 0):
         self.shape = tuple(int(s) for s in shape)
         self.dtype = dtype
-        self.partition = [list(map(int, s)) for s in partition]
-        self.nbytes = layout_nbytes(self.shape, dtype, self.partition)
+        self.partition = [_points(s).tolist() for s in partition]
+        nb, sp = _partition_args(self.partition)
+        shp, n = _arr(ctypes.c_int64, self.shape), ctypes.c_int64()
+        _check(lib().ea_layout_nbytes(len(self.shape), shp, DTYPES[dtype], nb, sp, ctypes.byref(n)))
+        self.nbytes = int(n.value)
         if data is None and allocate:
             data = torch.empty(max(self.nbytes, 1), dtype=torch.uint8, device=device)
         self.data = data
@@ -195,10 +211,9 @@ class Relation:
         if data is not None:
             ptr = data.data_ptr() + self._byte_offset
             cap = data.numel() * data.element_size() - self._byte_offset
-        nb, sp = _partition_args(self.partition)
         self._device = -1 if data is None else data.get_device()
         h = ctypes.c_void_p()
-        _check(lib().ea_relation_create(len(self.shape), _arr(ctypes.c_int64, self.shape), DTYPES[dtype], nb, sp,
+        _check(lib().ea_relation_create(len(self.shape), shp, DTYPES[dtype], nb, sp,
                                         ctypes.c_void_p(ptr) if ptr else None, cap, ctypes.byref(h)))
         self.handle = h
         self._h = h.value  # the handle as a plain integer
