@@ -19,14 +19,21 @@ one row block and 128-wide column blocks, so head h of Q, K or V is one
 contiguous [T, 128] block; Q, K and V are then viewed, without a copy, as
 [1, heads, T, 128] relations with 128-row blocks (the same bytes).  The
 attention output is viewed back as [T, heads*128] with 128-wide column blocks
-before the second repartition.  This module only sequences calls: every step
-runs in libea's kernels.
+before the second repartition.
+
+With position frequencies (``inv_freq``) or per-head norms of queries and keys
+(``qk_norm``) the first repartition is a call of ea.heads, which does both on
+the way to the heads.  LlamaBlockDecode runs the newest tokens of several
+sequences through a share's weights over a KVCache, without repartitions: the
+head rows go to the cache's pages, and attention reads and writes token rows.
+This module only sequences calls: every step runs in libea's kernels.
 """
 from __future__ import annotations
 
 import torch
 
 from . import ea
+from .cache import KVCache
 
 
 def _splits(n: int, b: int):
@@ -35,12 +42,19 @@ def _splits(n: int, b: int):
 
 class LlamaBlockShare:
     def __init__(self, t: int, hidden: int, heads: int, d_head: int, ffn: int, block: int = 512,
-                 eps: float = 1e-6, device="cuda", heads_kv: int | None = None, seq_ends=None):
+                 eps: float = 1e-6, device="cuda", heads_kv: int | None = None, seq_ends=None,
+                 inv_freq: torch.Tensor | None = None, interleaved: bool = False, qk_norm: bool = False):
         assert d_head == 128, "the attention join-agg takes head dim 128"
         heads_kv = heads if heads_kv is None else heads_kv
         assert heads % heads_kv == 0, "query heads must be a multiple of key/value heads"
         self.t, self.hidden, self.heads, self.d_head, self.ffn = t, hidden, heads, d_head, ffn
         self.heads_kv, self.seq_ends = heads_kv, None if seq_ends is None else [int(e) for e in seq_ends]
+        self.inv_freq, self.interleaved, self.qk_norm = inv_freq, interleaved, qk_norm
+        self.positions = None  # the token's index in its sequence (None: in the relation)
+        if self.seq_ends is not None:
+            lens = [e - s for s, e in zip([0] + self.seq_ends[:-1], self.seq_ends)]
+            self.positions = torch.cat([torch.arange(n, dtype=torch.int32) for n in lens]).to(device)
+        self.block = block
         self.eps = eps
         self.scale = 1.0 / d_head ** 0.5
         hd = heads * d_head
@@ -52,6 +66,8 @@ class LlamaBlockShare:
         # parameters (filled by load())
         self.n1 = R((hidden,), [ph])
         self.n2 = R((hidden,), [ph])
+        self.qn = R((d_head,), [[0, d_head]]) if qk_norm else None
+        self.kn = R((d_head,), [[0, d_head]]) if qk_norm else None
         self.wqkv = R((hidden, wqkv), [ph, pqkv])
         self.wo = R((hd, hidden), [phd, ph])
         self.wg = R((hidden, ffn), [ph, pf])
@@ -81,7 +97,7 @@ class LlamaBlockShare:
         """Copy dense bf16 tensors (uint16/int16 storage on the device) into
         the block-partitioned parameter and input relations (re-blocked by
         the library's repartition)."""
-        for name in ("x", "n1", "n2", "wqkv", "wo", "wg", "wu", "wd"):
+        for name in ("x", "n1", "n2", "wqkv", "wo", "wg", "wu", "wd") + (("qn", "kn") if self.qk_norm else ()):
             rel = getattr(self, name)
             src = ea.Relation(rel.shape, "bf16", ea.whole_partition(rel.shape),
                               data=dense[name].contiguous().view(torch.uint8).reshape(-1))
@@ -95,7 +111,7 @@ class LlamaBlockShare:
         return [
             ("rmsnorm1", lambda: J("tc,c->tc", ea.OP_RMSNORM, S, [self.x, self.n1], self.h1, eps=self.eps)),
             ("qkv_gemm", lambda: J("tj,jk->tk", ea.JOIN_MUL, S, [self.h1, self.wqkv], self.qkv)),
-            ("repart_heads", lambda: ea.repartition(self.qkv, self.qkv_heads)),
+            ("repart_heads", self._to_heads),
             ("attention", lambda: J(attn_spec, ea.OP_ATTENTION, ea.AGG_LSE, [self.q, self.k, self.v], self.o,
                                     scale=self.scale, causal=True, gqa_group=group, seq_ends=self.seq_ends)),
             ("repart_cols", lambda: ea.repartition(self.o_cols, self.attn)),
@@ -106,6 +122,21 @@ class LlamaBlockShare:
             ("down_gemm_residual", lambda: J("tj,jk->tk", ea.JOIN_MUL, S, [self.a, self.wd], self.y,
                                              residual=self.x2)),
         ]
+
+    def _to_heads(self):
+        if self.inv_freq is None and not self.qk_norm:
+            ea.repartition(self.qkv, self.qkv_heads)
+        else:
+            ea.heads(self.qkv, self.q, self.k, self.v, **self.head_options(self.positions))
+
+    def head_options(self, positions):
+        return dict(d_head=self.d_head, wq=self.qn, wk=self.kn, eps=self.eps, inv_freq=self.inv_freq,
+                    interleaved=self.interleaved, positions=positions)
+
+    def store(self, cache: KVCache, slots: torch.Tensor, layer: int = 0):
+        """The last forward's keys and values to the cache: token t to slot
+        slots[t] (queries are written again, as they are)."""
+        ea.heads(self.qkv, self.q, cache.k[layer], cache.v[layer], slots=slots, **self.head_options(self.positions))
 
     def forward(self):
         for _, fn in self.stages():
@@ -131,3 +162,46 @@ class LlamaBlockShare:
             "swiglu_gemm": dict(flops=2 * 2 * T * Hd * F),
             "down_gemm_residual": dict(flops=2 * T * F * Hd),
         }
+
+
+class LlamaBlockDecode:
+    """The newest tokens of the cache's sequences through a share's weights:
+    ``rows`` tokens a step (x: [rows, hidden], sequence by sequence), their
+    slots and positions from cache.extend."""
+
+    def __init__(self, share: LlamaBlockShare, cache: KVCache, rows: int, layer: int = 0, device="cuda"):
+        self.share, self.cache, self.rows, self.layer = share, cache, rows, layer
+        s, block = share, share.block
+        pt, ph, pf = _splits(rows, block), _splits(s.hidden, block), _splits(s.ffn, block)
+        phd, pqkv = _splits(s.hd, block), s.wqkv.partition[1]
+        R = lambda shape, part: ea.Relation(shape, "bf16", part, device=device)
+        self.x = R((rows, s.hidden), [pt, ph])
+        self.h1 = R((rows, s.hidden), [pt, ph])
+        self.qkv = R((rows, s.wqkv.shape[1]), [pt, pqkv])
+        self.q = R((rows, s.hd), [pt, phd])
+        self.attn = R((rows, s.hd), [pt, phd])
+        self.x2 = R((rows, s.hidden), [pt, ph])
+        self.h2 = R((rows, s.hidden), [pt, ph])
+        self.a = R((rows, s.ffn), [pt, pf])
+        self.y = R((rows, s.hidden), [pt, ph])
+
+    def stages(self, slots, positions, q_start=None, group_start=None, group_shared=None):
+        J, S, s, c = ea.joinagg, ea.AGG_SUM, self.share, self.cache
+        k, v = c.k[self.layer], c.v[self.layer]
+        return [
+            ("rmsnorm1", lambda: J("tc,c->tc", ea.OP_RMSNORM, S, [self.x, s.n1], self.h1, eps=s.eps)),
+            ("qkv_gemm", lambda: J("tj,jk->tk", ea.JOIN_MUL, S, [self.h1, s.wqkv], self.qkv)),
+            ("heads", lambda: ea.heads(self.qkv, self.q, k, v, slots=slots, **s.head_options(positions))),
+            ("attention", lambda: ea.attention_paged(self.q, k, v, self.attn, scale=s.scale, table=c.table,
+                                                     lengths=c.lengths, q_start=q_start, group_start=group_start,
+                                                     group_shared=group_shared)),
+            ("o_gemm_residual", lambda: J("tj,jk->tk", ea.JOIN_MUL, S, [self.attn, s.wo], self.x2, residual=self.x)),
+            ("rmsnorm2", lambda: J("tc,c->tc", ea.OP_RMSNORM, S, [self.x2, s.n2], self.h2, eps=s.eps)),
+            ("swiglu_gemm", lambda: J("tj,jk,jk->tk", ea.OP_SWIGLU, S, [self.h2, s.wg, s.wu], self.a)),
+            ("down_gemm_residual", lambda: J("tj,jk->tk", ea.JOIN_MUL, S, [self.a, s.wd], self.y, residual=self.x2)),
+        ]
+
+    def step(self, slots, positions, **batch):
+        for _, fn in self.stages(slots, positions, **batch):
+            fn()
+        return self.y
