@@ -263,19 +263,19 @@ struct PagedPlan {
 };
 
 // A pass over n segments of `cols` query columns in all, by the columns that a
-// segment has on the average: up to 16 or 32, the walk that loads keys into
-// registers (at 32 columns of width 128 its registers admit one workgroup a
-// CU); beyond, and for shared keys, the walk through shared memory, on tiles of
-// 64 or 128 columns, a step on the narrower costing about 0.55 of one on the
-// wider.
+// segment has on the average: up to 32, the walk that loads keys into registers
+// (tiles of 32 columns at width 64; at 128 its registers would admit one
+// workgroup a CU, and two tiles of 16, the second fed by the L2, are faster);
+// beyond, and for shared keys, the walk through shared memory, on tiles of 64 or
+// 128 columns, a step on the narrower costing about 0.55 of one on the wider.
 void plan_pass(PagedPass* p, bool shared, int first, int n, int64_t cols, int64_t hkv, int64_t d) {
   p->shared = shared;
   p->first = first;
   p->n = n;
   const int64_t avg = n ? (cols + n - 1) / n : 0;
-  if (avg <= 32 && !shared) p->cols = avg > 16 ? 32 : 16;
+  if (avg <= 32 && !shared) p->cols = avg > 16 && d == 64 ? 32 : 16;
   else p->cols = 0.55 * (double)((avg + 63) / 64) < (double)((avg + 127) / 128) ? 64 : 128;
-  p->grid = p->cols == 32 && d == 128 ? 256 : 512;
+  p->grid = 512;  // two workgroups a CU
   const int64_t tiles = (cols / p->cols + n) * hkv;
   p->tiles = (int32_t)(tiles < INT32_MAX ? tiles : INT32_MAX);
 }
@@ -299,9 +299,10 @@ int plan_paged(const ea_relation* q, const ea_relation* k, const ea_paged* b, bo
   const int64_t cols = (int64_t)mq->t * (mq->h / hkv);
   plan_pass(&p->shared, true, 0, b->n_group, cols, hkv, d);
   plan_pass(&p->own, false, b->n_group, b->n_seq, cols, hkv, d);
-  // without groups, and few tiles enough for the arrival counters, the last
-  // part of a tile joins them and no second launch follows
-  p->own.fused = b->n_group == 0 && p->own.cols <= 32 && p->own.tiles <= kWsCounterBytes / 4;
+  // without groups, where the arrival counters suffice and a tile has not more
+  // than 64 parts, the last one to arrive joins them and no second launch follows
+  p->own.fused = b->n_group == 0 && p->own.cols <= 32 && p->own.tiles <= kWsCounterBytes / 4 &&
+                 p->own.tiles * 64 >= p->own.grid;
   p->seg = kWsCounterBytes;
   int64_t at = p->seg + align256((b->n_seq + b->n_group) * (int64_t)sizeof(PagedSeg));
   int i = 0;

@@ -102,7 +102,7 @@ struct PagedSeg {  // what the join needs of a segment
   int32_t step, steps;  // first step of its first tile's walk; steps of a walk
   int32_t tile, tiles;  // first tile; tiles of a head
   int32_t group;        // own keys: the sequence's group or -1
-  int32_t total;        // steps of the launch
+  int32_t total, parts; // steps of the pass, and parts they are cut in
 };
 
 // One launch of the walk: the groups' shared keys, or the sequences' own.

@@ -97,12 +97,8 @@ __device__ __forceinline__ int first_row(const PagedArgs& a, int s) {
 struct Segment {
   int r0, r1;  // query rows
   int k0, k1;  // keys
+  int seq;     // whose table row lists the pages
 };
-
-// The sequence whose table row lists a segment's pages.
-__device__ __forceinline__ int table_row(const PagedArgs& a, const PagedPass& ps, int i) {
-  return ps.shared ? clampi(a.group_start[i], 0, a.n_seq - 1) : i;
-}
 
 // Keys that group g shares (no more than a table row holds).
 __device__ __forceinline__ int shared_keys(const PagedArgs& a, int g) {
@@ -131,12 +127,14 @@ __device__ __forceinline__ Segment segment(const PagedArgs& a, int i) {
     s.r1 = max(first_row(a, s1), s.r0);
     s.k0 = 0;
     s.k1 = shared_keys(a, i);
+    s.seq = min(s0, a.n_seq - 1);
   } else {
     const int seq = i - a.n_group, g = group_of(a, seq);
     s.r0 = first_row(a, seq);
     s.r1 = max(first_row(a, seq + 1), s.r0);
     s.k1 = clampi(a.len[seq], 0, a.stride * a.page_size);
     s.k0 = g >= 0 ? min(shared_keys(a, g), s.k1) : 0;
+    s.seq = seq;
   }
   return s;
 }
@@ -147,6 +145,7 @@ struct Seg {
   int r0, rows;    // query rows
   int k0, k1;      // keys
   int step, tile;  // first step and first tile
+  int seq;         // whose table row lists the pages
 };
 
 __device__ __forceinline__ int add_most(int a, int b) { return (int)min((int64_t)a + b, (int64_t)0x7fffffff); }
@@ -169,10 +168,11 @@ __device__ __forceinline__ int tiles_of(int rows, int g, int cols) {
   return (int)(((int64_t)rows * g + cols - 1) / cols);
 }
 
-// Every segment's first step and tile, by the whole workgroup.  Also hands the
-// join what it needs.  Returns the steps of all.
-template <int D, int COLS, int KEYS>
-__device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps, Seg* seg, int block) {
+// Every segment's first step and tile, by the whole workgroup.  Returns the
+// steps of all; none where there are more tiles than the rows can have, that
+// is, where the sequences' rows overlap.
+template <int COLS, int KEYS>
+__device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps, Seg* seg) {
   __shared__ int s_wave[kWaves][2];
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int per = (ps.n + kThreads - 1) / kThreads;
@@ -183,12 +183,13 @@ __device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps,
     const int n = steps_of(s.k0, s.k1, KEYS);
     const int64_t t = n ? (int64_t)tiles_of(s.r1 - s.r0, a.g, COLS) * a.hkv : 0;
     Seg x;
-    x.r0 = s.r0, x.rows = s.r1 - s.r0, x.k0 = s.k0, x.k1 = s.k1, x.step = steps, x.tile = ntile;
+    x.r0 = s.r0, x.rows = s.r1 - s.r0, x.k0 = s.k0, x.k1 = s.k1, x.step = steps, x.tile = ntile, x.seq = s.seq;
     seg[i] = x;
     steps = (int)min((int64_t)steps + n * t, (int64_t)0x7fffffff);
     ntile = (int)min((int64_t)ntile + t, (int64_t)0x7fffffff);
   }
   int st = wave_scan(steps), ti = wave_scan(ntile);
+  __syncthreads();
   if (lane == 63) {
     s_wave[wid][0] = st;
     s_wave[wid][1] = ti;
@@ -207,30 +208,36 @@ __device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps,
     seg[i].tile = add_most(seg[i].tile, ti - ntile);
   }
   __syncthreads();
-  // more tiles than the rows can have: the sequences' rows overlap, no walk
-  const bool off = seg[ps.n].tile > ps.tiles;
-  const int total = off ? 0 : seg[ps.n].step;
-  for (int i = block; i < ps.n; i += ps.grid) {
+  return seg[ps.n].tile > ps.tiles ? 0 : seg[ps.n].step;
+}
+
+// What the join needs of a pass's segments (by workgroup `block` of n).
+template <int COLS, int KEYS>
+__device__ __forceinline__ void publish(const PagedArgs& a, const PagedPass& ps, const Seg* seg, int total, int parts,
+                                        int block, int n) {
+  for (int i = block * kThreads + threadIdx.x; i < ps.n; i += n * kThreads) {
     const Seg s = seg[i];
-    if (ps.fused) {  // rows of a sequence without keys: no walk reaches them
-      if (s.k1 > 0) continue;
-      const int n = a.hkv * a.g * (D / 8);
-      for (int j = tid; j < s.rows * n; j += kThreads) {
-        const int r = j / n, x = j - r * n;
-        *reinterpret_cast<uint4*>(a.po + row_offset(a.o, s.r0 + r, x / (D / 8)) + x % (D / 8) * 16) =
-            make_uint4(0, 0, 0, 0);
-      }
-      continue;
-    }
-    if (tid == 0) {
-      PagedSeg g;
-      g.r0 = s.r0, g.r1 = s.r0 + s.rows, g.step = s.step, g.steps = off ? 0 : steps_of(s.k0, s.k1, KEYS);
-      g.tile = s.tile, g.tiles = tiles_of(s.rows, a.g, COLS), g.group = ps.shared ? -1 : group_of(a, i);
-      g.total = total;
-      a.seg[ps.first + i] = g;
+    PagedSeg g;
+    g.r0 = s.r0, g.r1 = s.r0 + s.rows, g.step = s.step, g.steps = total ? steps_of(s.k0, s.k1, KEYS) : 0;
+    g.tile = s.tile, g.tiles = tiles_of(s.rows, a.g, COLS), g.total = total, g.parts = parts;
+    g.group = ps.shared ? -1 : group_of(a, i);
+    a.seg[ps.first + i] = g;
+  }
+}
+
+// Zeros in the rows of sequences without keys, which no walk reaches.
+template <int D>
+__device__ __forceinline__ void clear_empty(const PagedArgs& a, const PagedPass& ps, const Seg* seg) {
+  const int n = a.hkv * a.g * (D / 8);
+  for (int i = blockIdx.x; i < ps.n; i += gridDim.x) {
+    const Seg s = seg[i];
+    if (s.k1 > 0) continue;
+    for (int j = threadIdx.x; j < s.rows * n; j += kThreads) {
+      const int r = j / n, x = j - r * n;
+      *reinterpret_cast<uint4*>(a.po + row_offset(a.o, s.r0 + r, x / (D / 8)) + x % (D / 8) * 16) =
+          make_uint4(0, 0, 0, 0);
     }
   }
-  return total;
 }
 
 // The segment that step `at` belongs to (empty ones share a step).
@@ -244,28 +251,17 @@ __device__ __forceinline__ int find_segment(const Seg* seg, int n, int at) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Keys that query row `row`, the rr-th of segment i, sees.  In a group the
-// row's own sequence says so.
-__device__ __forceinline__ int limit_of(const PagedArgs& a, const PagedPass& ps, const Seg& s, int i, int row, int rr) {
-  if (!ps.shared) return s.k1 - s.rows + rr + 1;
-  int lo = clampi(a.group_start[i], 0, a.n_seq), hi = clampi(a.group_start[i + 1], lo, a.n_seq);
-  if (!a.q_start) lo = clampi(row, lo, hi);
-  else
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (first_row(a, mid) <= row) lo = mid;
-      else hi = mid;
-    }
-  lo = min(lo, a.n_seq - 1);
-  return clampi(a.len[lo], 0, a.stride * a.page_size) - (first_row(a, lo + 1) - row) + 1;
-}
-
-// Workgroups that share a walk of `total` steps: all of them, but at least
-// eight steps each of a walk over many columns while half of them remain (a
-// part leaves D floats a column behind, which the join reads again).
-__device__ __forceinline__ int parts_of(const PagedPass& p, int total) {
-  if (p.cols <= 32) return min(p.grid, total);
-  return min(max(total / 8, min(total, p.grid / 2)), p.grid);
+// Keys that query row `row`, the rr-th of segment s, sees.  In a group the
+// row's own sequence says so: `own` are the sequences' segments.
+__device__ __forceinline__ int limit_of(const PagedArgs& a, const Seg& s, const Seg* own, int row, int rr) {
+  if (!own) return s.k1 - s.rows + rr + 1;
+  int lo = s.seq, hi = a.n_seq;  // sequences' rows ascend
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (own[mid].r0 <= row) lo = mid;
+    else hi = mid;
+  }
+  return own[lo].k1 - own[lo].rows + row - own[lo].r0 + 1;
 }
 
 // VE neighbouring elements of an output row, scaled.
@@ -310,8 +306,8 @@ struct __attribute__((aligned(1024))) ManyShared {
 };
 
 template <int D, bool BF, int COLS>
-__device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps, Seg* seg, FewShared<D>& sh,
-                                         int block) {
+__device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps, const Seg* seg, FewShared<D>& sh,
+                                         int total, int parts, int block) {
   constexpr int NC = COLS / kPagedCols;
   constexpr int VE = D / 16;          // d elements a lane holds of a V row
   constexpr int KS = D / 32;          // k steps of the score product
@@ -322,8 +318,6 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int total = schedule<D, COLS, kPagedStep>(a, ps, seg, block), parts = parts_of(ps, total);
-  if (block >= parts) return;
   const int w = xcd_part(block, parts);
   int at = (int)((int64_t)total * w / parts);
   const int end = (int)((int64_t)total * (w + 1) / parts);
@@ -341,10 +335,10 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
     p.tile = p.it - p.h * tiles;
     const int walk = min(p.n - step, end - at);
     // the only result of these columns: no join
-    p.whole = !ps.shared && walk == p.n && p.s.k0 == 0;
+    p.whole = walk == p.n && p.s.k0 == 0;
     p.ka = p.s.k0 + step * kPagedStep;
     p.kb = (int)min((int64_t)p.s.k1, (int64_t)p.ka + (int64_t)walk * kPagedStep);
-    p.pages = a.table + (int64_t)table_row(a, ps, p.si) * a.stride;
+    p.pages = a.table + (int64_t)p.s.seq * a.stride;
     p.head_off = (int64_t)p.h * a.page_size * D * 2;
     at += walk;
     return p;
@@ -421,7 +415,7 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
 #pragma unroll
     for (int t = 0; t < NC; ++t) {
       const int col = tile * COLS + t * kPagedCols + c, rr = div_fast(min(col, ncol - 1), a.gdiv);
-      lim[t] = col < ncol ? limit_of(a, ps, s, cur.si, s.r0 + rr, rr) : 0x7fffffff;  // (never stored: no mask)
+      lim[t] = col < ncol ? limit_of(a, s, nullptr, s.r0 + rr, rr) : 0x7fffffff;  // (never stored: no mask)
       lim_min = min(lim_min, lim[t]);
     }
     lim_min = min(lim_min, __shfl_xor(lim_min, 1));
@@ -685,8 +679,8 @@ __device__ __forceinline__ void load_to_lds(const char* p, uint32_t lds) {
 }
 
 template <int D, bool BF, int COLS>
-__device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& ps, Seg* seg, ManyShared<D>& sh,
-                                          int block) {
+__device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& ps, const Seg* seg, const Seg* own,
+                                          ManyShared<D>& sh, int total, int parts, int block) {
   constexpr int CW = COLS / 32, KEYS = kPagedWideStep;
   constexpr int KT = CW / 2;          // 32-key tiles that a wave computes of a step
   constexpr int NS = D / 16, ND = D / 32;
@@ -700,8 +694,6 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
   const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, g = lane >> 5;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wc = wid % CW, wk = wid / CW;  // the wave's columns, and its part of a step's keys
-  const int total = schedule<D, COLS, KEYS>(a, ps, seg, block), parts = parts_of(ps, total);
-  if (block >= parts) return;
   const int w = xcd_part(block, parts);
   int at = (int)((int64_t)total * w / parts);
   const int end = (int)((int64_t)total * (w + 1) / parts);
@@ -720,7 +712,7 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
     const int kb = (int)min((int64_t)s.k1, (int64_t)ka + (int64_t)walk * KEYS);
     at += walk;
 
-    const int32_t* pages = a.table + (int64_t)table_row(a, ps, si) * a.stride;
+    const int32_t* pages = a.table + (int64_t)s.seq * a.stride;
     const int64_t head_off = (int64_t)h * a.page_size * D * 2;
     const char* kbase = a.pk + head_off;
     const char* vbase = a.pv + head_off;
@@ -761,7 +753,7 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
     // ---- this lane's column
     const int ncol = s.rows * a.g, col = tile * COLS + wc * 32 + lq, cc = min(col, ncol - 1);
     const int rr = div_fast(cc, a.gdiv), row = s.r0 + rr, head = h * a.g + cc - rr * a.g;
-    const int lim = col < ncol ? limit_of(a, ps, s, si, row, rr) : 0x7fffffff;  // (never stored: no mask)
+    const int lim = col < ncol ? limit_of(a, s, own, row, rr) : 0x7fffffff;  // (never stored: no mask)
     const bool idle = tile * COLS + wc * 32 >= ncol;  // a wave without columns only fetches
     uint4 q[NS];
     {
@@ -942,7 +934,7 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
 // head), D / 4 lanes a part, several parts at a time and eight loads of each in
 // flight; what the lane groups (and waves) hold is joined at the end.
 template <int D, bool BF, int W>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a, const PagedPass sh,
+__global__ __launch_bounds__(W > kWaves ? W * 64 : kThreads) void paged_join_kernel(const PagedArgs a, const PagedPass sh,
                                                               const PagedPass own) {
   constexpr int LPP = D / 4, PPW = 64 / LPP, STRIDE = PPW * W;
   __shared__ float4 s_o[W][LPP];
@@ -961,7 +953,7 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
       if (s.steps == 0) return 0;
       const int col = (row - s.r0) * a.g + hg, tile = col / p.cols;
       const int it = h * s.tiles + tile;
-      const int64_t n = parts_of(p, s.total), from = s.step + (int64_t)it * s.steps;
+      const int64_t n = s.parts, from = s.step + (int64_t)it * s.steps;
       const int w0 = part_of(from, n, s.total), w1 = part_of(from + s.steps - 1, n, s.total);
       *at = ((int64_t)s.tile + it + w0) * p.cols + (col - tile * p.cols);
       return w1 - w0 + 1;
@@ -1041,72 +1033,104 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const PagedArgs a,
   }
 }
 
-// One pass alone, and both passes of a call with groups in one launch: the
-// first workgroups walk the shared keys, the others the sequences' own, which
-// then fill the CUs as the first ones end.
+template <int COLS>
+__device__ __forceinline__ constexpr int step_keys() {
+  return COLS <= 32 ? kPagedStep : kPagedWideStep;
+}
+
+// The sequences' own keys alone.
 template <int D, bool BF, int COLS>
-__global__ __launch_bounds__(kThreads, COLS == 32 && D > 64 ? 1 : 2) void paged_kernel(const PagedArgs a,
-                                                                                      const PagedPass ps) {
+__global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a, const PagedPass ps) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];
   Seg* seg = reinterpret_cast<Seg*>(dyn);
+  const int total = schedule<COLS, step_keys<COLS>()>(a, ps, seg), parts = min(ps.grid, total);
+  if (ps.fused) clear_empty<D>(a, ps, seg);
+  else publish<COLS, step_keys<COLS>()>(a, ps, seg, total, parts, blockIdx.x, gridDim.x);
+  if ((int)blockIdx.x >= parts) return;
   if constexpr (COLS <= 32) {
     __shared__ FewShared<D> sh;
-    walk_few<D, BF, COLS>(a, ps, seg, sh, blockIdx.x);
+    walk_few<D, BF, COLS>(a, ps, seg, sh, total, parts, blockIdx.x);
   } else {
     __shared__ ManyShared<D> sh;
-    walk_many<D, BF, COLS>(a, ps, seg, sh, blockIdx.x);
+    walk_many<D, BF, COLS>(a, ps, seg, nullptr, sh, total, parts, blockIdx.x);
   }
 }
+
+// Shared and own keys of a call with groups in one launch: as many workgroups
+// as the chip holds at once, dealt to the two walks by the bytes that their
+// steps read (twice as many in a walk over few columns), so that they end
+// together.
 template <int D, bool BF, int OWN, int SHARED>
-__global__ __launch_bounds__(kThreads, OWN == 32 && D > 64 ? 1 : 2) void paged_both_kernel(const PagedArgs a,
-                                                                                          const PagedPass own,
-                                                                                          const PagedPass shared) {
+__global__ __launch_bounds__(kThreads, 2) void paged_both_kernel(const PagedArgs a, const PagedPass own,
+                                                                 const PagedPass shared) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];
-  Seg* seg = reinterpret_cast<Seg*>(dyn);
+  Seg* seg_o = reinterpret_cast<Seg*>(dyn);
+  Seg* seg_s = seg_o + own.n + 1;
   __shared__ union Both {
     __device__ Both() {}
     FewShared<D> few;
     ManyShared<D> many;
   } sh;
-  if ((int)blockIdx.x < shared.grid) walk_many<D, BF, SHARED>(a, shared, seg, sh.many, blockIdx.x);
-  else walk_few<D, BF, OWN>(a, own, seg, sh.few, blockIdx.x - shared.grid);
+  constexpr int KO = step_keys<OWN>(), KS = step_keys<SHARED>();
+  const int to = schedule<OWN, KO>(a, own, seg_o), ts = schedule<SHARED, KS>(a, shared, seg_s);
+  const int n = gridDim.x;
+  const double ws = (double)ts * KS, wo = (double)to * KO;
+  // multiples of eight, so that neighbouring parts stay on one XCD
+  int ns = ts == 0 ? 0 : to == 0 ? n : min(max((int)(n * ws / (ws + wo) + 4.0) / 8 * 8, 8), n - 8);
+  const int ps = min(ns, ts), po = min(n - ns, to);
+  publish<OWN, KO>(a, own, seg_o, to, po, blockIdx.x, n);
+  publish<SHARED, KS>(a, shared, seg_s, ts, ps, blockIdx.x, n);
+  const int b = blockIdx.x;
+  if (b < ns) {
+    if (b >= ps) return;
+    walk_many<D, BF, SHARED>(a, shared, seg_s, seg_o, sh.many, ts, ps, b);
+  } else {
+    if (b - ns >= po) return;
+    if constexpr (OWN <= 32) walk_few<D, BF, OWN>(a, own, seg_o, sh.few, to, po, b - ns);
+    else walk_many<D, BF, OWN>(a, own, seg_o, nullptr, sh.many, to, po, b - ns);
+  }
 }
 
 template <int D, bool BF>
-hipError_t run_pass(const PagedArgs& a, const PagedPass& p, hipStream_t s) {
+hipError_t run_own(const PagedArgs& a, const PagedPass& p, hipStream_t s) {
   const dim3 g(p.grid), b(kThreads);
   const size_t lds = (p.n + 1) * sizeof(Seg);
-  if (p.cols == 16) paged_kernel<D, BF, 16><<<g, b, lds, s>>>(a, p);
-  else if (p.cols == 32) paged_kernel<D, BF, 32><<<g, b, lds, s>>>(a, p);
-  else if (p.cols == 64) paged_kernel<D, BF, 64><<<g, b, lds, s>>>(a, p);
-  else paged_kernel<D, BF, 128><<<g, b, lds, s>>>(a, p);
+  if (p.cols == 16) {
+    paged_kernel<D, BF, 16><<<g, b, lds, s>>>(a, p);
+  } else if (p.cols == 32) {
+    if constexpr (D == 64) paged_kernel<D, BF, 32><<<g, b, lds, s>>>(a, p);
+  } else if (p.cols == 64) {
+    paged_kernel<D, BF, 64><<<g, b, lds, s>>>(a, p);
+  } else {
+    paged_kernel<D, BF, 128><<<g, b, lds, s>>>(a, p);
+  }
   return hipGetLastError();
 }
-template <int D, bool BF>
+template <int D, bool BF, int OWN>
 hipError_t run_both(const PagedArgs& a, const PagedPass& own, const PagedPass& sh, hipStream_t s) {
-  const dim3 g(sh.grid + own.grid), b(kThreads);
-  const size_t lds = ((own.n > sh.n ? own.n : sh.n) + 1) * sizeof(Seg);
-  if (own.cols == 16 && sh.cols == 64) paged_both_kernel<D, BF, 16, 64><<<g, b, lds, s>>>(a, own, sh);
-  else if (own.cols == 16) paged_both_kernel<D, BF, 16, 128><<<g, b, lds, s>>>(a, own, sh);
-  else if (sh.cols == 64) paged_both_kernel<D, BF, 32, 64><<<g, b, lds, s>>>(a, own, sh);
-  else paged_both_kernel<D, BF, 32, 128><<<g, b, lds, s>>>(a, own, sh);
+  const dim3 g(own.grid), b(kThreads);
+  const size_t lds = (own.n + sh.n + 2) * sizeof(Seg);
+  if (sh.cols == 64) paged_both_kernel<D, BF, OWN, 64><<<g, b, lds, s>>>(a, own, sh);
+  else paged_both_kernel<D, BF, OWN, 128><<<g, b, lds, s>>>(a, own, sh);
   return hipGetLastError();
 }
 
 template <int D, bool BF>
 hipError_t run_paged(const PagedArgs& a, const PagedPass& sh, const PagedPass& own, hipStream_t s) {
-  hipError_t e;
-  if (sh.n && own.cols <= 32) {
-    if ((e = run_both<D, BF>(a, own, sh, s)) != hipSuccess) return e;
-  } else {
-    if ((e = run_pass<D, BF>(a, own, s)) != hipSuccess || own.fused) return e;
-    if (sh.n && (e = run_pass<D, BF>(a, sh, s)) != hipSuccess) return e;
-  }
+  hipError_t e = sh.n == 0         ? run_own<D, BF>(a, own, s)
+                 : own.cols == 16  ? run_both<D, BF, 16>(a, own, sh, s)
+                 : own.cols == 32  ? run_both<D, BF, D == 64 ? 32 : 16>(a, own, sh, s)
+                 : own.cols == 64  ? run_both<D, BF, 64>(a, own, sh, s)
+                                   : run_both<D, BF, 128>(a, own, sh, s);
+  if (e != hipSuccess || own.fused) return e;
   const int64_t avg = (a.rows + (int64_t)a.n_seq - 1) / a.n_seq;
   const int heads = a.hkv * a.g;
   const uint32_t z = (uint32_t)(avg < 64 ? avg : 64);
-  // many parts a row: all the waves of a workgroup join them
-  if (sh.n && sh.grid / (2 * sh.tiles) >= 8)
+  // the parts that a row may have: all the waves of a workgroup join many
+  const int parts = own.grid / (sh.n && sh.tiles < own.tiles ? sh.tiles : own.tiles);
+  if (parts >= 128)
+    paged_join_kernel<D, BF, 16><<<dim3(a.n_seq, heads, z), dim3(1024), 0, s>>>(a, sh, own);
+  else if (parts >= 8)
     paged_join_kernel<D, BF, kWaves><<<dim3(a.n_seq, heads, z), dim3(kThreads), 0, s>>>(a, sh, own);
   else
     paged_join_kernel<D, BF, 1><<<dim3(a.n_seq, (heads + kWaves - 1) / kWaves, z), dim3(kThreads), 0, s>>>(a, sh, own);

@@ -301,3 +301,12 @@ def test_query_rows_that_do_not_ascend_stay_inside():
         _run(q, k, v, table, lens, bad, [], 0.1, out=out[:8])
         assert (out[8] == 7.0).all()
         assert torch.equal(_run(q, k, v, table, lens, [0, 2, 5, 8], [], 0.1), good)
+
+
+@pytest.mark.parametrize("lens,groups", [([70000], []), ([20000, 3], []), ([30010, 30001, 29990], [(0, 3, 29984)])])
+def test_long_walks_of_few_tiles(lens, groups):
+    """One key-value head and few sequences: every tile's walk is cut in
+    hundreds of parts, whose results all the waves of a workgroup join."""
+    k, v, table = _batch(lens, None, groups, 16, 1, 128, "f16", 25)
+    q = torch.randn((len(lens), 4, 128), device="cuda").half()
+    _check(q, k, v, table, lens, None, groups, 16, "f16")
