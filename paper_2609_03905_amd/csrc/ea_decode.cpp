@@ -263,19 +263,21 @@ struct PagedPlan {
 };
 
 // A pass over n segments of `cols` query columns in all, by the columns that a
-// segment has on the average: up to 32, the walk that loads keys into registers
-// (tiles of 32 columns at width 64; at 128 its registers would admit one
-// workgroup a CU, and two tiles of 16, the second fed by the L2, are faster);
-// beyond, and for shared keys, the walk through shared memory, on tiles of 64 or
-// 128 columns, a step on the narrower costing about 0.55 of one on the wider.
+// segment has on the average: up to 32, the walk that loads keys into registers,
+// on tiles of 16 or 32 columns (at 32 columns of width 128 its registers admit
+// one workgroup a CU: 16 sequences of 5 tokens over 2500 keys 45 us against 54 on
+// two tiles of 16, but beside a walk over shared keys, which needs two, 61
+// against 45); beyond, and for shared keys, the walk through shared memory, on
+// tiles of 64 or 128 columns, a step on the narrower costing about 0.55 of one on
+// the wider.
 void plan_pass(PagedPass* p, bool shared, int first, int n, int64_t cols, int64_t hkv, int64_t d) {
   p->shared = shared;
   p->first = first;
   p->n = n;
   const int64_t avg = n ? (cols + n - 1) / n : 0;
-  if (avg <= 32 && !shared) p->cols = avg > 16 && d == 64 ? 32 : 16;
+  if (avg <= 32 && !shared) p->cols = avg > 16 && (d == 64 || first == 0) ? 32 : 16;
   else p->cols = 0.55 * (double)((avg + 63) / 64) < (double)((avg + 127) / 128) ? 64 : 128;
-  p->grid = 512;  // two workgroups a CU
+  p->grid = p->cols == 32 && d == 128 ? 256 : 512;
   const int64_t tiles = (cols / p->cols + n) * hkv;
   p->tiles = (int32_t)(tiles < INT32_MAX ? tiles : INT32_MAX);
 }

@@ -1040,7 +1040,7 @@ __device__ __forceinline__ constexpr int step_keys() {
 
 // The sequences' own keys alone.
 template <int D, bool BF, int COLS>
-__global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a, const PagedPass ps) {
+__global__ __launch_bounds__(kThreads, COLS == 32 && D == 128 ? 1 : 2) void paged_kernel(const PagedArgs a, const PagedPass ps) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];
   Seg* seg = reinterpret_cast<Seg*>(dyn);
   const int total = schedule<COLS, step_keys<COLS>()>(a, ps, seg), parts = min(ps.grid, total);
@@ -1057,9 +1057,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(const PagedArgs a, c
 }
 
 // Shared and own keys of a call with groups in one launch: as many workgroups
-// as the chip holds at once, dealt to the two walks by the bytes that their
-// steps read (twice as many in a walk over few columns), so that they end
-// together.
+// as the chip holds at once, dealt to the two walks so that they end together.
 template <int D, bool BF, int OWN, int SHARED>
 __global__ __launch_bounds__(kThreads, 2) void paged_both_kernel(const PagedArgs a, const PagedPass own,
                                                                  const PagedPass shared) {
@@ -1074,9 +1072,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_both_kernel(const PagedArgs
   constexpr int KO = step_keys<OWN>(), KS = step_keys<SHARED>();
   const int to = schedule<OWN, KO>(a, own, seg_o), ts = schedule<SHARED, KS>(a, shared, seg_s);
   const int n = gridDim.x;
-  const double ws = (double)ts * KS, wo = (double)to * KO;
+  // by the bytes that the walks read (with the measured times of their steps and
+  // of beginning and ending a walk instead: 8K prefix 43 us against 40); in
   // multiples of eight, so that neighbouring parts stay on one XCD
-  int ns = ts == 0 ? 0 : to == 0 ? n : min(max((int)(n * ws / (ws + wo) + 4.0) / 8 * 8, 8), n - 8);
+  const double ws = (double)ts * KS, wo = (double)to * KO;
+  const int ns = ts == 0 ? 0 : to == 0 ? n : min(max((int)(n * ws / (ws + wo) + 4.0) / 8 * 8, 8), n - 8);
   const int ps = min(ns, ts), po = min(n - ns, to);
   publish<OWN, KO>(a, own, seg_o, to, po, blockIdx.x, n);
   publish<SHARED, KS>(a, shared, seg_s, ts, ps, blockIdx.x, n);
@@ -1098,7 +1098,7 @@ hipError_t run_own(const PagedArgs& a, const PagedPass& p, hipStream_t s) {
   if (p.cols == 16) {
     paged_kernel<D, BF, 16><<<g, b, lds, s>>>(a, p);
   } else if (p.cols == 32) {
-    if constexpr (D == 64) paged_kernel<D, BF, 32><<<g, b, lds, s>>>(a, p);
+    paged_kernel<D, BF, 32><<<g, b, lds, s>>>(a, p);
   } else if (p.cols == 64) {
     paged_kernel<D, BF, 64><<<g, b, lds, s>>>(a, p);
   } else {
