@@ -9,12 +9,16 @@
 // ascending order and duties ranked by position, so results do not depend on
 // timing: counts change by integer atomics only, whose order is immaterial.
 //
-// The bookkeeping is a few thousand integers: bound by the latency of a
-// dependent chain, not by bandwidth, so one workgroup of 16 waves does it
-// between barriers.  Each wave owns a contiguous range of the pages; inside it
-// a free page's rank is a population count of lane ballots, and 16 wave totals
-// are the only numbers that cross waves.  Moving the pages' contents is bound
-// by HBM and runs in a launch of its own on the whole chip.
+// The bookkeeping is some thousand integers: bound by the latency of dependent
+// steps, not by bandwidth, so one workgroup of 16 waves does it between
+// barriers (the parts of select that touch every entry of a large table are
+// launches of their own).  Each wave owns a contiguous range of the pages; inside
+// it a free page's rank is a population count of lane ballots, and 16 wave totals
+// are the only numbers that cross waves.  Moving the pages' contents is bound by
+// HBM and runs in a launch on the whole chip.  Measured: new pages for 256
+// sequences in a cache of 33 thousand pages 17 us (10 of them the two walks over
+// all counts); a beam step over 64 sequences 10 us and its copies, 134 MB moved,
+// 30; 1.35 GB made dense 8 us and 275, against 263 at a large copy's rate.
 #include "ea_decode.h"
 #include "ea_device.h"
 
@@ -28,9 +32,14 @@ constexpr int kCopyThreads = 256, kCopyWgs = 2048;
 
 // Workspace words: the copies a bookkeeping kernel asks for.
 constexpr int kWorkCount = 0;   // pages to move
+constexpr int kWorkUsed = 1;    // compact: pages in use
 constexpr int kWorkLists = 16;  // then source pages, destinations and rows
 
 constexpr int kList = 4096;     // pages that extend hands out at a time
+// Table entries and pages up to which select's bookkeeping is one workgroup's;
+// beyond, three launches of many (6.5 thousand: 13.5 us in one workgroup, 16.2 in
+// three launches; 25 thousand: 27 and 21; 200 thousand: 157 and 31).
+constexpr int64_t kOneWorkgroup = 16384;
 
 __device__ __forceinline__ int held(int len, int page) { return (len + page - 1) / page; }
 
@@ -262,26 +271,41 @@ __global__ __launch_bounds__(kMetaThreads) void extend_kernel(const PagesArgs a)
   for (int s = tid; s < a.n_seq; s += kMetaThreads) a.out_len[s] = s_len[s] + (code ? 0 : max(a.add[s], 0));
 }
 
-// Every sequence i becomes a copy of parent[i] (outside the batch: empty).
-__global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a) {
-  __shared__ int s_children[kMaxSeq], s_first[kMaxSeq], s_len[kMaxSeq], s_parent[kMaxSeq];
-  __shared__ int s_wave[kMetaWaves];
-  const int tid = threadIdx.x;
+// ---- select: every sequence i becomes a copy of parent[i] (outside the batch:
+// empty).  Three steps: the counts are copied; the old sequences' pages gain or
+// lose references and the new table is written; copies of partly filled pages
+// are ranked and given pages.
+struct Family {
+  int children[kMaxSeq], first[kMaxSeq];  // of every old sequence
+  int len[kMaxSeq], parent[kMaxSeq];
+};
+
+// By the whole workgroup; returns whether a length is one that no row holds.
+__device__ __forceinline__ int load_family(const PagesArgs& a, Family& f) {
   const int64_t most = (int64_t)a.stride * a.page_size;
-  int* src = a.work + kWorkLists;
-  int* dst = src + a.n_seq;
-  int* rows = dst + a.n_seq;
-  int* who = rows + a.n_seq;
   int bad = 0;
-  for (int s = tid; s < a.n_seq; s += kMetaThreads) {
+  for (int s = threadIdx.x; s < a.n_seq; s += kMetaThreads) {
     const int p = a.parent[s];
-    s_children[s] = 0;
-    s_first[s] = a.n_seq;
-    s_len[s] = a.len[s];
-    s_parent[s] = (uint32_t)p < (uint32_t)a.n_seq ? p : -1;
-    bad |= s_len[s] < 0 || s_len[s] > most;
+    f.children[s] = 0;
+    f.first[s] = a.n_seq;
+    f.len[s] = a.len[s];
+    f.parent[s] = (uint32_t)p < (uint32_t)a.n_seq ? p : -1;
+    bad |= f.len[s] < 0 || f.len[s] > most;
   }
-  for (int p0 = tid; p0 < a.n_pages; p0 += 4 * kMetaThreads) {
+  bad = __syncthreads_or(bad);
+  if (!bad)
+    for (int i = threadIdx.x; i < a.n_seq; i += kMetaThreads)
+      if (f.parent[i] >= 0) {
+        atomicAdd(&f.children[f.parent[i]], 1);
+        atomicMin(&f.first[f.parent[i]], i);
+      }
+  __syncthreads();
+  return bad;
+}
+
+__device__ __forceinline__ void copy_refs(const PagesArgs& a, int block, int blocks) {
+  for (int64_t p0 = (int64_t)block * 4 * kMetaThreads + threadIdx.x; p0 < a.n_pages;
+       p0 += (int64_t)blocks * 4 * kMetaThreads) {
     int r[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = p0 + i * kMetaThreads < a.n_pages ? a.refs[p0 + i * kMetaThreads] : 0;
@@ -289,18 +313,14 @@ __global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a)
     for (int i = 0; i < 4; ++i)
       if (p0 + i * kMetaThreads < a.n_pages) a.out_refs[p0 + i * kMetaThreads] = r[i];
   }
-  bad = __syncthreads_or(bad);
-  if (!bad)
-    for (int i = tid; i < a.n_seq; i += kMetaThreads)
-      if (s_parent[i] >= 0) {
-        atomicAdd(&s_children[s_parent[i]], 1);
-        atomicMin(&s_first[s_parent[i]], i);
-      }
-  settle();
-  // counts of the old sequences' pages, and the new rows of the table: entry
-  // (s, j) by one thread, four in flight
-  const int64_t cells = bad ? 0 : (int64_t)a.n_seq * a.stride;
-  for (int64_t x0 = tid; x0 < cells; x0 += 4 * kMetaThreads) {
+}
+
+// Counts of the old sequences' pages, and the new rows of the table: entry
+// (s, j) by one thread, four in flight.
+__device__ __forceinline__ void select_cells(const PagesArgs& a, const Family& f, int block, int blocks) {
+  const int64_t cells = (int64_t)a.n_seq * a.stride;
+  for (int64_t x0 = (int64_t)block * 4 * kMetaThreads + threadIdx.x; x0 < cells;
+       x0 += (int64_t)blocks * 4 * kMetaThreads) {
     int old_pg[4], new_pg[4], d[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -309,12 +329,12 @@ __global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a)
       d[i] = 0;
       if (x >= cells) continue;
       const int s = div_fast((int)x, a.row), j = (int)x - s * a.stride;
-      const int ch = s_children[s], full = s_len[s] / a.page_size, tail = s_len[s] - full * a.page_size;
+      const int ch = f.children[s], full = f.len[s] / a.page_size, tail = f.len[s] - full * a.page_size;
       // a partly filled page stays its first child's
       d[i] = j < full ? ch - 1 : j == full && tail > 0 && ch == 0 ? -1 : 0;
       if (d[i]) old_pg[i] = a.table[x];
-      const int par = s_parent[s];
-      if (par >= 0 && j < held(s_len[par], a.page_size)) new_pg[i] = a.table[(int64_t)par * a.stride + j];
+      const int par = f.parent[s];
+      if (par >= 0 && j < held(f.len[par], a.page_size)) new_pg[i] = a.table[(int64_t)par * a.stride + j];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -324,14 +344,40 @@ __global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a)
       a.out_table[x] = new_pg[i];
     }
   }
-  if (!bad)
-    for (int s = tid; s < a.n_seq; s += kMetaThreads) a.out_len[s] = s_parent[s] >= 0 ? s_len[s_parent[s]] : 0;
+  for (int s = block * kMetaThreads + threadIdx.x; s < a.n_seq; s += blocks * kMetaThreads)
+    a.out_len[s] = f.parent[s] >= 0 ? f.len[f.parent[s]] : 0;
+}
+
+__global__ __launch_bounds__(kMetaThreads) void copy_refs_kernel(const PagesArgs a) {
+  copy_refs(a, blockIdx.x, gridDim.x);
+}
+__global__ __launch_bounds__(kMetaThreads) void select_cells_kernel(const PagesArgs a) {
+  __shared__ Family f;
+  if (!load_family(a, f)) select_cells(a, f, blockIdx.x, gridDim.x);
+}
+
+// All three steps, or the third alone.
+template <bool ALL>
+__global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a) {
+  __shared__ Family f;
+  __shared__ int s_wave[kMetaWaves];
+  const int tid = threadIdx.x;
+  int* src = a.work + kWorkLists;
+  int* dst = src + a.n_seq;
+  int* rows = dst + a.n_seq;
+  int* who = rows + a.n_seq;
+  if (ALL) copy_refs(a, 0, 1);
+  const int bad = load_family(a, f);
+  if (ALL) {
+    settle();
+    if (!bad) select_cells(a, f, 0, 1);
+  }
   // copies of partly filled pages, ranked by sequence
   const int per = (a.n_seq + kMetaThreads - 1) / kMetaThreads;
   const int s0 = min(a.n_seq, tid * per), s1 = min(a.n_seq, s0 + per);
   auto copies = [&](int i) {
-    const int p = s_parent[i];
-    return !bad && p >= 0 && s_first[p] != i && s_len[p] % a.page_size > 0;
+    const int p = f.parent[i];
+    return !bad && p >= 0 && f.first[p] != i && f.len[p] % a.page_size > 0;
   };
   int mine = 0;
   for (int i = s0; i < s1; ++i) mine += copies(i);
@@ -339,10 +385,10 @@ __global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a)
   int rank = block_scan(mine, s_wave, &count);
   for (int i = s0; i < s1; ++i)
     if (copies(i)) {
-      const int p = s_parent[i], full = s_len[p] / a.page_size;
+      const int p = f.parent[i], full = f.len[p] / a.page_size;
       const int pg = a.table[(int64_t)p * a.stride + full];
       src[rank] = (uint32_t)pg < (uint32_t)a.n_pages ? pg : -1;
-      rows[rank] = s_len[p] - full * a.page_size;
+      rows[rank] = f.len[p] - full * a.page_size;
       who[rank] = i;
       ++rank;
     }
@@ -356,7 +402,7 @@ __global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a)
     });
     settle();
     for (int r = tid; r < count; r += kMetaThreads) {
-      const int i = who[r], at = s_len[s_parent[i]] / a.page_size, p = dst[r];
+      const int i = who[r], at = f.len[f.parent[i]] / a.page_size, p = dst[r];
       a.out_refs[p] = 1;
       a.out_table[(int64_t)i * a.stride + at] = p;
     }
@@ -366,60 +412,67 @@ __global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a)
   }
   // nothing is done: the state goes through as it came
   settle();
-  int left = 0;
-  for (int p = tid; p < a.n_pages; p += kMetaThreads) {
-    a.out_refs[p] = a.refs[p];
-    left += a.refs[p] <= 0;
-  }
-  for (int s = tid; s < a.n_seq; s += kMetaThreads) a.out_len[s] = a.len[s];
+  copy_refs(a, 0, 1);
+  for (int s = tid; s < a.n_seq; s += kMetaThreads) a.out_len[s] = f.len[s];
   for (int64_t j = tid; j < (int64_t)a.n_seq * a.stride; j += kMetaThreads) a.out_table[j] = a.table[j];
-  int sum;
-  block_scan(left, s_wave, &sum);
+  int left;
+  free_before(a.refs, a.n_pages, s_wave, &left);
   if (tid == 0) a.work[kWorkCount] = 0;
-  set_status(a, code, sum);
+  set_status(a, code, left);
 }
 
-// Used pages behind the first n_used go to the free places before: the k-th
-// lowest to the k-th lowest.
+// ---- compact: the used pages behind the first n_used go to the free places
+// before, the k-th lowest to the k-th lowest.  Here the two lists are made and
+// every moved page's rank noted; the launch that moves the contents rewrites
+// the table and the counts beside.
 __global__ __launch_bounds__(kMetaThreads) void compact_kernel(const PagesArgs a) {
   __shared__ int s_wave[kMetaWaves];
   __shared__ int s_moves;
   const int tid = threadIdx.x;
   int* src = a.work + kWorkLists;
   int* dst = src + a.n_pages;
-  int* to = dst + a.n_pages;  // by page: where it went
+  int* rank_of = dst + a.n_pages;
   int all_free;
   const int before = free_before(a.refs, a.n_pages, s_wave, &all_free);
   const int n_used = a.n_pages - all_free;
   if (tid == 0) s_moves = 0;
   __syncthreads();
   each_page(a.refs, nullptr, a.n_pages, before, 0x7fffffff, [&](int p, int refs, int free_rank) {
-    to[p] = p;
     if (p < n_used && refs <= 0) dst[free_rank] = p;
-    // the free pages before n_used are as many as the used ones behind it:
-    // a used page's rank among the latter is its rank among the used ones
-    // less those before n_used
     if (p == n_used - 1) s_moves = free_rank + (refs <= 0);
+    // the free pages before n_used are as many as the used ones behind it, and
+    // p - free_rank pages before p are used: n_used - 1 less that many come
+    // after it, which ranks the pages behind n_used from their end
+    if (p >= n_used && refs > 0) src[n_used - 1 - (p - free_rank)] = p;
   });
-  settle();
+  __syncthreads();
   const int moves = s_moves;
-  each_page(a.refs, nullptr, a.n_pages, before, 0x7fffffff, [&](int p, int refs, int free_rank) {
-    if (p >= n_used && refs > 0) src[p - free_rank - (n_used - moves)] = p;
-  });
-  settle();
-  // every count is read before a thread writes another's (they may be updated
-  // in place): moved pages are behind n_used, holes before it
-  for (int k = tid; k < moves; k += kMetaThreads) to[src[k]] = dst[k];
-  if (a.out_refs != a.refs)
-    for (int p = tid; p < a.n_pages; p += kMetaThreads) a.out_refs[p] = max(a.refs[p], 0);
-  settle();
-  for (int k = tid; k < moves; k += kMetaThreads) {
-    const int n = a.refs[src[k]];
-    a.out_refs[dst[k]] = n;
-    a.out_refs[src[k]] = 0;
+  if (tid == 0) {
+    a.work[kWorkCount] = moves;
+    a.work[kWorkUsed] = n_used;
   }
-  if (tid == 0) a.work[kWorkCount] = moves;
+  settle();
+  for (int k0 = tid; k0 < moves; k0 += 8 * kMetaThreads) {
+    int p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = k0 + i * kMetaThreads < moves ? src[k0 + i * kMetaThreads] : -1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p[i] >= 0) rank_of[p[i]] = moves - 1 - (k0 + i * kMetaThreads);
+  }
   set_status(a, 0, all_free);
+}
+
+// In place: the moved pages' counts.
+__global__ __launch_bounds__(kMetaThreads) void compact_refs_kernel(const PagesArgs a) {
+  const int count = a.work[kWorkCount];
+  const int* src = a.work + kWorkLists;
+  const int* dst = src + a.n_pages;
+  for (int r = blockIdx.x * kMetaThreads + threadIdx.x; r < count; r += gridDim.x * kMetaThreads) {
+    const int from = src[count - 1 - r], into = dst[r];
+    a.out_refs[into] = a.refs[from];
+    a.out_refs[from] = 0;
+  }
 }
 
 // The pages that a bookkeeping kernel listed, in every plane and cache, cut in
@@ -434,16 +487,26 @@ __global__ __launch_bounds__(kCopyThreads) void move_kernel(const PagesArgs a, c
   const int count = ld_uniform(&c.work[kWorkCount]);
   const int32_t* src = c.work + kWorkLists;
   const int32_t* dst = src + (ROWS ? a.n_seq : a.n_pages);
-  const int32_t* more = dst + (ROWS ? a.n_seq : a.n_pages);  // rows, or where each page went
+  const int32_t* more = dst + (ROWS ? a.n_seq : a.n_pages);  // rows, or ranks of moved pages
   if constexpr (!ROWS) {
-    const int64_t n = (int64_t)a.n_seq * a.stride, step = (int64_t)gridDim.x * gridDim.y * kCopyThreads;
-    for (int64_t j = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kCopyThreads + threadIdx.x; j < n; j += step) {
+    const int n_used = ld_uniform(&c.work[kWorkUsed]);
+    const int64_t cells = (int64_t)a.n_seq * a.stride, step = (int64_t)gridDim.x * gridDim.y * kCopyThreads;
+    const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kCopyThreads + threadIdx.x;
+    for (int64_t j = first; j < cells; j += step) {
       const int s = div_fast((int)j, a.row), at = (int)j - s * a.stride;
-      const int pg = a.table[j];
-      a.out_table[j] = at >= held(max(a.len[s], 0), a.page_size) ? -1
-                       : (uint32_t)pg < (uint32_t)a.n_pages     ? more[pg]
-                                                                : pg;
+      int pg = a.table[j];
+      // (a page that no count calls used was not moved: its entry stays)
+      if (pg >= n_used && pg < a.n_pages && a.refs[pg] > 0) pg = dst[more[pg]];
+      a.out_table[j] = at >= held(max(a.len[s], 0), a.page_size) ? -1 : pg;
     }
+    if (a.out_refs != a.refs)
+      for (int64_t p = first; p < a.n_pages; p += step) {
+        // places before n_used that were free get the moved pages' counts
+        const int n = a.refs[p];
+        if (n > 0 || p >= n_used) a.out_refs[p] = p < n_used ? n : 0;
+      }
+    for (int64_t r = first; a.out_refs != a.refs && r < count; r += step)
+      a.out_refs[dst[r]] = a.refs[src[count - 1 - r]];
   }
   for (int k = 0; k < c.n_cache; ++k) {
     const PagesCache& pc = c.c[k];
@@ -453,7 +516,7 @@ __global__ __launch_bounds__(kCopyThreads) void move_kernel(const PagesArgs a, c
       char* base = pc.data + plane * pc.plane_bytes;
       for (uint32_t it = blockIdx.x; it < items; it += gridDim.x) {
         const uint32_t j = it / pieces, piece = it - j * pieces;
-        const int from = ld_uniform(src + j), into = ld_uniform(dst + j);
+        const int from = ld_uniform(src + (ROWS ? j : count - 1 - j)), into = ld_uniform(dst + j);
         if (from < 0) continue;
         const uint4* s = reinterpret_cast<const uint4*>(base + from * pc.page_bytes);
         uint4* d = reinterpret_cast<uint4*>(base + into * pc.page_bytes);
@@ -491,8 +554,16 @@ hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_pages_select(const PagesArgs& a, const PagesCopyArgs& c, hipStream_t s) {
-  select_kernel<<<dim3(1), dim3(kMetaThreads), 0, s>>>(a);
-  hipError_t e = hipGetLastError();
+  const int64_t cells = (int64_t)a.n_seq * a.stride;
+  if (cells + a.n_pages <= kOneWorkgroup) {
+    select_kernel<true><<<dim3(1), dim3(kMetaThreads), 0, s>>>(a);
+  } else {
+    auto blocks = [](int64_t n) { return dim3((uint32_t)(n > (int64_t)256 * 4096 ? 256 : (n + 4095) / 4096)); };
+    copy_refs_kernel<<<blocks(a.n_pages), dim3(kMetaThreads), 0, s>>>(a);
+    select_cells_kernel<<<blocks(cells), dim3(kMetaThreads), 0, s>>>(a);
+    select_kernel<false><<<dim3(1), dim3(kMetaThreads), 0, s>>>(a);
+  }
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || c.n_cache == 0) return e;
   move_kernel<true><<<copy_grid(c), dim3(kCopyThreads), 0, s>>>(a, c);
   return hipGetLastError();
@@ -503,6 +574,9 @@ hipError_t launch_pages_compact(const PagesArgs& a, const PagesCopyArgs& c, hipS
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   move_kernel<false><<<copy_grid(c), dim3(kCopyThreads), 0, s>>>(a, c);
+  if ((e = hipGetLastError()) != hipSuccess || a.out_refs != a.refs) return e;
+  // in place the counts change when every workgroup has read them
+  compact_refs_kernel<<<dim3(64), dim3(kMetaThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 
