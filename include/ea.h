@@ -461,7 +461,7 @@ typedef struct ea_heads_params {
                                pages of a cache, and a row's keys and values go
                                to page slot / page_size, row slot % page_size; a
                                slot outside the cache (-1: padding) stores none.
-                               A slot given twice holds either row.            */
+                               Rows given one slot leave it undefined.         */
 } ea_heads_params;
 /* qkv: [T, (Hq + 2 Hkv) d], columns [Q heads | K heads | V heads].  q: rank 2
    [T, Hq d], or rank 3 or 4 [.., Hq, T, d] (leading extent 1): token-major or
@@ -518,7 +518,7 @@ typedef struct ea_paged {
 } ea_paged;
 /* q, out: [rows, Hq d] or [.., Hq, rows, d] (forms as ea_heads' q).  bf16 or
    f16, d 64 or 128; scores and sums in f32, weights rounded to the dtype for
-   the product with V.  n_seq + n_group <= EA_PAGED_MAX_SEQ, rows * Hq < 2^31.
+   the product with V; a table row holds less than 2^31 - 1024 keys.  n_seq + n_group <= EA_PAGED_MAX_SEQ, rows * Hq < 2^31.
    workspace: as ea_joinagg's (a zeroed counter area, left zero; the rest needs
    no initial value), of at least ea_attention_paged_workspace's bytes for these
    operands; asynchronous, never allocates, deterministic.  Errors: EA_ERR_ARG, EA_ERR_DTYPE,
@@ -537,7 +537,7 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
    afterwards.  Entries behind a sequence's pages are not read, and are -1 in
    rewritten tables; an entry outside the cache counts no page.  n_seq <=
    EA_PAGED_MAX_SEQ; n_seq * stride, n_pages * page_size and (stride + 1) *
-   page_size < 2^31.  Asynchronous, no allocation, no plan. */
+   page_size < 2^31 (EA_ERR_UNSUPPORTED beyond).  Asynchronous, no allocation, no plan. */
 #define EA_PAGES_OK 0
 #define EA_PAGES_NONE_FREE 1 /* fewer free pages than the call needs            */
 #define EA_PAGES_TOO_LONG 2  /* a length below 0 or above a table row's keys    */
@@ -555,7 +555,7 @@ typedef struct ea_pages {
    itself, which gets the new pages; out_lengths and out_refs may be lengths
    and refs.  slots, positions (NULL: not wanted): for the new tokens, sequence
    by sequence, their slot (page * page_size + row) and position; entries
-   behind them, up to n_tokens, get -1 and 0. */
+   behind them, up to n_tokens, get -1 and 0.  No array may overlap an output. */
 int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, int32_t* positions, int32_t n_tokens,
                     void* stream);
 /* Sequence i becomes a copy of sequence parent[i] (outside [0, n_seq): empty),

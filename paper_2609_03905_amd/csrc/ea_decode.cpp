@@ -432,6 +432,14 @@ int check_pages(const ea_pages* p, PagesArgs* a) {
   return EA_OK;
 }
 
+// Whether [p, p + bytes) meets any array of the state.
+bool meets_state(const ea_pages* s, const void* p, int64_t bytes) {
+  const int64_t nt = (int64_t)s->n_seq * s->stride * 4, nl = s->n_seq * (int64_t)4, nr = s->n_pages * (int64_t)4;
+  return overlap(p, bytes, s->table, nt) || overlap(p, bytes, s->lengths, nl) || overlap(p, bytes, s->refs, nr) ||
+         overlap(p, bytes, s->out_table, nt) || overlap(p, bytes, s->out_lengths, nl) ||
+         overlap(p, bytes, s->out_refs, nr) || overlap(p, bytes, s->status, 8);
+}
+
 int check_caches(int32_t n, ea_relation* const* caches, const ea_pages* p, PagesCopyArgs* c) {
   if (n < 0 || n > kPagesMaxCaches || (n && !caches))
     return fail(EA_ERR_ARG, "n_cache %d outside [0, %d] or NULL caches", n, kPagesMaxCaches);
@@ -491,6 +499,14 @@ int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, i
   if (!add || !state->out_lengths) return fail(EA_ERR_ARG, "NULL add or out_lengths");
   if (a.out_table != a.table) return fail(EA_ERR_ARG, "extend works in its table: out_table must be table");
   if (n_tokens < 0) return fail(EA_ERR_ARG, "n_tokens %d", n_tokens);
+  const int64_t nt = n_tokens * (int64_t)4;
+  if (meets_state(state, slots, nt) || meets_state(state, positions, nt) || overlap(slots, nt, positions, nt) ||
+      overlap(slots, nt, add, a.n_seq * (int64_t)4) || overlap(positions, nt, add, a.n_seq * (int64_t)4))
+    return fail(EA_ERR_ARG, "slots or positions overlap another array");
+  if (overlap(add, a.n_seq * (int64_t)4, a.out_refs, a.n_pages * (int64_t)4) ||
+      overlap(add, a.n_seq * (int64_t)4, a.out_table, (int64_t)a.n_seq * a.stride * 4) ||
+      overlap(add, a.n_seq * (int64_t)4, a.out_len, a.n_seq * (int64_t)4))
+    return fail(EA_ERR_ARG, "add overlaps an output");
   a.add = add;
   a.slots = slots;
   a.pos = positions;
@@ -509,6 +525,10 @@ int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages*
   if (!parent || !state->out_lengths) return fail(EA_ERR_ARG, "NULL parent or out_lengths");
   if (a.out_table == a.table || a.out_len == a.len || a.out_refs == a.refs)
     return fail(EA_ERR_ARG, "select needs output arrays of their own");
+  const int64_t np = a.n_seq * (int64_t)4;
+  if (overlap(parent, np, a.out_table, np * a.stride) || overlap(parent, np, a.out_len, np) ||
+      overlap(parent, np, a.out_refs, a.n_pages * (int64_t)4) || overlap(parent, np, a.status, 8))
+    return fail(EA_ERR_ARG, "parent overlaps an output");
   if ((e = check_pages_ws(state, workspace, ws_bytes, &a, &c))) return e;
   a.parent = parent;
   EA_HIP_TRY(launch_pages_select(a, c, (hipStream_t)stream));

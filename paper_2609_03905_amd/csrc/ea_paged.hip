@@ -10,21 +10,22 @@
 //
 // A call is a set of segments: a group's shared keys under all of its rows,
 // and each sequence's own keys under its rows.  A segment's query columns
-// (rows x query heads of one key-value head) are cut in tiles of 16 NC; the
-// keys of each (segment, head, tile) are walked in steps of 128.  All steps of
-// a launch lie end to end, and workgroup w of n takes the w-th n-th part of
-// them, so that the work is even whatever the lengths are: a workgroup's part
-// may end one tile's walk and begin the next one's, and a tile's walk has as
-// many partial results as parts touch it.  The i-th tile's result from part w
-// is slot i + w (one of the two grows from piece to piece).  The lengths are
-// read on the device, by every workgroup for itself (a scan over the
-// segments), so a captured launch serves batches that grow.  Parts that run on
-// one XCD are neighbours: tiles over the same keys then share its L2.
+// (rows x query heads of one key-value head) are cut in tiles; the keys of each
+// (segment, head, tile) are walked in steps.  All steps of a pass lie end to
+// end, and workgroup w of n takes the w-th n-th part of them, so that the work
+// is even whatever the lengths are: a workgroup's part may end one tile's walk
+// and begin the next one's, and a tile's walk has as many partial results as
+// parts touch it.  The i-th tile's result from part w is slot i + w (one of the
+// two grows from piece to piece).  The lengths are read on the device, by every
+// workgroup for itself (a scan over the segments, 2.5 us), so a captured launch
+// serves batches that grow.  Parts that run on one XCD are neighbours: tiles
+// over the same keys then share its L2.
 //
-// Bound by HBM: 16 columns of D = 128 need 4 * 128 * 16 operations on a key's
-// 512 bytes, a tenth of what the matrix cores do while the bytes arrive.  So
-// nothing is staged in shared memory: each wave walks its own 32 keys of a
-// step and loads K and V from the pages straight into the registers of
+// Few columns (up to 32 a tile) are bound by HBM: 16 of D = 128 need
+// 4 * 128 * 16 operations on a key's 512 bytes, a tenth of what the matrix cores
+// do while the bytes arrive.  So nothing is staged in shared memory: each wave
+// walks its own 32 keys of a step of 128 and loads K and V from the pages
+// straight into the registers of
 //   S^T = K Q^T     (16x16x32: A = 16 keys x 32 d, B = 32 d x 16 columns)
 //   O^T += V^T P^T  (A = 16 d x 32 keys, B = 32 keys x 16 columns)
 // The B operand of the second product holds eight keys a lane, and the
@@ -33,7 +34,14 @@
 // in any order, so V is loaded for those eight keys, 8 (or 4) neighbouring d a
 // lane, and turned in registers: d index 16 m + j' becomes row m of tile j'.
 // The addresses of a wave's 32 key rows come from the page table, one lane a
-// key, through shared memory; a step's table entries are read a step ahead.
+// key, through shared memory, so that pages may be of any size; a step's table
+// entries are read a step ahead.
+//
+// Measured (bf16 or fp16, 32 query heads over 8, D = 128): 48 sequences of up to
+// 8K keys 148 us, 5.4 TB/s (5.1 is a large copy's rate); 64 sequences that share
+// 8K keys 40 + 8 us (walk, join), 32 that share 64K 82 + 8 us, where the bytes
+// take 20 and 66; one sequence of 1000 keys 9.7 us.  With every column tile
+// reading the shared keys for itself the last two took 92 and 213 us.
 #include "ea_decode.h"
 #include "ea_device.h"
 
@@ -139,6 +147,12 @@ __device__ __forceinline__ Segment segment(const PagedArgs& a, int i) {
   return s;
 }
 
+// Keys of a step of a walk over tiles of COLS columns.
+template <int COLS>
+__device__ __forceinline__ constexpr int step_keys() {
+  return COLS <= 32 ? kPagedStep : kPagedWideStep;
+}
+
 // A segment as the walk needs it, kept in shared memory (one more at the end
 // holds the totals).
 struct Seg {
@@ -168,47 +182,68 @@ __device__ __forceinline__ int tiles_of(int rows, int g, int cols) {
   return (int)(((int64_t)rows * g + cols - 1) / cols);
 }
 
-// Every segment's first step and tile, by the whole workgroup.  Returns the
-// steps of all; none where there are more tiles than the rows can have, that
-// is, where the sequences' rows overlap.
-template <int COLS, int KEYS>
-__device__ __forceinline__ int schedule(const PagedArgs& a, const PagedPass& ps, Seg* seg) {
-  __shared__ int s_wave[kWaves][2];
+// Every segment's first step and tile, by the whole workgroup: the groups' (none
+// where SHARED is 0) and the sequences', whose loads are one round trip.  *to and
+// *ts: the steps of all; none where there are more tiles than the rows can have,
+// that is, where the sequences' rows overlap.
+template <int OWN, int SHARED>
+__device__ __forceinline__ void schedule(const PagedArgs& a, const PagedPass& own, const PagedPass& shared, Seg* seg_o,
+                                         Seg* seg_s, int* to, int* ts) {
+  constexpr int N = SHARED ? 4 : 2;  // steps and tiles of the sequences, and of the groups
+  __shared__ int s_wave[kWaves][N];
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-  const int per = (ps.n + kThreads - 1) / kThreads;
-  const int i0 = min(ps.n, tid * per), i1 = min(ps.n, i0 + per);
-  int steps = 0, ntile = 0;
+  const int ng = SHARED ? shared.n : 0, n = ng + own.n;
+  const int per = (n + kThreads - 1) / kThreads;
+  const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  int mine[N] = {};
   for (int i = i0; i < i1; ++i) {
-    const Segment s = segment(a, ps.first + i);
-    const int n = steps_of(s.k0, s.k1, KEYS);
-    const int64_t t = n ? (int64_t)tiles_of(s.r1 - s.r0, a.g, COLS) * a.hkv : 0;
+    const bool g = SHARED && i < ng;
+    const Segment s = segment(a, i);
+    const int keys = g ? step_keys<SHARED>() : step_keys<OWN>(), cols = g ? SHARED : OWN;
+    const int steps = steps_of(s.k0, s.k1, keys);
+    const int64_t tiles = steps ? (((int64_t)(s.r1 - s.r0) * a.g + cols - 1) / cols) * a.hkv : 0;
     Seg x;
-    x.r0 = s.r0, x.rows = s.r1 - s.r0, x.k0 = s.k0, x.k1 = s.k1, x.step = steps, x.tile = ntile, x.seq = s.seq;
-    seg[i] = x;
-    steps = (int)min((int64_t)steps + n * t, (int64_t)0x7fffffff);
-    ntile = (int)min((int64_t)ntile + t, (int64_t)0x7fffffff);
+    x.r0 = s.r0, x.rows = s.r1 - s.r0, x.k0 = s.k0, x.k1 = s.k1, x.seq = s.seq;
+    x.step = g ? mine[N - 2] : mine[0];
+    x.tile = g ? mine[N - 1] : mine[1];
+    Seg* to_seg = g ? seg_s + i : seg_o + (i - ng);
+    *to_seg = x;
+    const int more_steps = (int)min(steps * tiles, (int64_t)0x7fffffff), more_tiles = (int)min(tiles, (int64_t)0x7fffffff);
+    if (g) {
+      mine[N - 2] = add_most(mine[N - 2], more_steps);
+      mine[N - 1] = add_most(mine[N - 1], more_tiles);
+    } else {
+      mine[0] = add_most(mine[0], more_steps);
+      mine[1] = add_most(mine[1], more_tiles);
+    }
   }
-  int st = wave_scan(steps), ti = wave_scan(ntile);
+  int sum[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    sum[k] = wave_scan(mine[k]);
+    if (lane == 63) s_wave[wid][k] = sum[k];
+  }
   __syncthreads();
-  if (lane == 63) {
-    s_wave[wid][0] = st;
-    s_wave[wid][1] = ti;
-  }
-  __syncthreads();
-  for (int w = 0; w < wid; ++w) {
-    st = add_most(st, s_wave[w][0]);
-    ti = add_most(ti, s_wave[w][1]);
-  }
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    for (int w = 0; w < wid; ++w) sum[k] = add_most(sum[k], s_wave[w][k]);
   if (tid == kThreads - 1) {
-    seg[ps.n].step = st;
-    seg[ps.n].tile = ti;
+    seg_o[own.n].step = sum[0];
+    seg_o[own.n].tile = sum[1];
+    if (SHARED) {
+      seg_s[ng].step = sum[N - 2];
+      seg_s[ng].tile = sum[N - 1];
+    }
   }
   for (int i = i0; i < i1; ++i) {
-    seg[i].step = add_most(seg[i].step, st - steps);
-    seg[i].tile = add_most(seg[i].tile, ti - ntile);
+    const bool g = SHARED && i < ng;
+    Seg* s = g ? seg_s + i : seg_o + (i - ng);
+    s->step = add_most(s->step, g ? sum[N - 2] - mine[N - 2] : sum[0] - mine[0]);
+    s->tile = add_most(s->tile, g ? sum[N - 1] - mine[N - 1] : sum[1] - mine[1]);
   }
   __syncthreads();
-  return seg[ps.n].tile > ps.tiles ? 0 : seg[ps.n].step;
+  *to = seg_o[own.n].tile > own.tiles ? 0 : seg_o[own.n].step;
+  if (SHARED) *ts = seg_s[ng].tile > shared.tiles ? 0 : seg_s[ng].step;
 }
 
 // What the join needs of a pass's segments (by workgroup `block` of n).
@@ -232,8 +267,8 @@ __device__ __forceinline__ void clear_empty(const PagedArgs& a, const PagedPass&
   for (int i = blockIdx.x; i < ps.n; i += gridDim.x) {
     const Seg s = seg[i];
     if (s.k1 > 0) continue;
-    for (int j = threadIdx.x; j < s.rows * n; j += kThreads) {
-      const int r = j / n, x = j - r * n;
+    for (int64_t j = threadIdx.x; j < (int64_t)s.rows * n; j += kThreads) {
+      const int r = (int)(j / n), x = (int)(j - (int64_t)r * n);
       *reinterpret_cast<uint4*>(a.po + row_offset(a.o, s.r0 + r, x / (D / 8)) + x % (D / 8) * 16) =
           make_uint4(0, 0, 0, 0);
     }
@@ -1033,17 +1068,14 @@ __global__ __launch_bounds__(W > kWaves ? W * 64 : kThreads) void paged_join_ker
   }
 }
 
-template <int COLS>
-__device__ __forceinline__ constexpr int step_keys() {
-  return COLS <= 32 ? kPagedStep : kPagedWideStep;
-}
-
 // The sequences' own keys alone.
 template <int D, bool BF, int COLS>
 __global__ __launch_bounds__(kThreads, COLS == 32 && D == 128 ? 1 : 2) void paged_kernel(const PagedArgs a, const PagedPass ps) {
   extern __shared__ __attribute__((aligned(16))) char dyn[];
   Seg* seg = reinterpret_cast<Seg*>(dyn);
-  const int total = schedule<COLS, step_keys<COLS>()>(a, ps, seg), parts = min(ps.grid, total);
+  int total;
+  schedule<COLS, 0>(a, ps, ps, seg, nullptr, &total, nullptr);
+  const int parts = min(ps.grid, total);
   if (ps.fused) clear_empty<D>(a, ps, seg);
   else publish<COLS, step_keys<COLS>()>(a, ps, seg, total, parts, blockIdx.x, gridDim.x);
   if ((int)blockIdx.x >= parts) return;
@@ -1070,7 +1102,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_both_kernel(const PagedArgs
     ManyShared<D> many;
   } sh;
   constexpr int KO = step_keys<OWN>(), KS = step_keys<SHARED>();
-  const int to = schedule<OWN, KO>(a, own, seg_o), ts = schedule<SHARED, KS>(a, shared, seg_s);
+  int to, ts;
+  schedule<OWN, SHARED>(a, own, shared, seg_o, seg_s, &to, &ts);
   const int n = gridDim.x;
   // by the bytes that the walks read (with the measured times of their steps and
   // of beginning and ending a walk instead: 8K prefix 43 us against 40); in

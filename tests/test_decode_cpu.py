@@ -223,6 +223,13 @@ def test_pages_refusals(call, code, change):
 def test_pages_refusals_of_one_call():
     assert extend(add=None) == ARG and extend(n_tokens=-1) == ARG and extend(out_lengths=None) == ARG
     assert extend(out_table=A + (3 << 20)) == ARG  # it works in its table
+    for bad in (A, A + (1 << 20), A + (2 << 20), A + (6 << 20), A + (7 << 20)):  # slots over another array
+        s = state(out_table=A)
+        assert ea.lib().ea_pages_extend(ctypes.byref(s), A + (7 << 20), bad, None, 3, None) == ARG
+        assert ea.lib().ea_pages_extend(ctypes.byref(s), A + (7 << 20), None, bad, 3, None) == ARG
+    assert extend(add=A + (4 << 20)) == ARG and extend(add=A + (5 << 20)) == ARG and extend(add=A) == ARG
+    for bad in (3, 4, 5, 6):
+        assert select(parent=A + (bad << 20)) == ARG
     assert select(parent=None) == ARG and select(out_lengths=None) == ARG
     for same in (dict(out_table=A), dict(out_lengths=A + (1 << 20)), dict(out_refs=A + (2 << 20))):
         assert select(**same) == ARG
