@@ -49,6 +49,9 @@ CASES = [
     (11, 2, 1, 512, 512, False, True, "bf16", 100),
     (11, 2, 1, 264, 0, False, True, "f16", 0),      # no rotation
     (300, 12, 12, 72, 72, False, True, "bf16", 0),  # the row's index
+    (23, 3, 2, 72, 16, False, True, "f32", 300),    # an odd number of eights stays unrotated
+    (23, 9, 3, 88, 64, False, False, "f16", 300),
+    (2000, 6, 1, 64, 64, True, True, "bf16", 300),
 ]
 
 
@@ -154,6 +157,8 @@ GRAD = [
     (70, 5, 1, 64, 10, True, True, "f32", 100),
     (9, 2, 2, 256, 256, True, False, "f32", 100),
     (9, 2, 1, 512, 0, False, True, "bf16", 0),
+    (23, 3, 2, 72, 16, False, True, "f32", 300),
+    (300, 7, 3, 40, 40, True, True, "f16", 300),
 ]
 
 
@@ -220,3 +225,58 @@ def test_heads_backward_repeats_to_the_bit():
         out.append((dx.clone(), dwq.clone(), dwk.clone()))
     for o in out[1:]:
         assert all(torch.equal(a, b) for a, b in zip(o, out[0]))
+
+
+def test_heads_into_padded_pages_on_another_stream():
+    """Pages of 240 bytes at 256-byte multiples, the call on a stream of its own."""
+    t, hq, hkv, d, page, n_pages = 10, 2, 1, 40, 3, 5
+    x, wq, wk, freq, pos = _inputs(t, hq, hkv, d, d, "f16", True, 90, 13)
+    slots = torch.tensor([14, 0, 3, 7, -1, 8, 2, 13, 5, 10], dtype=torch.int32, device="cuda")
+    kc, vc = (R.pages_rel(torch.zeros((n_pages, hkv, page, d), device="cuda", dtype=torch.float16)) for _ in range(2))
+    q = torch.empty((t, hq * d), device="cuda", dtype=torch.float16)
+    args = (R.rel(x), R.rel(q), kc, vc)
+    kw = dict(d_head=d, wq=R.rel(wq), wk=R.rel(wk), eps=EPS, inv_freq=freq, positions=pos, slots=slots)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    ea.heads(*args, stream=s, **kw)
+    s.synchronize()
+    ref, err = R.heads(R.f64(x), hq, hkv, d, _np(wq), _np(wk), EPS, R.f64(freq), False, pos.cpu().numpy())
+    R.check(R.f64(q).reshape(t, hq, d), ref[0], R.heads_tol(ref[0], err[0], "f16"))
+    k, v = R.f64(R.unblocked(kc)), R.f64(R.unblocked(vc))
+    for i, s in enumerate(slots.tolist()):
+        if s >= 0:
+            R.check(k[s // page, :, s % page], ref[1][i], R.heads_tol(ref[1][i], err[1][i], "f16"))
+            assert np.array_equal(v[s // page, :, s % page], ref[2][i])
+    assert not k[4, 0, 0].any() and not k[0, 0, 1].any()  # rows that no slot names
+
+
+def test_heads_rows_past_4_gib():
+    """The last rows of an activation whose offsets pass 2^32."""
+    t, hq, hkv, d = 360001, 32, 8, 128
+    x = torch.empty((t, (hq + 2 * hkv) * d), device="cuda", dtype=torch.bfloat16)
+    assert x.numel() * 2 > 1 << 32
+    rows = [0, 174762, 174763, 349525, 349526, t - 1]
+    x[rows] = torch.randn((len(rows), x.shape[1]), device="cuda").to(torch.bfloat16)
+    freq = _freq(d)
+    q, k, v = (torch.empty((t, h * d), device="cuda", dtype=torch.bfloat16) for h in (hq, hkv, hkv))
+    ea.heads(R.rel(x), R.rel(q), R.rel(k), R.rel(v), d_head=d, inv_freq=freq)
+    ref, err = R.heads(R.f64(x[rows]), hq, hkv, d, None, None, 0.0, R.f64(freq), False, np.asarray(rows))
+    for got, r, e in zip((q, k, v), ref, err):
+        R.check(R.f64(got[rows]).reshape(len(rows), -1, d), r, R.heads_tol(r, e, "bf16"))
+
+
+def test_weights_and_their_gradients_of_other_types():
+    t, hq, hkv, d = 30, 4, 2, 64
+    x, _, _, freq, pos = _inputs(t, hq, hkv, d, d, "bf16", True, 50, 14)
+    g = torch.Generator(device="cuda").manual_seed(15)
+    wq, wk = torch.randn(d, generator=g, device="cuda").half(), torch.randn(d, generator=g, device="cuda")
+    dq, dk, dv = (torch.randn((t, h * d), generator=g, device="cuda").to(torch.bfloat16) for h in (hq, hkv, hkv))
+    dx, dwq = torch.empty_like(x), torch.empty(d, device="cuda", dtype=torch.bfloat16)
+    # the keys' weight gradient is not wanted
+    ea.heads_backward(R.rel(x), R.rel(dq), R.rel(dk), R.rel(dv), R.rel(dx), d_head=d, wq=R.rel(wq), wk=R.rel(wk),
+                      dwq=R.rel(dwq), eps=EPS, inv_freq=freq, positions=pos)
+    tm = lambda z: R.f64(z).reshape(t, -1, d)
+    ref, scale, dws = R.heads_grad(R.f64(x), tm(dq), tm(dk), tm(dv), hq, hkv, d, R.f64(wq), R.f64(wk), EPS,
+                                   R.f64(freq), False, pos.cpu().numpy())
+    R.check(R.f64(dx), ref, R.HALF["bf16"] * np.abs(ref) + 1.01 * 96 * R.F * scale)
+    R.check(R.f64(dwq), dws[0], R.HALF["bf16"] * np.abs(dws[0]) + 1.01 * 160 * R.F * dws[1])

@@ -310,3 +310,30 @@ def test_long_walks_of_few_tiles(lens, groups):
     k, v, table = _batch(lens, None, groups, 16, 1, 128, "f16", 25)
     q = torch.randn((len(lens), 4, 128), device="cuda").half()
     _check(q, k, v, table, lens, None, groups, 16, "f16")
+
+
+def test_partitions_of_queries_and_output():
+    """Queries in blocks of 3 rows and 2 heads, the last ones shorter; the output
+    head-major in blocks of 4 rows."""
+    lens, hq, hkv, d, page = [40, 7, 0, 130, 64], 6, 2, 64, 16
+    k, v, table = _batch(lens, None, [], page, hkv, d, "bf16", 26)
+    q = torch.randn((5, hq, d), device="cuda").to(torch.bfloat16)
+    rq = R.blocked(q.view(5, hq * d), [R.splits(5, 3), R.splits(hq * d, 2 * d)])
+    out = ea.Relation((1, hq, 5, d), "bf16", [[0, 1], R.splits(hq, 4), R.splits(5, 4), [0, d]])
+    out.data.fill_(0xFF)
+    ea.attention_paged(rq, R.pages_rel(k), R.pages_rel(v), out, scale=0.2, table=R.i32(table), lengths=R.i32(lens))
+    ref, info = R.attention(R.f64(q), R.f64(k), R.f64(v), table, lens, page, list(range(6)), 0.2)
+    R.check(R.f64(R.unblocked(out)[0].transpose(0, 1)), ref, R.attention_tol(ref, info, "bf16", d))
+
+
+@pytest.mark.parametrize("groups", [[], [(0, 3, 48)]])
+def test_a_nan_query_is_its_own(groups):
+    lens = [60, 50, 90]
+    k, v, table = _batch(lens, None, groups, 16, 1, 64, "bf16", 27)
+    q = torch.randn((3, 4, 64), device="cuda").to(torch.bfloat16)
+    clean = _run(q, k, v, table, lens, None, groups, 0.125).clone()
+    q[1, 2, 5] = float("nan")
+    got = _run(q, k, v, table, lens, None, groups, 0.125)
+    assert torch.isnan(got[1, 2]).all()
+    got[1, 2] = clean[1, 2]
+    assert torch.equal(got, clean)
