@@ -536,8 +536,8 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
    the outputs hold the state as it came; status[1] is the number of free pages
    afterwards.  Entries behind a sequence's pages are not read, and are -1 in
    rewritten tables; an entry outside the cache counts no page.  n_seq <=
-   EA_PAGED_MAX_SEQ; n_seq * stride, n_pages * page_size and (stride + 1) *
-   page_size < 2^31 (EA_ERR_UNSUPPORTED beyond).  Asynchronous, no allocation, no plan. */
+   EA_PAGED_MAX_SEQ, n_pages <= 2^30; n_seq * stride, n_pages * page_size and
+   (stride + 1) * page_size < 2^31 (EA_ERR_UNSUPPORTED beyond).  Asynchronous, no allocation, no plan. */
 #define EA_PAGES_OK 0
 #define EA_PAGES_NONE_FREE 1 /* fewer free pages than the call needs            */
 #define EA_PAGES_TOO_LONG 2  /* a length below 0 or above a table row's keys    */
@@ -557,7 +557,7 @@ typedef struct ea_pages {
    by sequence, their slot (page * page_size + row) and position; entries
    behind them, up to n_tokens, get -1 and 0.  No array may overlap an output. */
 int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, int32_t* positions, int32_t n_tokens,
-                    void* stream);
+                    void* workspace, int64_t ws_bytes, void* stream);
 /* Sequence i becomes a copy of sequence parent[i] (outside [0, n_seq): empty),
    which forks, reorders and frees: whole pages are shared, a partly filled last
    page stays with the parent's first child and its rows are copied to a new
@@ -572,8 +572,8 @@ int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages*
    (out_lengths is not written); out_table and out_refs may be table and refs. */
 int ea_pages_compact(int32_t n_cache, ea_relation* const* caches, const ea_pages* state, void* workspace,
                      int64_t ws_bytes, void* stream);
-/* Workspace of select and compact: 256-byte aligned, behind its counter area
-   (which stays untouched) no initial value is needed. */
+/* Workspace of the three: 256-byte aligned, behind its counter area (which
+   stays untouched) no initial value is needed. */
 int ea_pages_workspace(int32_t n_seq, int32_t n_pages, int64_t* ws_bytes);
 
 /* ---- plan cache --------------------------------------------------------- */

@@ -31,6 +31,8 @@ class KVCache:
         self.table, self.lengths, self.refs = zeros(sequences, max_pages), zeros(sequences), zeros(pages)
         self._other = (zeros(sequences, max_pages), zeros(sequences), zeros(pages))
         self.status = zeros(2)
+        # of its own: captured calls share no workspace with another cache's
+        self._workspace = ea.new_workspace(ea.pages_workspace(sequences, pages), device=device)
 
     def extend(self, add: torch.Tensor, tokens: int):
         """add[s] more keys for every sequence; the new tokens' slots and
@@ -38,17 +40,18 @@ class KVCache:
         slots = torch.empty(tokens, dtype=torch.int32, device=self.table.device)
         positions = torch.empty_like(slots)
         ea.pages_extend(self.table, self.lengths, self.refs, add, page_size=self.page_size, status=self.status,
-                        slots=slots, positions=positions)
+                        slots=slots, positions=positions, workspace=self._workspace)
         return slots, positions
 
     def select(self, parent: torch.Tensor):
         """Sequence i becomes a copy of sequence parent[i] (-1: empty)."""
         table, lengths, refs = self._other
         ea.pages_select([self.data], parent, self.table, self.lengths, self.refs, out_table=table, out_lengths=lengths,
-                        out_refs=refs, status=self.status)
+                        out_refs=refs, status=self.status, workspace=self._workspace)
         self._other = (self.table, self.lengths, self.refs)
         self.table, self.lengths, self.refs = table, lengths, refs
 
     def compact(self):
         """Move the used pages to the first places."""
-        ea.pages_compact([self.data], self.table, self.lengths, self.refs, status=self.status)
+        ea.pages_compact([self.data], self.table, self.lengths, self.refs, status=self.status,
+                         workspace=self._workspace)

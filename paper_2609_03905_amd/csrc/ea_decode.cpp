@@ -406,8 +406,8 @@ int check_pages(const ea_pages* p, PagesArgs* a) {
   if (p->n_seq > EA_PAGED_MAX_SEQ)
     return fail(EA_ERR_UNSUPPORTED, "%d sequences, at most %d", p->n_seq, EA_PAGED_MAX_SEQ);
   if ((int64_t)p->n_seq * p->stride > INT32_MAX || (int64_t)p->n_pages * p->page_size > INT32_MAX ||
-      ((int64_t)p->stride + 1) * p->page_size > INT32_MAX)
-    return fail(EA_ERR_UNSUPPORTED, "a table, a cache or a table row of 2^31 or more");
+      ((int64_t)p->stride + 1) * p->page_size > INT32_MAX || p->n_pages > (1 << 30))
+    return fail(EA_ERR_UNSUPPORTED, "a table, a cache or a table row of 2^31 or more, or more than 2^30 pages");
   if (!p->table || !p->lengths || !p->refs || !p->out_table || !p->out_refs || !p->status)
     return fail(EA_ERR_ARG, "NULL array");
   a->n_seq = p->n_seq;
@@ -492,9 +492,10 @@ int ea_pages_workspace(int32_t n_seq, int32_t n_pages, int64_t* ws_bytes) {
 }
 
 int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, int32_t* positions, int32_t n_tokens,
-                    void* stream) {
+                    void* workspace, int64_t ws_bytes, void* stream) {
   PagesArgs a{};
-  const int e = check_pages(state, &a);
+  PagesCopyArgs c{};
+  int e = check_pages(state, &a);
   if (e) return e;
   if (!add || !state->out_lengths) return fail(EA_ERR_ARG, "NULL add or out_lengths");
   if (a.out_table != a.table) return fail(EA_ERR_ARG, "extend works in its table: out_table must be table");
@@ -507,6 +508,7 @@ int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, i
       overlap(add, a.n_seq * (int64_t)4, a.out_table, (int64_t)a.n_seq * a.stride * 4) ||
       overlap(add, a.n_seq * (int64_t)4, a.out_len, a.n_seq * (int64_t)4))
     return fail(EA_ERR_ARG, "add overlaps an output");
+  if ((e = check_pages_ws(state, workspace, ws_bytes, &a, &c))) return e;
   a.add = add;
   a.slots = slots;
   a.pos = positions;

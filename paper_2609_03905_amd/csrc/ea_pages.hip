@@ -11,14 +11,14 @@
 //
 // The bookkeeping is some thousand integers: bound by the latency of dependent
 // steps, not by bandwidth, so one workgroup of 16 waves does it between
-// barriers (the parts of select that touch every entry of a large table are
-// launches of their own).  Each wave owns a contiguous range of the pages; inside
-// it a free page's rank is a population count of lane ballots, and 16 wave totals
-// are the only numbers that cross waves.  Moving the pages' contents is bound by
-// HBM and runs in a launch on the whole chip.  Measured: new pages for 256
-// sequences in a cache of 33 thousand pages 17 us (10 of them the two walks over
-// all counts); a beam step over 64 sequences 10 us and its copies, 134 MB moved,
-// 30; 1.35 GB made dense 8 us and 275, against 263 at a large copy's rate.
+// barriers (extend's counting, and the parts of select that touch every entry of
+// a large table, are launches of their own).  Each wave owns a contiguous range
+// of the pages; inside it a free page's rank is a population count of lane
+// ballots, and 16 wave totals are the only numbers that cross waves.  Moving the
+// pages' contents is bound by HBM and runs in a launch on the whole chip.
+// Measured: new pages for 256 sequences in a cache of 33 thousand pages 11.5 us;
+// a beam step over 64 sequences 10 us and its copies, 134 MB moved, 30; 1.35 GB
+// made dense 8 us and 275, against 263 at a large copy's rate.
 #include "ea_decode.h"
 #include "ea_device.h"
 
@@ -35,7 +35,7 @@ constexpr int kWorkCount = 0;   // pages to move
 constexpr int kWorkUsed = 1;    // compact: pages in use
 constexpr int kWorkLists = 16;  // then source pages, destinations and rows
 
-constexpr int kList = 4096;     // pages that extend hands out at a time
+constexpr int kBlock = 4 * kMetaThreads;  // pages that a workgroup looks at together
 // Table entries and pages up to which select's bookkeeping is one workgroup's;
 // beyond, three launches of many (6.5 thousand: 13.5 us in one workgroup, 16.2 in
 // three launches; 25 thousand: 27 and 21; 200 thousand: 157 and 31).
@@ -134,10 +134,9 @@ __device__ __forceinline__ int free_before(const int32_t* refs, int n_pages, int
 }
 
 // Walk of a wave's pages in order: f(page, refs, rank among the free pages),
-// until the rank `limit`; copies the counts to `copy` (null: no copy) on the
-// way, to the end.
+// until the rank `limit`.
 template <class F>
-__device__ __forceinline__ void each_page(const int32_t* refs, int32_t* copy, int n_pages, int before, int limit, F f) {
+__device__ __forceinline__ void each_page(const int32_t* refs, int n_pages, int before, int limit, F f) {
   constexpr int kAhead = 4;
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   int begin, end;
@@ -147,36 +146,26 @@ __device__ __forceinline__ void each_page(const int32_t* refs, int32_t* copy, in
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) ahead[i] = load_refs(refs, begin + 256 * i + 4 * lane, n_pages);
   for (int p0 = begin; p0 < end; p0 += 256) {
-    if (run >= limit && !copy) return;
+    if (run >= limit) return;
     const int p = p0 + 4 * lane;
     const i32x4_t v = ahead[0];
 #pragma unroll
     for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
     ahead[kAhead - 1] = load_refs(refs, p + 256 * kAhead, n_pages);
-    if (run < limit) {
-      int rank = run, all = 0;
+    int rank = run, all = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint64_t b = __ballot(p + i < end && v[i] <= 0);
-        rank += __popcll(b & ((uint64_t(1) << lane) - 1));
-        all += __popcll(b);
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t b = __ballot(p + i < end && v[i] <= 0);
+      rank += __popcll(b & ((uint64_t(1) << lane) - 1));
+      all += __popcll(b);
+    }
+    run += all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p + i < end) {
+        f(p + i, v[i], rank);
+        rank += v[i] <= 0;
       }
-      run += all;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (p + i < end) {
-          f(p + i, v[i], rank);
-          rank += v[i] <= 0;
-        }
-    }
-    if (!copy) continue;
-    if (p + 3 < end) {
-      *reinterpret_cast<i32x4_t*>(copy + p) = v;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (p + i < end) copy[p + i] = v[i];
-    }
   }
 }
 
@@ -198,13 +187,45 @@ __device__ __forceinline__ void set_status(const PagesArgs& a, int code, int lef
   }
 }
 
-// New pages for add[s] more keys of every sequence; slots and positions of the
-// new tokens, sequence by sequence.
-__global__ __launch_bounds__(kMetaThreads) void extend_kernel(const PagesArgs a) {
-  __shared__ int s_need[kMaxSeq], s_tok[kMaxSeq], s_len[kMaxSeq];  // exclusive sums over sequences
-  __shared__ int s_list[kList];
+// ---- extend: new pages for add[s] more keys of every sequence; slots and
+// positions of the new tokens, sequence by sequence.
+// Free pages of every block of 4096, in a launch on the whole chip; copies the
+// counts on the way where they are not updated in place.  (Counted and copied by
+// the one workgroup that goes on: 3 thousand pages 8.4 us in place and 11.6 into
+// other arrays instead of 7.2 and 10.6, 33 thousand 9.2 and 17.4 instead of 7.8
+// and 11.5, a million 84 and 309 instead of 8.2 and 12.2.)
+__global__ __launch_bounds__(kMetaThreads) void count_free_kernel(const PagesArgs a) {
   __shared__ int s_wave[kMetaWaves];
-  const int tid = threadIdx.x;
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const int blocks = (a.n_pages + kBlock - 1) / kBlock;
+  for (int b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const int p = b * kBlock + 4 * threadIdx.x;
+    const i32x4_t v = load_refs(a.refs, p, a.n_pages);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (p + i >= a.n_pages) continue;
+      n += v[i] <= 0;
+      if (a.out_refs != a.refs) a.out_refs[p + i] = v[i];
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) n += __shfl_xor(n, o);
+    __syncthreads();
+    if (lane == 0) s_wave[wid] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int all = 0;
+      for (int i = 0; i < kMetaWaves; ++i) all += s_wave[i];
+      a.work[kWorkLists + b] = all;
+    }
+  }
+}
+
+__global__ __launch_bounds__(kMetaThreads) void extend_kernel(const PagesArgs a) {
+  __shared__ int s_need[kMaxSeq], s_tok[kMaxSeq], s_len[kMaxSeq];  // the first two: exclusive sums over sequences
+  __shared__ int s_list[kBlock], s_block[kMetaThreads], s_base[kMetaThreads];
+  __shared__ int s_wave[kMetaWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int per = (a.n_seq + kMetaThreads - 1) / kMetaThreads;
   const int s0 = min(a.n_seq, tid * per), s1 = min(a.n_seq, s0 + per);
   int need = 0, tok = 0, bad = 0;
@@ -220,7 +241,10 @@ __global__ __launch_bounds__(kMetaThreads) void extend_kernel(const PagesArgs a)
       tok += (int)add;
     }
   }
-  int all_need, all_tok;
+  const int blocks = (a.n_pages + kBlock - 1) / kBlock;
+  int in_mine = 0, all_free, all_need, all_tok;
+  for (int b = tid; b < blocks; b += kMetaThreads) in_mine += a.work[kWorkLists + b];
+  block_scan(in_mine, s_wave, &all_free);
   const int need0 = block_scan(need, s_wave, &all_need);
   const int tok0 = block_scan(tok, s_wave, &all_tok);
   for (int s = s0; s < s1; ++s) {
@@ -228,31 +252,53 @@ __global__ __launch_bounds__(kMetaThreads) void extend_kernel(const PagesArgs a)
     s_tok[s] += tok0;
   }
   bad = __syncthreads_or(bad);
-  int all_free;
-  int before = free_before(a.refs, a.n_pages, s_wave, &all_free);
   const int code = bad ? EA_PAGES_TOO_LONG : all_need > all_free ? EA_PAGES_NONE_FREE : 0;
   if (code) all_need = all_tok = 0;
-  // the lowest free pages into a list, as many as it holds at a time; then a
-  // thread each to hand them out
-  const int32_t* from = a.refs;
-  int32_t* copy = a.out_refs == a.refs ? nullptr : a.out_refs;
-  for (int base = 0; base == 0 || base < all_need; base += kList) {
-    const int n = min(kList, all_need - base);
-    each_page(from, copy, a.n_pages, before, n, [&](int p, int refs, int rank) {
-      if (refs <= 0 && rank < n) s_list[rank] = p;
-    });
-    settle();
-    for (int i = tid; i < n; i += kMetaThreads) {
-      const int s = last_at_most(s_need, a.n_seq, base + i), p = s_list[i];
-      a.out_table[(int64_t)s * a.stride + held(s_len[s], a.page_size) + base + i - s_need[s]] = p;
-      a.out_refs[p] = 1;
+  // the lowest free pages, a block of 4096 at a time: listed by rank, then
+  // handed out a thread each.  Blocks without free pages are passed over.
+  int run = 0;
+  for (int c0 = 0; c0 < blocks && run < all_need; c0 += kMetaThreads) {
+    const int b = c0 + tid;
+    const int n = b < blocks ? a.work[kWorkLists + b] : 0;
+    int in_chunk, some;
+    const int before = block_scan(n, s_wave, &in_chunk);
+    const bool mine = n > 0 && run + before < all_need;
+    const int at = block_scan(mine, s_wave, &some);
+    if (mine) {
+      s_block[at] = b;
+      s_base[at] = run + before;
     }
-    if (base + n >= all_need) break;
-    settle();  // the pages handed out are no longer free
-    from = a.out_refs;
-    copy = nullptr;
-    int left;
-    before = free_before(from, a.n_pages, s_wave, &left);
+    __syncthreads();
+    for (int k = 0; k < some; ++k) {
+      const int base = s_base[k], p = s_block[k] * kBlock + 4 * tid;
+      const i32x4_t v = load_refs(a.out_refs, p, a.n_pages);
+      int rank = 0, here = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t m = __ballot(p + i < a.n_pages && v[i] <= 0);
+        rank += __popcll(m & ((uint64_t(1) << lane) - 1));
+        here += __popcll(m);
+      }
+      if (lane == 0) s_wave[wid] = here;
+      __syncthreads();
+      int found = 0;
+      for (int i = 0; i < kMetaWaves; ++i) {
+        if (i < wid) rank += s_wave[i];
+        found += s_wave[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (p + i < a.n_pages && v[i] <= 0) s_list[rank++] = p + i;
+      __syncthreads();
+      found = min(found, all_need - base);
+      for (int i = tid; i < found; i += kMetaThreads) {
+        const int s = last_at_most(s_need, a.n_seq, base + i), pg = s_list[i];
+        a.out_table[(int64_t)s * a.stride + held(s_len[s], a.page_size) + base + i - s_need[s]] = pg;
+        a.out_refs[pg] = 1;
+      }
+      run = base + found;
+      __syncthreads();
+    }
   }
   set_status(a, code, all_free - all_need);
   settle();
@@ -303,6 +349,7 @@ __device__ __forceinline__ int load_family(const PagesArgs& a, Family& f) {
   return bad;
 }
 
+// The counts as they come, by workgroup `block` of `blocks`.
 __device__ __forceinline__ void copy_refs(const PagesArgs& a, int block, int blocks) {
   for (int64_t p0 = (int64_t)block * 4 * kMetaThreads + threadIdx.x; p0 < a.n_pages;
        p0 += (int64_t)blocks * 4 * kMetaThreads) {
@@ -397,7 +444,7 @@ __global__ __launch_bounds__(kMetaThreads) void select_kernel(const PagesArgs a)
   const int before = free_before(a.out_refs, a.n_pages, s_wave, &all_free);
   const int code = bad ? EA_PAGES_TOO_LONG : count > all_free ? EA_PAGES_NONE_FREE : 0;
   if (!code) {
-    each_page(a.out_refs, nullptr, a.n_pages, before, count, [&](int p, int refs, int r) {
+    each_page(a.out_refs, a.n_pages, before, count, [&](int p, int refs, int r) {
       if (refs <= 0 && r < count) dst[r] = p;
     });
     settle();
@@ -437,7 +484,7 @@ __global__ __launch_bounds__(kMetaThreads) void compact_kernel(const PagesArgs a
   const int n_used = a.n_pages - all_free;
   if (tid == 0) s_moves = 0;
   __syncthreads();
-  each_page(a.refs, nullptr, a.n_pages, before, 0x7fffffff, [&](int p, int refs, int free_rank) {
+  each_page(a.refs, a.n_pages, before, 0x7fffffff, [&](int p, int refs, int free_rank) {
     if (p < n_used && refs <= 0) dst[free_rank] = p;
     if (p == n_used - 1) s_moves = free_rank + (refs <= 0);
     // the free pages before n_used are as many as the used ones behind it, and
@@ -549,6 +596,8 @@ dim3 copy_grid(const PagesCopyArgs& c) {
 }  // namespace
 
 hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s) {
+  const int blocks = (a.n_pages + kBlock - 1) / kBlock;
+  count_free_kernel<<<dim3(blocks < 1024 ? blocks : 1024), dim3(kMetaThreads), 0, s>>>(a);
   extend_kernel<<<dim3(1), dim3(kMetaThreads), 0, s>>>(a);
   return hipGetLastError();
 }

@@ -108,7 +108,7 @@ def lib() -> ctypes.CDLL:
         L.ea_attention_paged_workspace.argtypes = [vp, vp, P(_Paged), P(i64)]
         L.ea_attention_paged.argtypes = [vp] * 4 + [P(_Paged), vp, i64, vp]
         L.ea_pages_workspace.argtypes = [i32, i32, P(i64)]
-        L.ea_pages_extend.argtypes = [P(_Pages), vp, vp, vp, i32, vp]
+        L.ea_pages_extend.argtypes = [P(_Pages), vp, vp, vp, i32, vp, i64, vp]
         L.ea_pages_select.argtypes = [i32, P(vp), P(_Pages), vp, vp, i64, vp]
         L.ea_pages_compact.argtypes = [i32, P(vp), P(_Pages), vp, i64, vp]
         L.ea_plan_cache_size.restype = i64
@@ -408,19 +408,21 @@ _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_d
 def _device_array(t, name: str, shape, dtype=torch.int32, optional: bool = False):
     """The address of a small device array, checked: type, shape (None: any
     extent), rows without gaps, on the current device."""
+    if t is None and optional:
+        return None
+    # the usual case in five cheap questions; what is wrong is found below
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and 0 <= t.get_device() == _get_device() and t.is_contiguous() \
+            and (t.shape == shape or len(t.shape) == len(shape) == 1 and shape[0] is None):
+        return t.data_ptr()
     if t is None:
-        if optional:
-            return None
         raise EAError(ERR_ARG, f"{name} is missing")
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
         raise EAError(ERR_ARG, f"{name} is no {dtype} tensor")
-    if t.shape != shape and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
         raise EAError(ERR_ARG, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if not t.is_contiguous():
         raise EAError(ERR_ARG, f"{name} is not contiguous")
-    if not t.is_cuda or t.get_device() != _get_device():
-        raise EAError(ERR_ARG, f"{name} is on {t.device}, not on the current GPU")
-    return t.data_ptr()
+    raise EAError(ERR_ARG, f"{name} is on {t.device}, not on the current GPU")
 
 
 def _on_device(*rels):
@@ -546,7 +548,8 @@ def _pages(table, lengths, refs, page_size, out_table, out_lengths, out_refs, st
 
 def pages_extend(table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, add: torch.Tensor, *, page_size: int,
                  status: torch.Tensor, out_lengths: torch.Tensor | None = None, out_refs: torch.Tensor | None = None,
-                 slots: torch.Tensor | None = None, positions: torch.Tensor | None = None, stream=None) -> None:
+                 slots: torch.Tensor | None = None, positions: torch.Tensor | None = None, stream=None,
+                 workspace: torch.Tensor | None = None) -> None:
     """Pages for add[s] more keys of every sequence, lowest free ones first:
     written into ``table``; ``lengths`` and ``refs`` are updated (in place
     unless outputs are given).  ``slots`` and ``positions`` receive the new
@@ -557,8 +560,10 @@ def pages_extend(table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor,
     ps = _device_array(slots, "slots", (None,), optional=True)
     pp = _device_array(positions, "positions", (None if slots is None else slots.numel(),), optional=True)
     n = slots.numel() if ps else positions.numel() if pp else 0
-    _check(lib().ea_pages_extend(ctypes.byref(st), _device_array(add, "add", (table.shape[0],)), ps, pp, n,
-                                 _stream(stream)))
+    a = _device_array(add, "add", (table.shape[0],))
+    s = _stream(stream)
+    ws, nbytes = _pages_workspace(st, workspace, s)
+    _check(lib().ea_pages_extend(ctypes.byref(st), a, ps, pp, n, ws, nbytes, s))
 
 
 def _page_caches(caches):
@@ -567,10 +572,15 @@ def _page_caches(caches):
     return len(caches), _handles(caches), caches[0].shape[-2] if caches else None
 
 
-def _pages_workspace(st, workspace, s):
+def pages_workspace(sequences: int, pages: int) -> int:
+    """Workspace bytes of the page table's calls."""
     need = ctypes.c_int64()
-    _check(lib().ea_pages_workspace(st.n_seq, st.n_pages, ctypes.byref(need)))
-    return _workspace(need.value, workspace, s)
+    _check(lib().ea_pages_workspace(sequences, pages, ctypes.byref(need)))
+    return need.value
+
+
+def _pages_workspace(st, workspace, s):
+    return _workspace(pages_workspace(st.n_seq, st.n_pages), workspace, s)
 
 
 def pages_select(caches: Sequence[Relation], parent: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,

@@ -188,9 +188,11 @@ def state(**change):
     return E._Pages(*[f[n] for n, _ in E._Pages._fields_])
 
 
-def extend(add=A + (7 << 20), n_tokens=3, **change):
-    s = state(**{"out_table": A, **change})
-    return ea.lib().ea_pages_extend(ctypes.byref(s), add, A + (8 << 20), None, n_tokens, None)
+def extend(add=A + (7 << 20), n_tokens=3, ws=256, n=None, **change):
+    s, need = state(**{"out_table": A, **change}), ctypes.c_int64()
+    ea.lib().ea_pages_workspace(max(s.n_seq, 1), max(s.n_pages, 1), ctypes.byref(need))
+    return ea.lib().ea_pages_extend(ctypes.byref(s), add, A + (8 << 20), None, n_tokens, ws,
+                                    need.value if n is None else n, None)
 
 
 def select(caches=(), parent=A + (7 << 20), ws=256, n=None, **change):
@@ -211,7 +213,8 @@ def compact(caches=(), ws=256, n=None, **change):
 @pytest.mark.parametrize("code,change", [
     (ARG, dict(n_seq=0)), (ARG, dict(stride=0)), (ARG, dict(n_pages=0)), (ARG, dict(page_size=0)),
     (ARG, dict(n_pages=-5)), (UNSUPPORTED, dict(n_seq=2049)), (UNSUPPORTED, dict(n_seq=2048, stride=1 << 20)),
-    (UNSUPPORTED, dict(n_pages=1 << 28)), (UNSUPPORTED, dict(stride=1 << 27, n_seq=1)),
+    (UNSUPPORTED, dict(n_pages=1 << 28)), (UNSUPPORTED, dict(n_pages=(1 << 30) + 1, page_size=1)),
+    (UNSUPPORTED, dict(stride=1 << 27, n_seq=1)),
     (ARG, dict(table=None)), (ARG, dict(lengths=None)), (ARG, dict(refs=None)), (ARG, dict(out_refs=None)),
     (ARG, dict(status=None)), (ARG, dict(out_refs=A + 4)), (ARG, dict(status=A + (2 << 20))),
     (ARG, dict(out_refs=A + (2 << 20) + 4)),
@@ -225,14 +228,15 @@ def test_pages_refusals_of_one_call():
     assert extend(out_table=A + (3 << 20)) == ARG  # it works in its table
     for bad in (A, A + (1 << 20), A + (2 << 20), A + (6 << 20), A + (7 << 20)):  # slots over another array
         s = state(out_table=A)
-        assert ea.lib().ea_pages_extend(ctypes.byref(s), A + (7 << 20), bad, None, 3, None) == ARG
-        assert ea.lib().ea_pages_extend(ctypes.byref(s), A + (7 << 20), None, bad, 3, None) == ARG
+        assert ea.lib().ea_pages_extend(ctypes.byref(s), A + (7 << 20), bad, None, 3, 256, 1 << 30, None) == ARG
+        assert ea.lib().ea_pages_extend(ctypes.byref(s), A + (7 << 20), None, bad, 3, 256, 1 << 30, None) == ARG
     assert extend(add=A + (4 << 20)) == ARG and extend(add=A + (5 << 20)) == ARG and extend(add=A) == ARG
     for bad in (3, 4, 5, 6):
         assert select(parent=A + (bad << 20)) == ARG
     assert select(parent=None) == ARG and select(out_lengths=None) == ARG
     for same in (dict(out_table=A), dict(out_lengths=A + (1 << 20)), dict(out_refs=A + (2 << 20))):
         assert select(**same) == ARG
+    assert extend(ws=None) == ARG and extend(ws=64) == ARG and extend(n=100) == CAPACITY
     for call in (select, compact):
         assert call(ws=None) == ARG and call(ws=64) == ARG and call(n=100) == CAPACITY
         c = cache(30, 2, 16, 64, planes=3)

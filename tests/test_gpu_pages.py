@@ -55,7 +55,8 @@ class Device:
 
 @pytest.mark.parametrize("n_seq,stride,n_pages,page,seed", [(1, 3, 4, 1, 0), (1, 1, 1, 16, 1), (5, 6, 17, 4, 2),
                                                             (40, 9, 300, 7, 3), (300, 5, 1025, 16, 4),
-                                                            (7, 40, 5000, 3, 5)])
+                                                            (7, 40, 5000, 3, 5),
+                                                            (200, 60, 9000, 2, 6), (4, 5000, 3000, 2, 7)])
 def test_random_walk(n_seq, stride, n_pages, page, seed):
     rng = np.random.default_rng(seed)
     planes = rng.integers(-30000, 30000, (2, n_pages, 2, page, 64)).astype(np.int16)
@@ -128,6 +129,31 @@ def test_more_pages_than_one_round_hands_out(in_place):
         dev.same(ref)
 
 
+@pytest.mark.parametrize("n_pages", [4096, 16384, 16385, 40000])
+def test_few_free_places_of_many(n_pages):
+    """Free pages at the ends of blocks of pages, and one short of enough."""
+    ref = R.Pages(5, 20, n_pages, 3)
+    ref.refs[:] = 1
+    places = sorted({0, 4095, n_pages // 2, n_pages - 4, n_pages - 1} | ({4096, 8191, 8192, 16383} if n_pages > 16384
+                                                                       else set()))
+    ref.refs[places] = 0
+    dev = Device(ref)
+    for add in ([0, 3, 1, 0, 0], [1, 0, 0, 0, 4], [60, 0, 0, 0, 0], [3] * 5):
+        want, got = ref.extend(add, sum(add)), dev.extend(add, sum(add), in_place=n_pages % 2 == 0)
+        assert got[0] == want[0] and np.array_equal(got[1], want[1]) and np.array_equal(got[2], want[2])
+        dev.same(ref)
+
+
+def test_a_fork_over_a_large_table_that_fits_nowhere():
+    ref = R.Pages(4, 5000, 100, 4)
+    dev = Device(ref)
+    assert dev.extend([200, 99, 99, 0], 0)[0] == ref.extend([200, 99, 99, 0], 0)[0] == (ea.PAGES_OK, 0)
+    assert dev.select([0, 1, 2, 1]) == ref.select([0, 1, 2, 1]) == (ea.PAGES_NONE_FREE, 0)
+    dev.same(ref)
+    assert dev.select([0, 1, 0, 1]) == ref.select([0, 1, 0, 1]) == (ea.PAGES_OK, 24)
+    dev.same(ref)
+
+
 def test_a_fork_that_fits_nowhere_does_nothing():
     ref = R.Pages(2, 3, 2, 4)
     dev = Device(ref)
@@ -196,7 +222,7 @@ def test_captured_step():
     st, ws = R.i32([0, 0]), ea.new_workspace(1 << 20)
 
     def step():
-        ea.pages_extend(table, ln, refs, add, page_size=page, status=st)
+        ea.pages_extend(table, ln, refs, add, page_size=page, status=st, workspace=ws)
         ea.pages_select([], parent, table, ln, refs, out_table=t2, out_lengths=l2, out_refs=r2, status=st,
                         page_size=page, workspace=ws)
         table.copy_(t2), ln.copy_(l2), refs.copy_(r2)
@@ -212,3 +238,41 @@ def test_captured_step():
         assert tuple(st.tolist()) == code
         assert np.array_equal(table.cpu().numpy(), ref.table) and np.array_equal(refs.cpu().numpy(), ref.refs)
         assert torch.equal(ln.cpu(), torch.from_numpy(ref.len))
+
+
+def test_pages_past_4_gib():
+    """Copies and moves between pages whose byte offsets pass 2^32, in two
+    planes; a page of several pieces."""
+    heads, page, d, n_pages = 8, 100, 128, 12000
+    cache = torch.empty((2, n_pages, heads, page, d), device="cuda", dtype=torch.bfloat16)
+    assert cache[0].numel() * 2 > 2 << 30 and cache.numel() * 2 > 1 << 32
+    rel = R.pages_rel(cache)
+    table, ln = R.i32([[n_pages - 1, n_pages - 2], [-1, -1]]), R.i32([page + 37, 0])
+    refs = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+    refs[n_pages - 7] = 0  # the only free place
+    cache[:, n_pages - 2:] = torch.randn((2, 2, heads, page, d), device="cuda").to(torch.bfloat16)
+    cache[:, n_pages - 7] = 5.0
+    want = cache[:, n_pages - 2, :, :37].clone()
+    t2, l2, r2, st = torch.empty_like(table), torch.empty_like(ln), torch.empty_like(refs), R.i32([9, 9])
+    ea.pages_select([rel], R.i32([0, 0]), table, ln, refs, out_table=t2, out_lengths=l2, out_refs=r2, status=st)
+    assert st.tolist() == [ea.PAGES_OK, 0]
+    assert t2.tolist() == [[n_pages - 1, n_pages - 2], [n_pages - 1, n_pages - 7]] and l2.tolist() == [page + 37] * 2
+    assert torch.equal(cache[:, n_pages - 7, :, :37], want) and (cache[:, n_pages - 7, :, 37:] == 5.0).all()
+    assert r2[n_pages - 1] == 2 and r2[n_pages - 7] == 1
+    # three places of the first pages become free: the last three used pages move there
+    r2[[2, 9, 11]] = 0
+    last = cache[:, n_pages - 3:].clone()
+    ea.pages_compact([rel], t2, l2, r2, status=st)
+    assert st.tolist() == [ea.PAGES_OK, 3] and t2.tolist() == [[11, 9], [11, n_pages - 7]]
+    assert all(torch.equal(cache[:, p], last[:, i]) for i, p in enumerate((2, 9, 11)))
+    assert r2[:n_pages - 3].min() == 1 and r2[11] == 2 and not r2[n_pages - 3:].any()
+
+
+def test_positions_alone_and_nothing_wanted():
+    ref = R.Pages(3, 4, 9, 4)
+    t, ln, rf, st = R.i32(ref.table), R.i32(ref.len), R.i32(ref.refs), R.i32([9, 9])
+    pos = R.i32([7] * 6)
+    ea.pages_extend(t, ln, rf, R.i32([2, 0, 3]), page_size=4, status=st, positions=pos)
+    assert pos.tolist() == [0, 1, 0, 1, 2, 0] and st.tolist() == [ea.PAGES_OK, 7]
+    ea.pages_extend(t, ln, rf, R.i32([3, 1, 0]), page_size=4, status=st)
+    assert ln.tolist() == [5, 1, 3] and t[0, :2].tolist() == [0, 2] and t[1, 0] == 3 and st.tolist() == [0, 5]
