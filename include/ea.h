@@ -502,7 +502,7 @@ int ea_heads_backward(const ea_relation* qkv, const ea_relation* wq, const ea_re
    captured call follows them.  Lengths are taken as at most a table row's
    keys; a key whose page lies outside the cache is invisible.  Rows behind the
    last sequence's stay as they were.  Keys and values that a row does not see
-   must be finite where the same call sees them in another row. */
+   leave it alone whatever they hold, infinities and NaN among them. */
 #define EA_PAGED_MAX_SEQ 2048
 typedef struct ea_paged {
   float scale;                 /* of the scores: positive, finite                  */

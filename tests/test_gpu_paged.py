@@ -337,3 +337,55 @@ def test_a_nan_query_is_its_own(groups):
     assert torch.isnan(got[1, 2]).all()
     got[1, 2] = clean[1, 2]
     assert torch.equal(got, clean)
+
+
+HIDDEN = [
+    # lens, groups, n_q, hq, hkv, d, dtype, key of sequence 0 (as the last of all the first rows do not see it)
+    ([70, 45], [], 3, 4, 2, 128, "bf16", 69),
+    ([300, 200], [], 2, 4, 1, 64, "f16", 299),
+    ([161, 40], [], 5, 4, 1, 128, "f16", 158),
+    ([129, 40], [], 5, 8, 2, 64, "bf16", 126),
+    ([90, 200], [], 12, 4, 1, 128, "bf16", 80),
+    ([64, 20], [], 12, 8, 2, 64, "f16", 60),
+    ([130, 70], [], 30, 4, 1, 128, "f16", 128),
+    ([500, 70], [], 30, 4, 1, 64, "bf16", 480),
+    ([64, 100, 64], [(0, 3, 64)], 5, 8, 2, 64, "bf16", 62),
+    ([64, 100, 80], [(0, 3, 64)], 5, 8, 1, 128, "f16", 61),  # 120 columns
+    ([64, 200, 210, 220, 230], [(0, 5, 64)], 5, 8, 1, 128, "bf16", 63),
+]
+
+
+@pytest.mark.parametrize("case", HIDDEN, ids=[f"n{len(c[0])}_g{len(c[1])}_q{c[2]}_h{c[3]}_{c[4]}_d{c[5]}_{c[6]}"
+                                              for c in HIDDEN])
+def test_what_a_row_does_not_see_may_be_anything(case):
+    """A value's infinities and NaN reach the rows that see its key, in their own
+    elements, and no other; then its key is NaN too."""
+    lens, groups, n_q, hq, hkv, d, dtype, key = case
+    page, h, g = 16, hkv - 1, hq // hkv
+    k, v, table = _batch(lens, None, groups, page, hkv, d, dtype, 28)
+    q = torch.randn((len(lens) * n_q, hq, d), device="cuda").to(R.TORCH[dtype])
+    starts = [n_q * i for i in range(len(lens) + 1)]
+    at = (table[0, key // page], h, key % page)
+    v[at][3], v[at][d // 2], v[at][d - 1] = float("inf"), -float("inf"), float("nan")
+    finite = torch.nan_to_num(v.double(), nan=0.0, posinf=0.0, neginf=0.0)
+    ref, info = R.attention(R.f64(q), R.f64(k), R.f64(finite), table, lens, page, starts, 0.125)
+    tol = R.attention_tol(ref, info, dtype, d)
+    sees = np.zeros(len(q), bool)
+    for s, n in enumerate(lens):
+        for i in range(n_q):
+            sees[s * n_q + i] = table[s, key // page] == at[0] and key < n - n_q + i + 1
+    assert sees.any() and not sees[:n_q].all()
+    heads = slice(h * g, (h + 1) * g)
+    for _ in range(2):
+        got = R.f64(_run(q, k, v, table, lens, starts, groups, 0.125))
+        rows = got[sees][:, heads]
+        if not np.isnan(R.f64(k)).any():
+            assert (rows[..., 3] == np.inf).all() and (rows[..., d // 2] == -np.inf).all()
+            assert np.isnan(rows[..., d - 1]).all()
+            rows[..., [3, d // 2, d - 1]] = ref[sees][:, heads][..., [3, d // 2, d - 1]]
+        else:
+            assert np.isnan(rows).all()
+            rows = ref[sees][:, heads]
+        got[np.ix_(np.flatnonzero(sees), np.arange(hq)[heads])] = rows
+        R.check(got, ref, tol)
+        k[at][5] = float("nan")
