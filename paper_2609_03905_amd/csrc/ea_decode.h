@@ -92,10 +92,9 @@ constexpr int kHeadsGradMaxWg = 768;
 hipError_t launch_heads_grad(const HeadsGradArgs& a, int32_t dtype, hipStream_t s);
 
 // ---- attention over pages ------------------------------------------------------
-constexpr int kPagedMaxSeg = EA_PAGED_MAX_SEQ;  // sequences and groups of one call
-constexpr int kPagedCols = 16;                  // query columns of a matrix tile
-constexpr int kPagedStep = 128;                 // keys that a workgroup takes at a time
-constexpr int kPagedWideStep = 64;              // and with many columns
+constexpr int kPagedCols = 16;      // query columns of a matrix tile
+constexpr int kPagedStep = 128;     // keys that a workgroup takes at a time
+constexpr int kPagedWideStep = 64;  // and with many columns
 
 struct PagedSeg {  // what the join needs of a segment
   int32_t r0, r1;       // query rows
