@@ -39,8 +39,8 @@
 //
 // Measured (bf16 or fp16, 32 query heads over 8, D = 128): 48 sequences of up to
 // 8K keys 148 us, 5.4 TB/s (5.1 is a large copy's rate); 64 sequences that share
-// 8K keys 40 + 8 us (walk, join), 32 that share 64K 82 + 8 us, where the bytes
-// take 20 and 66; one sequence of 1000 keys 9.7 us.  With every column tile
+// 8K keys 40 + 8 us (walk, join), 32 that share 64K 84 + 8 us, where the bytes
+// take 20 and 66; one sequence of 1000 keys 10.3 us.  With every column tile
 // reading the shared keys for itself the last two took 92 and 213 us.
 #include "ea_decode.h"
 #include "ea_device.h"
