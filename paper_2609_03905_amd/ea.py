@@ -446,6 +446,8 @@ def _workspace(need: int, workspace, stream):
         return None, 0
     if workspace is None:
         workspace = _stream_workspace(need, stream)
+    elif not 0 <= workspace.get_device() == _get_device() or not workspace.is_contiguous():
+        raise EAError(ERR_ARG, f"the workspace is on {workspace.device}, not on the current GPU, or has gaps")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 

@@ -276,3 +276,8 @@ def test_binding_checks_device_arrays():
     _raises(ARG, lambda: ea.pages_extend(i(20), i(4), i(30), i(4), **st))
     _raises(ARG, lambda: ea.pages_extend(i(4, 5), i(4), None, i(4), **st))
     _raises(ARG, lambda: ea.pages_extend(i(4, 5), i(4), i(30), i(4), **st))
+
+
+def test_a_workspace_of_the_host_is_refused():
+    with pytest.raises(ea.EAError, match="workspace"):
+        E._workspace(256, torch.zeros(512, dtype=torch.uint8), None)
