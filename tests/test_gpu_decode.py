@@ -115,3 +115,31 @@ def test_packed_sequences_start_at_position_zero():
     both = R.unblocked(_share(384, w, x, seq_ends=[128, 384]).forward()).clone()
     _close(both[:128], R.unblocked(_share(128, w, x[:128]).forward()))
     _close(both[128:], R.unblocked(_share(256, w, x[128:]).forward()))
+
+
+def test_two_caches_captured_grow_as_by_eager_calls():
+    """Each cache has a workspace of its own: two graphs replayed on two streams
+    give what eager calls give, every replay."""
+    add = [R.i32([1, 3, 0]), R.i32([2, 0, 5])]
+    make = lambda: [KVCache(1, 9000 + 100 * i, 1, 4, 64, 3, 40) for i in range(2)]
+    caches, eager = make(), make()
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for c, a in zip(caches, add):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c.extend(a, 8))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(6):
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        want = [c.extend(a, 8) for c, a in zip(eager, add)]
+        torch.cuda.synchronize()
+        for c, e, o, w in zip(caches, eager, outs, want):
+            assert torch.equal(o[0], w[0]) and torch.equal(o[1], w[1])
+            for x, y in ((c.table, e.table), (c.lengths, e.lengths), (c.refs, e.refs), (c.status, e.status)):
+                assert torch.equal(x, y)
+        assert caches[0].status.tolist()[0] == ea.PAGES_OK
