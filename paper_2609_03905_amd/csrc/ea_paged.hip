@@ -66,41 +66,38 @@ __device__ __forceinline__ f32x4_t mfma16(const uint4& a, const uint4& b, const 
                                                   0, 0, 0);
 }
 
-// Two weights rounded to the cache's type, and the same two as floats.  A
-// rounding is off by at most half a step of the type relative to the weight
-// (2^-8 in bf16, 2^-11 in fp16), no more than the output's own store; the sum
-// takes the rounded weights too, so that an error common to numerator and
-// denominator cancels.
-template <bool BF>
-__device__ __forceinline__ uint32_t pack_p(float a, float b, float& sum) {
-  if constexpr (BF) {
-    const uint32_t w = pack_bf16x2(a, b);
-    sum += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
-    return w;
-  } else {
-    const uint16_t x = f32_to_f16(a), y = f32_to_f16(b);
-    sum += f16_to_f32(x) + f16_to_f32(y);
-    return (uint32_t)x | ((uint32_t)y << 16);
-  }
-}
-
 template <bool BF>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return BF ? pack_bf16x2(a, b) : (uint32_t)f32_to_f16(a) | ((uint32_t)f32_to_f16(b) << 16);
 }
 
-// 0 V is no number where V is not finite: a value that some column of a tile
-// does not see would reach it through the product.  Where a step has keys that
-// some column does not see, its values are looked through: the first of these
-// takes such values out of the product, the second adds them to the columns that
-// see them (0.4 us of 10 for 1000 keys of one sequence, 1 of 40 and 2 of 82 for
-// shared prefixes of 8K and 64K, 2 of 39 for 4 chunks of 64 rows).
-// A word's two elements, zeros in the place of those that are not finite (the
-// exponent is all ones); adds to odd where there are any.
+// Two weights for the product with V, each as two values of the cache's type:
+// the weight rounded, and what that leaves, rounded.  The first alone is off by
+// half a step of the type (2^-8 of the weight in bf16, 2^-11 in fp16), as much
+// as the output's own store; the two by half a step of half a step (2^-16 and
+// 2^-22; in fp16 also by half the smallest step).  The sum takes the weights as
+// they are.  Twice the products with V: 64 sequences that share 8K keys 47 to
+// 48.5 us, 32 that share 64K 90 to 97; without shared keys no change.
 template <bool BF>
-__device__ __forceinline__ uint32_t finite(uint32_t w, uint32_t& odd) {
-  const uint32_t top = ((w & (BF ? 0x7f807f80u : 0x7c007c00u)) + (BF ? 0x00800080u : 0x04000400u)) & 0x80008000u;
-  odd |= top;
+__device__ __forceinline__ void split_p(float a, float b, uint32_t& hi, uint32_t& lo) {
+  hi = pack2<BF>(a, b);
+  if constexpr (BF) lo = pack2<BF>(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+  else lo = pack2<BF>(a - f16_to_f32((uint16_t)hi), b - f16_to_f32((uint16_t)(hi >> 16)));
+}
+
+// 0 V is no number where V is not finite: a value that a column does not see, or
+// whose weight's second part is zero, would reach it through the product.  So
+// every step's values are looked through; those that are not finite are taken
+// out of the product and added to the columns that see them.
+// The top bit of a word's elements that are not finite (the exponent is all ones).
+template <bool BF>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return ((w & (BF ? 0x7f807f80u : 0x7c007c00u)) + (BF ? 0x00800080u : 0x04000400u)) & 0x80008000u;
+}
+// The word with zeros in their place.
+template <bool BF>
+__device__ __forceinline__ uint32_t finite(uint32_t w) {
+  const uint32_t top = not_finite<BF>(w);
   return w & ~(top | (top - (top >> 15)));
 }
 // What the others add to the sums lo and hi.
@@ -361,7 +358,6 @@ template <int D>
 struct __attribute__((aligned(1024))) ManyShared {
   uint16_t kv[2][2 * kPagedWideStep * D];  // two steps' buffers: K, then V
   int64_t off[2][kPagedWideStep];
-  int lim[kWaves];      // keys that every column of a wave sees
   int odd[2][kWaves];   // whether a wave found values that are not finite in its rows of a step
 };
 
@@ -518,7 +514,6 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
       }
       if (again) load_k(cur, slot ^ 1);
       else if (have) load_k(next, slot ^ 1);
-      uint32_t odd = 0;
       if (!full) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -533,14 +528,8 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
 #pragma unroll
           for (int j = 0; j < VE / 2; ++j) vr[i][j] = row_there ? vr[i][j] : 0u;
         }
-        if (kb > lim_min) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < VE / 2; ++j) vr[i][j] = finite<BF>(vr[i][j], odd);
-        }
       }
-      uint4 p[NC];
+      uint4 p[NC], p2[NC];
 #pragma unroll
       for (int t = 0; t < NC; ++t) {
         // online softmax in the log2 domain; the scale (> 0) is one FMA ahead of exp2
@@ -561,10 +550,22 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i >> 2][i & 3], a.scale, -m_use));
-        p[t].x = pack_p<BF>(x[0], x[1], l[t]);
-        p[t].y = pack_p<BF>(x[2], x[3], l[t]);
-        p[t].z = pack_p<BF>(x[4], x[5], l[t]);
-        p[t].w = pack_p<BF>(x[6], x[7], l[t]);
+        split_p<BF>(x[0], x[1], p[t].x, p2[t].x);
+        split_p<BF>(x[2], x[3], p[t].y, p2[t].y);
+        split_p<BF>(x[4], x[5], p[t].z, p2[t].z);
+        split_p<BF>(x[6], x[7], p[t].w, p2[t].w);
+        l[t] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+      }
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < VE / 2; ++j) odd |= not_finite<BF>(vr[i][j]);
+      if (__builtin_expect(__any(odd != 0), 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int j = 0; j < VE / 2; ++j) vr[i][j] = finite<BF>(vr[i][j]);
       }
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
@@ -575,7 +576,10 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
         v.z = __builtin_amdgcn_perm(vr[5][j / 2], vr[4][j / 2], sel);
         v.w = __builtin_amdgcn_perm(vr[7][j / 2], vr[6][j / 2], sel);
 #pragma unroll
-        for (int t = 0; t < NC; ++t) acc[t][j] = mfma16<BF>(v, p[t], acc[t][j]);
+        for (int t = 0; t < NC; ++t) {
+          acc[t][j] = mfma16<BF>(v, p[t], acc[t][j]);
+          acc[t][j] = mfma16<BF>(v, p2[t], acc[t][j]);
+        }
       }
       if (__builtin_expect(__any(odd != 0), 0)) {
 #pragma unroll 1
@@ -820,25 +824,31 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
       const char* p = (i < LPW ? kbase : vbase) + (off < 0 ? 0 : off) + 16 * ((lane % CPR) ^ sw);
       load_to_lds(p, lds0 + (b * BUF + (i < LPW ? 0 : KEYS * D)) * 2 + inst * 1024);
     };
-    auto landed = [&](int b) {  // this wave's loads are there; rows that do not exist hold no value
+    // this wave's loads are there; zeros in the place of values whose rows do not
+    // exist and of those that are not finite, which sh.odd tells of
+    auto landed = [&](int b) {
       asm volatile("" ::: "memory");
       drain_vmem();
       asm volatile("" ::: "memory");
+      uint4* at = reinterpret_cast<uint4*>(sKV + b * BUF + KEYS * D + wid * LPW * 512 + lane * 8);
+      uint4 x[LPW];
+      uint32_t gone[LPW], odd = 0, change = 0;
 #pragma unroll
       for (int i = 0; i < LPW; ++i) {
-        const int inst = wid * LPW + i, r = inst * RPI + lane / CPR;
-        if (s_off[b][r] < 0)
-          *reinterpret_cast<uint4*>(sKV + b * BUF + KEYS * D + inst * 512 + lane * 8) = make_uint4(0, 0, 0, 0);
+        x[i] = at[i * 64];
+        gone[i] = s_off[b][(wid * LPW + i) * RPI + lane / CPR] < 0;
       }
-    };
-    // zeros in the place of this wave's values that are not finite
-    auto clean = [&](int b) {
-      uint32_t odd = 0;
 #pragma unroll
       for (int i = 0; i < LPW; ++i) {
-        uint4* p = reinterpret_cast<uint4*>(sKV + b * BUF + KEYS * D + (wid * LPW + i) * 512 + lane * 8);
-        const uint4 x = *p;
-        *p = make_uint4(finite<BF>(x.x, odd), finite<BF>(x.y, odd), finite<BF>(x.z, odd), finite<BF>(x.w, odd));
+        const uint32_t o = not_finite<BF>(x[i].x) | not_finite<BF>(x[i].y) | not_finite<BF>(x[i].z) | not_finite<BF>(x[i].w);
+        odd |= gone[i] ? 0 : o;
+        change |= gone[i] | o;
+      }
+      if (__builtin_expect(__any(change != 0), 0)) {
+#pragma unroll
+        for (int i = 0; i < LPW; ++i)
+          at[i * 64] = gone[i] ? make_uint4(0, 0, 0, 0)
+                               : make_uint4(finite<BF>(x[i].x), finite<BF>(x[i].y), finite<BF>(x[i].z), finite<BF>(x[i].w));
       }
       const bool any = __any(odd != 0);
       if (lane == 0) sh.odd[b][wid] = any;
@@ -864,14 +874,13 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) lim_min = min(lim_min, __shfl_xor(lim_min, o));
     lim_min = __builtin_amdgcn_readfirstlane(lim_min);
-    if (lane == 0) sh.lim[wid] = lim_min;
 
     f32x16_t acc[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i) acc[i] = f32x16_t{};
     float m = -INFINITY, l = 0.0f;
 
-    auto compute = [&](int b, int k, bool full, bool hidden, auto&& load) {
+    auto compute = [&](int b, int k, bool full, auto&& load) {
       const uint16_t* sK = sKV + b * BUF;
       const uint16_t* sV = sK + KEYS * D;
       f32x16_t sc[KT];
@@ -925,12 +934,15 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
       for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
-          uint4 p;
-          p.x = pack_p<BF>(sc[t][8 * hh], sc[t][8 * hh + 1], l);
-          p.y = pack_p<BF>(sc[t][8 * hh + 2], sc[t][8 * hh + 3], l);
-          p.z = pack_p<BF>(sc[t][8 * hh + 4], sc[t][8 * hh + 5], l);
-          p.w = pack_p<BF>(sc[t][8 * hh + 6], sc[t][8 * hh + 7], l);
+          uint4 p, p2;
+          split_p<BF>(sc[t][8 * hh], sc[t][8 * hh + 1], p.x, p2.x);
+          split_p<BF>(sc[t][8 * hh + 2], sc[t][8 * hh + 3], p.y, p2.y);
+          split_p<BF>(sc[t][8 * hh + 4], sc[t][8 * hh + 5], p.z, p2.z);
+          split_p<BF>(sc[t][8 * hh + 6], sc[t][8 * hh + 7], p.w, p2.w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) l += sc[t][8 * hh + i];
           const int k0 = 32 * (wk * KT + t) + 16 * hh + 4 * (gq >> 1) + (li >> 2);
+          uint4 x[ND];
 #pragma unroll
           for (int i = 0; i < ND; ++i) {
             const int d = 32 * i + 16 * (gq & 1) + 4 * (li & 3);
@@ -939,11 +951,14 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
                   sV + r * D + 8 * ((d >> 3) ^ swz_v<D>(r)) + (d & 4)));
             };
             const s16x8_t v = __builtin_shufflevector(tr(k0), tr(k0 + 8), 0, 1, 2, 3, 4, 5, 6, 7);
-            acc[i] = mfma32<BF>(__builtin_bit_cast(uint4, v), p, acc[i]);
+            x[i] = __builtin_bit_cast(uint4, v);
+            acc[i] = mfma32<BF>(x[i], p, acc[i]);
           }
+#pragma unroll
+          for (int i = 0; i < ND; ++i) acc[i] = mfma32<BF>(x[i], p2, acc[i]);
         }
       __builtin_amdgcn_s_setprio(0);
-      if (__builtin_expect(hidden && (sh.odd[b][0] | sh.odd[b][1] | sh.odd[b][2] | sh.odd[b][3]), 0)) {
+      if (__builtin_expect(sh.odd[b][0] | sh.odd[b][1] | sh.odd[b][2] | sh.odd[b][3], 0)) {
 #pragma unroll 1
         for (int kk = 32 * wk * KT; kk < 32 * (wk + 1) * KT; ++kk) {
           const int64_t off = s_off[b][kk];
@@ -967,12 +982,6 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
 
     landed(0);
     __syncthreads();
-    const int tile_lim = min(min(sh.lim[0], sh.lim[1]), min(sh.lim[2], sh.lim[3]));
-    auto hides = [&](int k) { return min(k + KEYS, kb) > tile_lim; };  // keys of a step from some column
-    if (hides(ka)) {
-      clean(0);
-      __syncthreads();
-    }
     int b = 0;
     for (int k = ka; k < kb; k += KEYS, b ^= 1) {
       const bool more = k + KEYS < kb;
@@ -986,14 +995,11 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
           if (more) issue(b ^ 1, i);
       } else {
         const bool full = k + KEYS <= lim_min && __all(s_off[b][lane] >= 0);
-        compute(b, k, full, hides(k), [&](int i) {
+        compute(b, k, full, [&](int i) {
           if (more) issue(b ^ 1, i);
         });
       }
-      if (more) {
-        landed(b ^ 1);
-        if (hides(k + KEYS)) clean(b ^ 1);
-      }
+      if (more) landed(b ^ 1);
       __syncthreads();
     }
     l += other32(l);

@@ -1,0 +1,76 @@
+"""What the softmax weights of attention over pages keep on their way through
+the product with V: sums that cancel show every bit that a weight has lost."""
+import numpy as np
+import pytest
+import torch
+
+import decode_ref as R
+from paper_2609_03905_amd import ea
+
+pytestmark = pytest.mark.gpu
+
+# A weight is held as two values of the cache's type, the second what the first
+# leaves: each rounding is off by at most half a step, so the two by half a step
+# of half a step.  The denominator is summed in f32.
+WEIGHT = {"bf16": 2.0 ** -16, "f16": 2.0 ** -22}
+
+
+def _tol(ref, info, dtype, d):
+    a, mag, vmax, n_keys = info
+    u = R.HALF[dtype]
+    soft = (WEIGHT[dtype] + 2 * (d + 8) * R.F * mag + 64 * R.F) * a + R.TINY[dtype] * n_keys * vmax
+    return u * np.abs(ref) + (1 + u) * soft + R.TINY[dtype]
+
+
+CASES = [
+    # lens, groups, n_q, hq, hkv, d: tiles of 16, 32, 64 and 128 columns, with and without shared keys
+    ([2, 3, 5, 9, 17, 40], [], 1, 4, 1, 128),
+    ([3, 6, 200], [], 4, 8, 2, 64),
+    ([40, 70], [], 12, 4, 1, 128),
+    ([33, 90], [], 30, 4, 1, 64),
+    ([20, 21, 22], [(0, 3, 16)], 5, 8, 2, 64),
+    ([40, 36, 39, 33], [(0, 4, 32)], 5, 8, 1, 128),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", CASES, ids=[f"n{len(c[0])}_g{len(c[1])}_q{c[2]}_h{c[3]}_{c[4]}_d{c[5]}" for c in CASES])
+def test_weights_keep_more_than_the_cache_type(case, dtype):
+    lens, groups, n_q, hq, hkv, d = case
+    page = 4
+    rng = np.random.default_rng(5)
+    held = [-(-n // page) for n in lens]
+    table = np.full((len(lens), max(held)), -1, np.int64)
+    ids = list(rng.permutation(sum(held)))
+    for s, n in enumerate(held):
+        table[s, :n] = [ids.pop() for _ in range(n)]
+    for first, last, keys in groups:
+        table[first:last, :keys // page] = table[first, :keys // page]
+    g = torch.Generator(device="cuda").manual_seed(6)
+    k, v = (torch.randn((sum(held), hkv, page, d), generator=g, device="cuda").to(R.TORCH[dtype]) for _ in range(2))
+    q = torch.randn((len(lens) * n_q, hq, d), generator=g, device="cuda").to(R.TORCH[dtype])
+    out = torch.empty((len(q), hq * d), device="cuda", dtype=R.TORCH[dtype])
+    starts = [n_q * i for i in range(len(lens) + 1)]
+    kw = {"group_start": R.i32([groups[0][0], groups[0][1]]), "group_shared": R.i32([groups[0][2]])} if groups else {}
+    ea.attention_paged(R.rel(q.view(len(q), -1)), R.pages_rel(k), R.pages_rel(v), R.rel(out), scale=d ** -0.5,
+                       table=R.i32(table), lengths=R.i32(lens), q_start=R.i32(starts), **kw)
+    ref, info = R.attention(R.f64(q), R.f64(k), R.f64(v), table, lens, page, starts, d ** -0.5)
+    R.check(R.f64(out.view(q.shape)), ref, _tol(ref, info, dtype, d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n_q,hq,d", [(1, 4, 128), (3, 8, 64), (12, 4, 128), (30, 4, 64)])
+def test_an_infinite_value_that_every_row_sees(n_q, hq, d, dtype):
+    """Equal weights, held without a rest: infinities come out as they are, the
+    other elements' means beside them."""
+    n, page = 256 + n_q, 16
+    k = torch.randn((20, 1, page, d), device="cuda").to(R.TORCH[dtype])
+    v = torch.ones_like(k)
+    v[2, 0, 3, 5], v[4, 0, 7, 6], v[1, 0, 0, d - 1] = float("inf"), -float("inf"), float("nan")
+    q = torch.zeros((n_q, hq * d), device="cuda", dtype=R.TORCH[dtype])
+    out = torch.empty_like(q)
+    ea.attention_paged(R.rel(q), R.pages_rel(k), R.pages_rel(v), R.rel(out), scale=1.0,
+                       table=R.i32([list(range(20))]), lengths=R.i32([n]), q_start=R.i32([0, n_q]))
+    got = R.f64(out).reshape(n_q, hq, d)
+    assert (got[..., 5] == np.inf).all() and (got[..., 6] == -np.inf).all() and np.isnan(got[..., d - 1]).all()
+    assert (got[..., [i for i in range(d) if i not in (5, 6, d - 1)]] == 1.0).all()
