@@ -51,6 +51,12 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr float kLazyMax = 8.0f;  // log2 of the largest P: the running max moves only past this
+// Weights are held 2^7 times as large in fp16: the largest of a walk is then from
+// 2^7 to 2^15, and half the smallest step, what a small one may lose, 2^-32 or less
+// of it (beside a weight of 1, 2^-26 would be nothing).  The factor is in
+// every partial result's O and l alike.
+template <bool BF>
+constexpr float kRaise = BF ? 0.0f : 7.0f;
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
@@ -75,8 +81,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // the weight rounded, and what that leaves, rounded.  The first alone is off by
 // half a step of the type (2^-8 of the weight in bf16, 2^-11 in fp16), as much
 // as the output's own store; the two by half a step of half a step (2^-16 and
-// 2^-22; in fp16 also by half the smallest step).  The sum takes the weights as
-// they are.  Twice the products with V: 64 sequences that share 8K keys 47 to
+// 2^-22; in fp16 also by half the smallest step, see kRaise).  The sum takes the
+// weights as they are.  Twice the products with V: 64 sequences that share 8K keys 47 to
 // 48.5 us, 32 that share 64K 90 to 97; without shared keys no change.
 template <bool BF>
 __device__ __forceinline__ void split_p(float a, float b, uint32_t& hi, uint32_t& lo) {
@@ -549,7 +555,7 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
         m[t] = m_new;
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i >> 2][i & 3], a.scale, -m_use));
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i >> 2][i & 3], a.scale, kRaise<BF> - m_use));
         split_p<BF>(x[0], x[1], p[t].x, p2[t].x);
         split_p<BF>(x[2], x[3], p[t].y, p2[t].y);
         split_p<BF>(x[4], x[5], p[t].z, p2[t].z);
@@ -928,7 +934,7 @@ __device__ __forceinline__ void walk_many(const PagedArgs& a, const PagedPass& p
 #pragma unroll
       for (int t = 0; t < KT; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sc[t][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][r], a.scale, -m_use));
+        for (int r = 0; r < 16; ++r) sc[t][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][r], a.scale, kRaise<BF> - m_use));
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int t = 0; t < KT; ++t)

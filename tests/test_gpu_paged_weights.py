@@ -11,14 +11,16 @@ pytestmark = pytest.mark.gpu
 
 # A weight is held as two values of the cache's type, the second what the first
 # leaves: each rounding is off by at most half a step, so the two by half a step
-# of half a step.  The denominator is summed in f32.
+# of half a step.  The denominator is summed in f32.  In fp16 the largest weight
+# of a row is 2^7 or more, so that half the smallest step is 2^-25 / 2^7 of it.
 WEIGHT = {"bf16": 2.0 ** -16, "f16": 2.0 ** -22}
+SMALLEST = {"bf16": 0.0, "f16": 2.0 ** -32}
 
 
 def _tol(ref, info, dtype, d):
     a, mag, vmax, n_keys = info
     u = R.HALF[dtype]
-    soft = (WEIGHT[dtype] + 2 * (d + 8) * R.F * mag + 64 * R.F) * a + R.TINY[dtype] * n_keys * vmax
+    soft = (WEIGHT[dtype] + 2 * (d + 8) * R.F * mag + 64 * R.F) * a + SMALLEST[dtype] * n_keys * vmax
     return u * np.abs(ref) + (1 + u) * soft + R.TINY[dtype]
 
 
@@ -74,3 +76,29 @@ def test_an_infinite_value_that_every_row_sees(n_q, hq, d, dtype):
     got = R.f64(out).reshape(n_q, hq, d)
     assert (got[..., 5] == np.inf).all() and (got[..., 6] == -np.inf).all() and np.isnan(got[..., d - 1]).all()
     assert (got[..., [i for i in range(d) if i not in (5, 6, d - 1)]] == 1.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,n_q,hq,d,shared", [(64, 1, 4, 128, 0), (900, 2, 8, 64, 0), (320, 12, 4, 128, 0),
+                                               (200, 30, 4, 64, 0), (320, 8, 8, 128, 256)])
+def test_many_small_weights_beside_large_ones(n, n_q, hq, d, shared, dtype):
+    """Every 32nd key's score is 26 octaves above the others', whose values make
+    the sum: weights of 2^-26 count, below what one fp16 number holds beside 1."""
+    page, seqs = 16, 2
+    held = -(-n // page)
+    key = torch.arange(held * page, device="cuda").view(held, 1, page, 1)
+    k = torch.zeros((held, 1, page, d), device="cuda")
+    k[..., 0:1] = 26.0 * (key % 32 == 0)
+    v = torch.where(key % 32 == 0, 0.0, 48000.0 + 1024 * (key % 7)).expand(-1, -1, -1, d).contiguous()
+    k, v = k.to(R.TORCH[dtype]), v.to(R.TORCH[dtype])
+    q = torch.zeros((seqs * n_q, hq, d), device="cuda", dtype=R.TORCH[dtype])
+    q[..., 0] = 1.0
+    table, starts = np.arange(held)[None].repeat(seqs, 0), [0, n_q, 2 * n_q]
+    out = torch.empty((len(q), hq * d), device="cuda", dtype=R.TORCH[dtype])
+    kw = {"group_start": R.i32([0, seqs]), "group_shared": R.i32([shared])} if shared else {}
+    ea.attention_paged(R.rel(q.view(len(q), -1)), R.pages_rel(k), R.pages_rel(v), R.rel(out), scale=float(np.log(2)),
+                       table=R.i32(table), lengths=R.i32([n] * seqs), q_start=R.i32(starts), **kw)
+    scale = float(np.float32(np.log(2)))
+    ref, info = R.attention(R.f64(q), R.f64(k), R.f64(v), table, [n] * seqs, page, starts, scale)
+    assert ref.min() > 0.01
+    R.check(R.f64(out.view(q.shape)), ref, _tol(ref, info, dtype, d))
