@@ -1089,9 +1089,10 @@ __global__ __launch_bounds__(W > kWaves ? W * 64 : kThreads) void paged_join_ker
   PagedSeg g = {};
   if (q.group >= 0) g = a.seg[q.group];
   for (int row = q.r0 + blockIdx.z; row < q.r1; row += gridDim.z) {
-    // parts of a walk, and the column of the first one's slot
+    // parts of a walk, and the column of the first one's slot; none where the
+    // row is not the segment's (query rows that do not ascend, under a group)
     auto range = [&](const PagedSeg& s, const PagedPass& p, int64_t* at) {
-      if (s.steps == 0) return 0;
+      if (s.steps == 0 || row < s.r0 || row >= s.r1) return 0;
       const int col = (row - s.r0) * a.g + hg, tile = col / p.cols;
       const int it = h * s.tiles + tile;
       const int64_t n = s.parts, from = s.step + (int64_t)it * s.steps;

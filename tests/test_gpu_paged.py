@@ -389,3 +389,17 @@ def test_what_a_row_does_not_see_may_be_anything(case):
         got[np.ix_(np.flatnonzero(sees), np.arange(hq)[heads])] = rows
         R.check(got, ref, tol)
         k[at][5] = float("nan")
+
+
+def test_query_rows_that_do_not_ascend_under_a_group():
+    """As without groups: rows of a sequence that are not its group's join no
+    part of the group's walk."""
+    lens, groups = [100, 200, 300], [(0, 3, 96)]
+    k, v, table = _batch(lens, None, groups, 16, 1, 64, "bf16", 24)
+    q = torch.randn((8, 4, 64), device="cuda").to(torch.bfloat16)
+    good = _run(q, k, v, table, lens, [0, 2, 5, 8], groups, 0.1).clone()
+    for bad in ([0, 8, 0, 8], [8, 0, 8, 0], [5, 0, 6, 6], [-5, 2 ** 31 - 1, -2 ** 31, 8], [3, 3, 3, 3]):
+        out = torch.full((9, 4 * 64), 7.0, device="cuda", dtype=torch.bfloat16)
+        _run(q, k, v, table, lens, bad, groups, 0.1, out=out[:8])
+        assert (out[8] == 7.0).all()
+        assert torch.equal(_run(q, k, v, table, lens, [0, 2, 5, 8], groups, 0.1), good)
