@@ -519,7 +519,10 @@ typedef struct ea_paged {
 /* q, out: [rows, Hq d] or [.., Hq, rows, d] (forms as ea_heads' q).  bf16 or
    f16, d 64 or 128; scores and sums in f32, weights as two values of the dtype
    (2^-16 of the weight in bf16, 2^-22 in f16) for the product with V; a table
-   row holds less than 2^31 - 1024 keys.  n_seq + n_group <= EA_PAGED_MAX_SEQ, rows * Hq < 2^31.
+   row holds less than 2^31 - 1024 keys.  n_seq + n_group <= EA_PAGED_MAX_SEQ, rows * Hq < 2^31;
+   a call whose tiles of query columns could take 2^31 steps over full table
+   rows is EA_ERR_UNSUPPORTED ((rows * Hq / 64 + (n_seq + n_group) * Hkv) *
+   (stride * page_size / 64 + 1) below 2^31 always passes).
    workspace: as ea_joinagg's (a zeroed counter area, left zero; the rest needs
    no initial value), of at least ea_attention_paged_workspace's bytes for these
    operands; asynchronous, never allocates, deterministic.  Errors: EA_ERR_ARG, EA_ERR_DTYPE,

@@ -354,6 +354,14 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
   if (b.n_group && (!b.group_start || !b.group_shared)) return fail(EA_ERR_ARG, "NULL group_start or group_shared");
   if (b.stride < 1) return fail(EA_ERR_ARG, "table stride %d", b.stride);
   if ((b.stride + (int64_t)1) * k->shape[2] > INT32_MAX - 1024) return fail(EA_ERR_UNSUPPORTED, "a table row of 2^31 keys or more");
+  // the steps of a pass are counted in 31 bits, whatever the lengths turn out to be
+  for (const PagedPass* s : {&p.shared, &p.own}) {
+    const int64_t keys = s->cols <= 32 ? kPagedStep : kPagedWideStep;
+    const int64_t steps = s->n ? (b.stride * k->shape[2] + keys - 1) / keys : 0;
+    if (s->tiles * steps > INT32_MAX)
+      return fail(EA_ERR_UNSUPPORTED, "%d tiles of query rows over table rows of %lld keys: 2^31 steps or more", s->tiles,
+                  (long long)(b.stride * k->shape[2]));
+  }
   if (!b.q_start && a.q.t < b.n_seq) return fail(EA_ERR_ARG, "%d query rows for %d sequences", a.q.t, b.n_seq);
   for (const ea_relation* r : {q, k, v})
     if (overlap(out, r)) return fail(EA_ERR_ARG, "out overlaps an input");

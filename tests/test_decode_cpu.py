@@ -281,3 +281,22 @@ def test_binding_checks_device_arrays():
 def test_a_workspace_of_the_host_is_refused():
     with pytest.raises(ea.EAError, match="workspace"):
         E._workspace(256, torch.zeros(512, dtype=torch.uint8), None)
+
+
+def test_paged_refuses_more_steps_than_it_counts():
+    """Tiles of 128 columns times steps of 64 keys, and of 16 times 128, 2^31 or
+    more of them; one page less passes that check and fails for its workspace."""
+    # 65536 rows of 4 heads a key-value head: (262144 / 128 + 5) * 2 tiles
+    big = dict(q=fake([65536, 1024]), out=fake([65536, 1024]), start=256, n=4096)
+    most = (2 ** 31 - 1) // ((262144 // 128 + 5) * 2) * 64 // 16
+    assert paged(stride=most + 4, **big) == UNSUPPORTED and paged(stride=most, **big) == CAPACITY
+    # 5 sequences of 4 columns: (20 / 16 + 5) * 2 tiles over 2^31 keys are within
+    assert paged(stride=2 ** 27 - 128, n=4096) == CAPACITY
+    # 2000 sequences over 8 heads, groups among them
+    q = fake([2000, 4096])
+    few = dict(q=q, out=fake([2000, 4096]), k=cache(30, 8, 16, 128), v=cache(30, 8, 16, 128), n_seq=2000, n=4096)
+    tiles = (8000 // 16 + 2000) * 8
+    most = (2 ** 31 - 1) // tiles * 128 // 16
+    assert paged(stride=most + 8, **few) == UNSUPPORTED and paged(stride=most, **few) == CAPACITY
+    # 40 groups' tiles of 128 columns, in steps of 64 keys
+    assert paged(stride=most // 2, n_group=40, gs=256, gk=256, **few) == CAPACITY
