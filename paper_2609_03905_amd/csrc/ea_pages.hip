@@ -32,7 +32,7 @@ constexpr int kCopyThreads = 256, kCopyWgs = 2048;
 
 // Workspace words: the copies a bookkeeping kernel asks for.
 constexpr int kWorkCount = 0;   // pages to move
-constexpr int kWorkUsed = 1;    // compact: pages in use
+constexpr int kWorkUsed = 1;    // compact: pages in use; -1: the state goes through as it came
 constexpr int kWorkLists = 16;  // then source pages, destinations and rows
 
 constexpr int kBlock = 4 * kMetaThreads;  // pages that a workgroup looks at together
@@ -479,8 +479,17 @@ __global__ __launch_bounds__(kMetaThreads) void compact_kernel(const PagesArgs a
   int* src = a.work + kWorkLists;
   int* dst = src + a.n_pages;
   int* rank_of = dst + a.n_pages;
-  int all_free;
+  int all_free, bad = 0;
+  for (int s = tid; s < a.n_seq; s += kMetaThreads) bad |= a.len[s] < 0 || a.len[s] > (int64_t)a.stride * a.page_size;
   const int before = free_before(a.refs, a.n_pages, s_wave, &all_free);
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) {
+      a.work[kWorkCount] = 0;
+      a.work[kWorkUsed] = -1;
+    }
+    set_status(a, EA_PAGES_TOO_LONG, all_free);
+    return;
+  }
   const int n_used = a.n_pages - all_free;
   if (tid == 0) s_moves = 0;
   __syncthreads();
@@ -542,15 +551,18 @@ __global__ __launch_bounds__(kCopyThreads) void move_kernel(const PagesArgs a, c
     for (int64_t j = first; j < cells; j += step) {
       const int s = div_fast((int)j, a.row), at = (int)j - s * a.stride;
       int pg = a.table[j];
-      // (a page that no count calls used was not moved: its entry stays)
-      if (pg >= n_used && pg < a.n_pages && a.refs[pg] > 0) pg = dst[more[pg]];
-      a.out_table[j] = at >= held(max(a.len[s], 0), a.page_size) ? -1 : pg;
+      if (n_used >= 0) {
+        // (a page that no count calls used was not moved: its entry stays)
+        if (pg >= n_used && pg < a.n_pages && a.refs[pg] > 0) pg = dst[more[pg]];
+        if (at >= held(a.len[s], a.page_size)) pg = -1;
+      }
+      a.out_table[j] = pg;
     }
     if (a.out_refs != a.refs)
       for (int64_t p = first; p < a.n_pages; p += step) {
         // places before n_used that were free get the moved pages' counts
         const int n = a.refs[p];
-        if (n > 0 || p >= n_used) a.out_refs[p] = p < n_used ? n : 0;
+        if (n > 0 || p >= n_used) a.out_refs[p] = p < n_used || n_used < 0 ? n : 0;
       }
     for (int64_t r = first; a.out_refs != a.refs && r < count; r += step)
       a.out_refs[dst[r]] = a.refs[src[count - 1 - r]];

@@ -276,3 +276,26 @@ def test_positions_alone_and_nothing_wanted():
     assert pos.tolist() == [0, 1, 0, 1, 2, 0] and st.tolist() == [ea.PAGES_OK, 7]
     ea.pages_extend(t, ln, rf, R.i32([3, 1, 0]), page_size=4, status=st)
     assert ln.tolist() == [5, 1, 3] and t[0, :2].tolist() == [0, 2] and t[1, 0] == 3 and st.tolist() == [0, 5]
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("length", [-1, -2 ** 31, 3 * 4 + 1, 2 ** 31 - 1, 2 ** 31 - 4])
+def test_compact_of_lengths_that_no_row_holds(length, in_place):
+    """Nothing is done: table, counts and pages stay as they came, entries behind
+    the sequences' pages too."""
+    data = torch.randn((2, 9, 1, 4, 32), device="cuda").to(torch.bfloat16)
+    table = R.i32([[7, 8, 5], [6, 3, 11]])
+    lengths, refs, status = R.i32([9, length]), R.i32([0, 0, 0, 1, 0, 1, 1, 1, 1]), R.i32([9, 9])
+    kept = [z.clone() for z in (data, table, lengths, refs)]
+    t, r = (table, refs) if in_place else (torch.full_like(table, 5), torch.full_like(refs, 5))
+    ea.pages_compact([R.pages_rel(data)], table, lengths, refs, out_table=t, out_refs=r, status=status)
+    assert status.tolist() == [ea.PAGES_TOO_LONG, 4]
+    for got, want in zip((data, table, lengths, refs), kept):
+        assert torch.equal(got.view(torch.uint8) if got.dtype == torch.bfloat16 else got,
+                           want.view(torch.uint8) if want.dtype == torch.bfloat16 else want)
+    assert torch.equal(t, kept[1]) and torch.equal(r, kept[3])
+    # with a length that the row holds, the same call moves the pages together
+    lengths[1] = 8
+    ea.pages_compact([R.pages_rel(data)], table, lengths, refs, out_table=t, out_refs=r, status=status)
+    assert status.tolist() == [ea.PAGES_OK, 4] and r.tolist() == [1] * 5 + [0] * 4
+    assert t.tolist() == [[2, 4, 0], [1, 3, -1]]  # pages 5, 6, 7, 8 to 0, 1, 2, 4
