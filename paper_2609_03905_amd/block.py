@@ -167,9 +167,14 @@ class LlamaBlockShare:
 class LlamaBlockDecode:
     """The newest tokens of the cache's sequences through a share's weights:
     ``rows`` tokens a step (x: [rows, hidden], sequence by sequence), their
-    slots and positions from cache.extend."""
+    slots and positions from cache.extend, at most ``groups`` shared prefixes
+    (None: as many as sequences).  The calls' plans are made and their workspace
+    is allocated here, so a step can be captured at once, and steps of several
+    decoders may overlap in time (steps of one may not: its activations and its
+    workspace are one step's)."""
 
-    def __init__(self, share: LlamaBlockShare, cache: KVCache, rows: int, layer: int = 0, device="cuda"):
+    def __init__(self, share: LlamaBlockShare, cache: KVCache, rows: int, layer: int = 0, device="cuda",
+                 groups: int | None = None):
         self.share, self.cache, self.rows, self.layer = share, cache, rows, layer
         s, block = share, share.block
         pt, ph, pf = _splits(rows, block), _splits(s.hidden, block), _splits(s.ffn, block)
@@ -184,21 +189,42 @@ class LlamaBlockDecode:
         self.h2 = R((rows, s.hidden), [pt, ph])
         self.a = R((rows, s.ffn), [pt, pf])
         self.y = R((rows, s.hidden), [pt, ph])
+        S = ea.AGG_SUM
+        self._joinaggs = {
+            "rmsnorm1": (("tc,c->tc", ea.OP_RMSNORM, S, [self.x, s.n1], self.h1), dict(eps=s.eps)),
+            "qkv_gemm": (("tj,jk->tk", ea.JOIN_MUL, S, [self.h1, s.wqkv], self.qkv), {}),
+            "o_gemm_residual": (("tj,jk->tk", ea.JOIN_MUL, S, [self.attn, s.wo], self.x2), dict(residual=self.x)),
+            "rmsnorm2": (("tc,c->tc", ea.OP_RMSNORM, S, [self.x2, s.n2], self.h2), dict(eps=s.eps)),
+            "swiglu_gemm": (("tj,jk,jk->tk", ea.OP_SWIGLU, S, [self.h2, s.wg, s.wu], self.a), {}),
+            "down_gemm_residual": (("tj,jk->tk", ea.JOIN_MUL, S, [self.a, s.wd], self.y), dict(residual=self.x2)),
+        }
+        n_seq = cache.lengths.numel()
+        most = max(0, min(n_seq if groups is None else groups, ea.PAGED_MAX_SEQ - n_seq))
+        # (how the columns are tiled depends on the number of groups: fewer may need more)
+        need = [ea.attention_paged_workspace(self.q, cache.k[layer], n_seq, g) for g in range(most + 1)]
+        if self.x.data.is_cuda:
+            need += [ea.joinagg_workspace(*args, **kw) for args, kw in self._joinaggs.values()]
+        self.workspace = ea.new_workspace(max(need), device=device)
 
     def stages(self, slots, positions, q_start=None, group_start=None, group_shared=None):
-        J, S, s, c = ea.joinagg, ea.AGG_SUM, self.share, self.cache
+        s, c, ws = self.share, self.cache, self.workspace
         k, v = c.k[self.layer], c.v[self.layer]
+
+        def joinagg(name):
+            args, kw = self._joinaggs[name]
+            return name, lambda: ea.joinagg(*args, workspace=ws, **kw)
+
         return [
-            ("rmsnorm1", lambda: J("tc,c->tc", ea.OP_RMSNORM, S, [self.x, s.n1], self.h1, eps=s.eps)),
-            ("qkv_gemm", lambda: J("tj,jk->tk", ea.JOIN_MUL, S, [self.h1, s.wqkv], self.qkv)),
+            joinagg("rmsnorm1"),
+            joinagg("qkv_gemm"),
             ("heads", lambda: ea.heads(self.qkv, self.q, k, v, slots=slots, **s.head_options(positions))),
             ("attention", lambda: ea.attention_paged(self.q, k, v, self.attn, scale=s.scale, table=c.table,
                                                      lengths=c.lengths, q_start=q_start, group_start=group_start,
-                                                     group_shared=group_shared)),
-            ("o_gemm_residual", lambda: J("tj,jk->tk", ea.JOIN_MUL, S, [self.attn, s.wo], self.x2, residual=self.x)),
-            ("rmsnorm2", lambda: J("tc,c->tc", ea.OP_RMSNORM, S, [self.x2, s.n2], self.h2, eps=s.eps)),
-            ("swiglu_gemm", lambda: J("tj,jk,jk->tk", ea.OP_SWIGLU, S, [self.h2, s.wg, s.wu], self.a)),
-            ("down_gemm_residual", lambda: J("tj,jk->tk", ea.JOIN_MUL, S, [self.a, s.wd], self.y, residual=self.x2)),
+                                                     group_shared=group_shared, workspace=ws)),
+            joinagg("o_gemm_residual"),
+            joinagg("rmsnorm2"),
+            joinagg("swiglu_gemm"),
+            joinagg("down_gemm_residual"),
         ]
 
     def step(self, slots, positions, **batch):

@@ -300,3 +300,23 @@ def test_paged_refuses_more_steps_than_it_counts():
     assert paged(stride=most + 8, **few) == UNSUPPORTED and paged(stride=most, **few) == CAPACITY
     # 40 groups' tiles of 128 columns, in steps of 64 keys
     assert paged(stride=most // 2, n_group=40, gs=256, gk=256, **few) == CAPACITY
+
+
+def test_decoders_have_workspaces_of_their_own(monkeypatch):
+    """Every call of a step that takes a workspace is given the decoder's, which
+    holds what attention needs for any number of groups."""
+    from paper_2609_03905_amd.block import LlamaBlockDecode, LlamaBlockShare
+    from paper_2609_03905_amd.cache import KVCache
+
+    share = LlamaBlockShare(16, 256, 2, 128, 256, block=128, heads_kv=1, device="meta")
+    c = KVCache(1, 20, 1, 16, 128, 6, 3, device="meta")
+    decoders = [LlamaBlockDecode(share, c, 6, device="meta") for _ in range(2)]
+    assert decoders[0].workspace is not decoders[1].workspace
+    for d in decoders:
+        assert all(ea.attention_paged_workspace(d.q, c.k[0], 6, g) <= d.workspace.numel() for g in range(7))
+    seen = []
+    for name in ("joinagg", "attention_paged"):
+        monkeypatch.setattr(E, name, lambda *a, **kw: seen.append(kw.get("workspace")))
+    monkeypatch.setattr(E, "heads", lambda *a, **kw: None)
+    assert decoders[0].step(None, None) is decoders[0].y
+    assert len(seen) == 7 and all(w is decoders[0].workspace for w in seen)

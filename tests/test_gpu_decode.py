@@ -143,3 +143,48 @@ def test_two_caches_captured_grow_as_by_eager_calls():
             for x, y in ((c.table, e.table), (c.lengths, e.lengths), (c.refs, e.refs), (c.status, e.status)):
                 assert torch.equal(x, y)
         assert caches[0].status.tolist()[0] == ea.PAGES_OK
+
+
+def test_two_decoders_captured_step_as_by_eager_calls():
+    """Steps captured one after the other on one stream, without a call before,
+    and replayed on two: the same bits as eager steps of a third decoder."""
+    w, tokens = _weights(4)
+    share = _share(PROMPT, w, tokens(PROMPT))
+    share.forward()
+    n, long = 5, [300, 20, 170, 1, 64]
+    caches, decoders, graphs, batches = [], [], [], []
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for i in range(2):
+        c = KVCache(1, 80, HEADS_KV, 16, 128, n, 24)
+        c.k[0].bytes().view(torch.bfloat16).normal_(generator=g)
+        c.v[0].bytes().view(torch.bfloat16).normal_(generator=g)
+        slots, positions = c.extend(R.i32([x + 30 * i for x in long]), sum(long) + 30 * n * i)
+        caches.append(c)
+        # the second one's groups share nothing, but take the other walk
+        batches.append({} if i == 0 else dict(group_start=R.i32([0, 2, 5]), group_shared=R.i32([0, 0])))
+        decoders.append(LlamaBlockDecode(share, c, n))
+    one = [c.extend(R.i32([1] * n), n) for c in caches]
+    eager = [LlamaBlockDecode(share, c, n) for c in caches]
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    for d, (slots, positions), b in zip(decoders, one, batches):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            d.step(slots, positions, **b)
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(5):
+        xs = [tokens(n) for _ in graphs]
+        for d, e, x in zip(decoders, eager, xs):
+            _set(d.x, x)
+            _set(e.x, x)
+            d.y.data.fill_(0xFF)
+        torch.cuda.synchronize()
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for d, e, (slots, positions), b in zip(decoders, eager, one, batches):
+            want = R.unblocked(e.step(slots, positions, **b))
+            assert torch.isfinite(want.float()).all() and torch.equal(R.unblocked(d.y), want)
+    assert not decoders[0].workspace[:ea.WS_COUNTER_BYTES].any()
