@@ -51,8 +51,10 @@ class LlamaBlockShare:
         self.heads_kv, self.seq_ends = heads_kv, None if seq_ends is None else [int(e) for e in seq_ends]
         self.inv_freq, self.interleaved, self.qk_norm = inv_freq, interleaved, qk_norm
         self.positions = None  # the token's index in its sequence (None: in the relation)
-        if self.seq_ends is not None:
+        if self.seq_ends and inv_freq is not None:
             lens = [e - s for s, e in zip([0] + self.seq_ends[:-1], self.seq_ends)]
+            if min(lens) < 1 or self.seq_ends[-1] != t:
+                raise ea.EAError(ea.ERR_ARG, f"sequence ends {self.seq_ends} do not ascend to {t}")
             self.positions = torch.cat([torch.arange(n, dtype=torch.int32) for n in lens]).to(device)
         self.block = block
         self.eps = eps

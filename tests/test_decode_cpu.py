@@ -320,3 +320,17 @@ def test_decoders_have_workspaces_of_their_own(monkeypatch):
     monkeypatch.setattr(E, "heads", lambda *a, **kw: None)
     assert decoders[0].step(None, None) is decoders[0].y
     assert len(seen) == 7 and all(w is decoders[0].workspace for w in seen)
+
+
+def test_share_of_packed_sequences_without_frequencies():
+    """Positions are needed where heads are rotated: no ends are one sequence, as
+    for attention, and ends that do not ascend are refused there as ever."""
+    from paper_2609_03905_amd.block import LlamaBlockShare
+
+    make = lambda **kw: LlamaBlockShare(16, 256, 2, 128, 256, block=128, heads_kv=1, device="meta", **kw)
+    freq = torch.ones(64)
+    assert make(seq_ends=[]).positions is None and make(seq_ends=[], inv_freq=freq).positions is None
+    assert make(seq_ends=[5, 3, 16]).seq_ends == [5, 3, 16]
+    assert make(seq_ends=[4, 16], inv_freq=freq).positions.shape == (16,)
+    for ends in ([5, 3, 16], [4, 4, 16], [0, 16], [4], [4, 17]):
+        _raises(ARG, lambda: make(seq_ends=ends, inv_freq=freq))
