@@ -139,6 +139,8 @@ def _partition_args(partition):
 
 def _points(s) -> array.array:
     """Split points as 64-bit integers (a cache has one a page: tens of thousands)."""
+    if not isinstance(s, (list, tuple, range)):
+        s = list(s)  # an array reads bytes as they lie, and what it takes of an iterator is gone
     try:
         return array.array("q", s)
     except TypeError:

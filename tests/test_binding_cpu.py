@@ -82,3 +82,17 @@ def test_a_missing_or_small_workspace_is_looked_up(monkeypatch, code, given):
 def test_a_bad_argument_beside_a_workspace_is_raised(monkeypatch):
     calls, raised = _calls(monkeypatch, [-1], "joinagg", workspace=torch.zeros(512, dtype=torch.uint8))
     assert raised == -1 and len(calls) == 1
+
+
+def test_split_points_of_any_iterable():
+    """Each dim's points may be any iterable of numbers, a generator of floats or
+    bytes among them."""
+    import numpy as np
+
+    want = [[0, 2, 4], [0, 5]]
+    make = lambda *part: ea.Relation((4, 5), "f32", part, allocate=False).partition
+    assert make(range(0, 5, 2), (0, 5)) == want
+    assert make((float(x) for x in (0, 2, 4)), iter([0.0, 5.0])) == want
+    assert make(np.array([0.0, 2.0, 4.0]), np.array([0, 5], np.uint8)) == want
+    assert make(b"\x00\x02\x04", bytearray([0, 5])) == want
+    assert make("024", map(str, (0, 5))) == want
