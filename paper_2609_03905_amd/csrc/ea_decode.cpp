@@ -514,7 +514,8 @@ int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, i
     return fail(EA_ERR_ARG, "slots or positions overlap another array");
   if (overlap(add, a.n_seq * (int64_t)4, a.out_refs, a.n_pages * (int64_t)4) ||
       overlap(add, a.n_seq * (int64_t)4, a.out_table, (int64_t)a.n_seq * a.stride * 4) ||
-      overlap(add, a.n_seq * (int64_t)4, a.out_len, a.n_seq * (int64_t)4))
+      overlap(add, a.n_seq * (int64_t)4, a.out_len, a.n_seq * (int64_t)4) ||
+      overlap(add, a.n_seq * (int64_t)4, a.status, 8))
     return fail(EA_ERR_ARG, "add overlaps an output");
   if ((e = check_pages_ws(state, workspace, ws_bytes, &a, &c))) return e;
   a.add = add;

@@ -334,3 +334,8 @@ def test_share_of_packed_sequences_without_frequencies():
     assert make(seq_ends=[4, 16], inv_freq=freq).positions.shape == (16,)
     for ends in ([5, 3, 16], [4, 4, 16], [0, 16], [4], [4, 17]):
         _raises(ARG, lambda: make(seq_ends=ends, inv_freq=freq))
+
+
+def test_extend_refuses_counts_over_its_status():
+    assert extend(add=A + (6 << 20)) == ARG and extend(add=A + (6 << 20) - 12) == ARG
+    assert extend(add=A + (6 << 20) + 8, n=100) == CAPACITY
