@@ -469,7 +469,8 @@ typedef struct ea_heads_params {
    [pages, Hkv, page_size, d], one block a page.  Partitions: equal blocks (the
    last may be shorter), columns at multiples of d, d never split
    (EA_ERR_UNSUPPORTED otherwise).  wq, wk: norm weights [d], both or neither,
-   of any dtype.  All others of one dtype; memory must not overlap.
+   of any dtype.  All others of one dtype; outputs must not overlap anything
+   else, the parameters' arrays among it.
    Asynchronous on `stream`: no plan, no workspace, never allocates.
    Errors: EA_ERR_ARG, EA_ERR_DTYPE, EA_ERR_UNSUPPORTED, EA_ERR_HIP. */
 int ea_heads(const ea_relation* qkv, const ea_relation* wq, const ea_relation* wk, ea_relation* q, ea_relation* k,
@@ -525,7 +526,8 @@ typedef struct ea_paged {
    (stride * page_size / 64 + 1) below 2^31 always passes).
    workspace: as ea_joinagg's (a zeroed counter area, left zero; the rest needs
    no initial value), of at least ea_attention_paged_workspace's bytes for these
-   operands; asynchronous, never allocates, deterministic.  Errors: EA_ERR_ARG, EA_ERR_DTYPE,
+   operands; asynchronous, never allocates, deterministic.  out and the workspace
+   must not overlap anything else.  Errors: EA_ERR_ARG, EA_ERR_DTYPE,
    EA_ERR_UNSUPPORTED, EA_ERR_CAPACITY, EA_ERR_HIP. */
 int ea_attention_paged_workspace(const ea_relation* q, const ea_relation* k, const ea_paged* batch, int64_t* ws_bytes);
 int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_relation* v, ea_relation* out,
@@ -576,8 +578,8 @@ int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages*
    (out_lengths is not written); out_table and out_refs may be table and refs. */
 int ea_pages_compact(int32_t n_cache, ea_relation* const* caches, const ea_pages* state, void* workspace,
                      int64_t ws_bytes, void* stream);
-/* Workspace of the three: 256-byte aligned, behind its counter area (which
-   stays untouched) no initial value is needed. */
+/* Workspace of the three: 256-byte aligned, over no argument; behind its
+   counter area (which stays untouched) no initial value is needed. */
 int ea_pages_workspace(int32_t n_seq, int32_t n_pages, int64_t* ws_bytes);
 
 /* ---- plan cache --------------------------------------------------------- */

@@ -6,6 +6,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 using namespace ea;
 
@@ -81,6 +82,19 @@ bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
 }
 bool overlap(const ea_relation* a, const ea_relation* b) {
   return a && b && overlap(a->data, a->nbytes, b->data, b->nbytes);
+}
+
+// A stretch of device memory, none where p is null.
+struct Span {
+  const void* p;
+  int64_t n;
+};
+Span span(const ea_relation* r) { return {r ? r->data : nullptr, r ? r->nbytes : 0}; }
+Span ints(const int32_t* p, int64_t n) { return {p, n * 4}; }
+bool overlap(const Span& a, std::initializer_list<Span> others) {
+  for (const Span& b : others)
+    if (overlap(a.p, a.n, b.p, b.n)) return true;
+  return false;
 }
 
 // Equal dtype, shape and partition (layout ids may differ where these do not).
@@ -159,6 +173,9 @@ int ea_heads(const ea_relation* qkv, const ea_relation* wq, const ea_relation* w
       if (overlap(out[i], r)) return fail(EA_ERR_ARG, "an output overlaps an input");
     for (int j = 0; j < i; ++j)
       if (overlap(out[i], out[j])) return fail(EA_ERR_ARG, "q, k and v overlap");
+    if (overlap(span(out[i]), {Span{params->inv_freq, params->rotary * (int64_t)2}, ints(params->positions, a.x.t),
+                               ints(params->slots, a.x.t)}))
+      return fail(EA_ERR_ARG, "an output overlaps inv_freq, positions or slots");
   }
   a.px = (const char*)qkv->data;
   a.pq = (char*)q->data;
@@ -216,6 +233,8 @@ int ea_heads_backward(const ea_relation* qkv, const ea_relation* wq, const ea_re
       if (overlap(out[i], r)) return fail(EA_ERR_ARG, "an output overlaps an input");
     for (int j = 0; j < i; ++j)
       if (overlap(out[i], out[j])) return fail(EA_ERR_ARG, "outputs overlap");
+    if (overlap(span(out[i]), {Span{params->inv_freq, params->rotary * (int64_t)2}, ints(params->positions, a.x.t)}))
+      return fail(EA_ERR_ARG, "an output overlaps inv_freq or positions");
   }
   if (dwq || dwk) {
     int64_t need;
@@ -223,6 +242,10 @@ int ea_heads_backward(const ea_relation* qkv, const ea_relation* wq, const ea_re
     if (!workspace || (uintptr_t)workspace % 256) return fail(EA_ERR_ARG, "workspace missing or not 256-byte aligned");
     if (ws_bytes < need)
       return fail(EA_ERR_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
+    if (overlap(Span{workspace, need},
+                {span(qkv), span(wq), span(wk), span(dq), span(dk), span(dv), span(dqkv), span(dwq), span(dwk),
+                 Span{params->inv_freq, params->rotary * (int64_t)2}, ints(params->positions, a.x.t)}))
+      return fail(EA_ERR_ARG, "the workspace overlaps an argument");
     a.part = (float*)((char*)workspace + kWsCounterBytes);
   }
   a.px = (const char*)qkv->data;
@@ -369,6 +392,14 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
   if (!workspace || (uintptr_t)workspace % 256) return fail(EA_ERR_ARG, "workspace missing or not 256-byte aligned");
   if (ws_bytes < need)
     return fail(EA_ERR_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
+  for (const Span& w : {span(out), Span{workspace, need}})
+    if (overlap(w, {ints(b.q_start, b.n_seq + (int64_t)1), ints(b.lengths, b.n_seq),
+                    ints(b.table, b.n_seq * (int64_t)b.stride),
+                    b.n_group ? ints(b.group_start, b.n_group + (int64_t)1) : Span{nullptr, 0},
+                    b.n_group ? ints(b.group_shared, b.n_group) : Span{nullptr, 0}}))
+      return fail(EA_ERR_ARG, "out or the workspace overlaps an array of the batch");
+  if (overlap(Span{workspace, need}, {span(q), span(k), span(v), span(out)}))
+    return fail(EA_ERR_ARG, "the workspace overlaps a relation");
   a.pq = (const char*)q->data;
   a.pk = (const char*)k->data;
   a.pv = (const char*)v->data;
@@ -448,7 +479,7 @@ bool meets_state(const ea_pages* s, const void* p, int64_t bytes) {
          overlap(p, bytes, s->out_refs, nr) || overlap(p, bytes, s->status, 8);
 }
 
-int check_caches(int32_t n, ea_relation* const* caches, const ea_pages* p, PagesCopyArgs* c) {
+int check_caches(int32_t n, ea_relation* const* caches, const ea_pages* p, const int32_t* parent, PagesCopyArgs* c) {
   if (n < 0 || n > kPagesMaxCaches || (n && !caches))
     return fail(EA_ERR_ARG, "n_cache %d outside [0, %d] or NULL caches", n, kPagesMaxCaches);
   c->n_cache = n;
@@ -465,6 +496,8 @@ int check_caches(int32_t n, ea_relation* const* caches, const ea_pages* p, Pages
     if (row % 16) return fail(EA_ERR_UNSUPPORTED, "cache rows of %lld bytes, no multiple of 16", (long long)row);
     for (int j = 0; j < i; ++j)
       if (overlap(r, caches[j])) return fail(EA_ERR_ARG, "caches overlap");
+    if (meets_state(p, r->data, r->nbytes) || overlap(span(r), {ints(parent, p->n_seq)}))
+      return fail(EA_ERR_ARG, "a cache overlaps an array of the state");
     if (r->shape[q + 1] * p->page_size * row > INT32_MAX)
       return fail(EA_ERR_UNSUPPORTED, "a page of 2 GiB or more");
     c->c[i] = {(char*)r->data, page_bytes(r) * p->n_pages, page_bytes(r), row, (int32_t)(q ? r->shape[0] : 1),
@@ -479,11 +512,15 @@ int64_t pages_bytes(int32_t n_seq, int32_t n_pages) {
   return kWsCounterBytes + (16 + lists) * 4;
 }
 
-int check_pages_ws(const ea_pages* p, void* ws, int64_t bytes, PagesArgs* a, PagesCopyArgs* c) {
+int check_pages_ws(const ea_pages* p, std::initializer_list<Span> more, int32_t n_cache, ea_relation* const* caches,
+                   void* ws, int64_t bytes, PagesArgs* a, PagesCopyArgs* c) {
   if (!ws || (uintptr_t)ws % 256) return fail(EA_ERR_ARG, "workspace missing or not 256-byte aligned");
   const int64_t need = pages_bytes(p->n_seq, p->n_pages);
   if (bytes < need)
     return fail(EA_ERR_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)bytes, (long long)need);
+  bool meets = meets_state(p, ws, need) || overlap(Span{ws, need}, more);
+  for (int i = 0; i < n_cache; ++i) meets = meets || overlap(Span{ws, need}, {span(caches[i])});
+  if (meets) return fail(EA_ERR_ARG, "the workspace overlaps an argument");
   a->work = (int32_t*)((char*)ws + kWsCounterBytes);
   c->work = a->work;
   return EA_OK;
@@ -517,7 +554,9 @@ int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, i
       overlap(add, a.n_seq * (int64_t)4, a.out_len, a.n_seq * (int64_t)4) ||
       overlap(add, a.n_seq * (int64_t)4, a.status, 8))
     return fail(EA_ERR_ARG, "add overlaps an output");
-  if ((e = check_pages_ws(state, workspace, ws_bytes, &a, &c))) return e;
+  if ((e = check_pages_ws(state, {ints(add, a.n_seq), ints(slots, n_tokens), ints(positions, n_tokens)}, 0, nullptr,
+                          workspace, ws_bytes, &a, &c)))
+    return e;
   a.add = add;
   a.slots = slots;
   a.pos = positions;
@@ -532,7 +571,7 @@ int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages*
   PagesCopyArgs c{};
   int e = check_pages(state, &a);
   if (e) return e;
-  if ((e = check_caches(n_cache, caches, state, &c))) return e;
+  if ((e = check_caches(n_cache, caches, state, parent, &c))) return e;
   if (!parent || !state->out_lengths) return fail(EA_ERR_ARG, "NULL parent or out_lengths");
   if (a.out_table == a.table || a.out_len == a.len || a.out_refs == a.refs)
     return fail(EA_ERR_ARG, "select needs output arrays of their own");
@@ -540,7 +579,7 @@ int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages*
   if (overlap(parent, np, a.out_table, np * a.stride) || overlap(parent, np, a.out_len, np) ||
       overlap(parent, np, a.out_refs, a.n_pages * (int64_t)4) || overlap(parent, np, a.status, 8))
     return fail(EA_ERR_ARG, "parent overlaps an output");
-  if ((e = check_pages_ws(state, workspace, ws_bytes, &a, &c))) return e;
+  if ((e = check_pages_ws(state, {ints(parent, a.n_seq)}, n_cache, caches, workspace, ws_bytes, &a, &c))) return e;
   a.parent = parent;
   EA_HIP_TRY(launch_pages_select(a, c, (hipStream_t)stream));
   return ok();
@@ -552,8 +591,8 @@ int ea_pages_compact(int32_t n_cache, ea_relation* const* caches, const ea_pages
   PagesCopyArgs c{};
   int e = check_pages(state, &a);
   if (e) return e;
-  if ((e = check_caches(n_cache, caches, state, &c))) return e;
-  if ((e = check_pages_ws(state, workspace, ws_bytes, &a, &c))) return e;
+  if ((e = check_caches(n_cache, caches, state, nullptr, &c))) return e;
+  if ((e = check_pages_ws(state, {}, n_cache, caches, workspace, ws_bytes, &a, &c))) return e;
   EA_HIP_TRY(launch_pages_compact(a, c, (hipStream_t)stream));
   return ok();
 }

@@ -339,3 +339,52 @@ def test_share_of_packed_sequences_without_frequencies():
 def test_extend_refuses_counts_over_its_status():
     assert extend(add=A + (6 << 20)) == ARG and extend(add=A + (6 << 20) - 12) == ARG
     assert extend(add=A + (6 << 20) + 8, n=100) == CAPACITY
+
+
+def _at(r):
+    """The address that ``fake`` gave the newest relation, ``r``."""
+    return _next[0] - (r.nbytes + 511) // 256 * 256
+
+
+def test_arrays_and_workspaces_over_other_memory():
+    """No output and no workspace lies over an array that a kernel reads."""
+    # head rows
+    q = fake([9, 256])
+    at = _at(q)
+    assert heads(q=q, freq=at) == ARG and heads(q=q, freq=at + 4 * 32 * 4, slots=at + 9 * 512 - 4) == ARG
+    L, h = ea.lib(), lambda r: None if r is None else r._h
+    x, k, v = fake([9, 512]), fake([9, 128]), fake([9, 128])
+    run = lambda pos: L.ea_heads(h(x), None, None, h(q), h(k), h(v),
+                                 ctypes.byref(E._HeadsParams(64, 0.0, 0, 0, None, pos, None)), None)
+    assert run(at - 32) == ARG and run(at + 9 * 512 - 4) == ARG
+    # their gradient
+    dx = fake([9, 512])
+    at = _at(dx)
+    big = 1 << 30
+    assert grad(dx=dx, ws=at, n=big) == ARG and grad(dx=dx, ws=at - 256, n=big) == ARG
+    assert grad(ws=1 << 50, n=1000, dx=dx) == CAPACITY
+    # attention over pages
+    out = fake([8, 5, 128])
+    at = _at(out)
+    for name in ("lengths", "table", "start"):
+        assert paged(out=out, ws=1 << 50, **{name: at}) == ARG
+        assert paged(ws=1 << 50, **{name: (1 << 50) + 4096}) == ARG
+    assert paged(out=out, ws=1 << 50, table=at - 5 * 4 * 4 + 4) == ARG
+    for name in ("gs", "gk"):
+        assert paged(out=out, ws=1 << 50, **{"n_group": 2, "gs": 1 << 45, "gk": 1 << 46, name: at}) == ARG
+    assert paged(out=out, ws=at, lengths=1 << 45, table=1 << 46) == ARG
+    q = fake([5, 1024])
+    assert paged(q=q, ws=_at(q), lengths=1 << 45, table=1 << 46) == ARG
+    # the page table
+    c = cache(30, 2, 16, 64)
+    at = _at(c)
+    for bad in ("table", "lengths", "refs", "out_table", "out_refs", "status"):
+        assert select([c], **{bad: at}) == ARG and compact([c], **{bad: at}) == ARG
+    assert select([c], parent=at) == ARG and select([c], parent=at + c.nbytes - 4) == ARG
+    for call in (select, compact):
+        assert call([c], ws=at) == ARG
+        for bad in (0, 1, 2, 3, 5, 6):
+            assert call(ws=A + (bad << 20)) == ARG
+    assert select(ws=A + (7 << 20)) == ARG
+    for bad in (0, 1, 2, 5, 6, 7, 8):
+        assert extend(ws=A + (bad << 20)) == ARG
