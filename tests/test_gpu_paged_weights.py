@@ -102,3 +102,64 @@ def test_many_small_weights_beside_large_ones(n, n_q, hq, d, shared, dtype):
     ref, info = R.attention(R.f64(q), R.f64(k), R.f64(v), table, [n] * seqs, page, starts, scale)
     assert ref.min() > 0.01
     R.check(R.f64(out.view(q.shape)), ref, _tol(ref, info, dtype, d))
+
+
+LONG = [
+    # lens, groups, n_q, hq, hkv, d
+    ([70000], [], 1, 4, 1, 128),                                       # parts joined by the waves of a workgroup
+    ([20000, 3], [], 1, 4, 1, 128),
+    ([30010, 30001, 29990], [(0, 3, 29984)], 1, 4, 1, 128),            # shared and own parts
+    ([9000 + i for i in range(12)], [(0, 12, 8960)], 1, 8, 1, 64),
+    ([131072, 5, 900, 1, 70, 300, 64, 2], [], 1, 4, 1, 128),           # the last to arrive joins hundreds of parts
+    ([32000 - 100 * i for i in range(8)], [], 1, 4, 1, 64),
+    ([40000, 17], [], 12, 4, 1, 128),                                  # 48 columns a sequence
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("case", LONG, ids=[f"n{len(c[0])}_{c[0][0]}_g{len(c[1])}_q{c[2]}_d{c[5]}" for c in LONG])
+def test_every_stretch_of_a_long_walk_counts(case, dtype):
+    """Each 64 keys add to an element of their own (one of d, in turn) with a
+    weight of 1, 2 or 4: a stretch that is lost, counted twice or joined with
+    another's maximum changes its element by far more than the tolerance."""
+    lens, groups, n_q, hq, hkv, d = case
+    page, longest = 64, max(lens)
+    held = -(-longest // page)
+    rng = np.random.default_rng(9)
+    octave = rng.integers(0, 3, held)
+    octave[0], octave[-1] = 2, 2
+    # every sequence reads the same pages, in an order of their own
+    order = rng.permutation(held)
+    place = torch.from_numpy(order).cuda()
+    k = torch.zeros((held, hkv, page, d), device="cuda")
+    v = torch.zeros_like(k)
+    k[place, :, :, 0] = torch.from_numpy(octave).cuda().float()[:, None, None]
+    v[place, :, :, torch.arange(held, device="cuda") % d] = 1.0
+    k, v = k.to(R.TORCH[dtype]), v.to(R.TORCH[dtype])
+    q = torch.zeros((len(lens) * n_q, hq, d), device="cuda", dtype=R.TORCH[dtype])
+    q[..., 0] = 1.0
+    starts = [n_q * i for i in range(len(lens) + 1)]
+    table = order[None].repeat(len(lens), 0)
+    kw = {"group_start": R.i32([groups[0][0], groups[0][1]]), "group_shared": R.i32([groups[0][2]])} if groups else {}
+    scale = float(np.float32(np.log(2)))
+    outs = []
+    for _ in range(3):
+        out = torch.full((len(q), hq * d), float("nan"), device="cuda", dtype=R.TORCH[dtype])
+        ea.attention_paged(R.rel(q.view(len(q), -1)), R.pages_rel(k), R.pages_rel(v), R.rel(out), scale=scale,
+                           table=R.i32(table), lengths=R.i32(lens), q_start=R.i32(starts), **kw)
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    got = R.f64(outs[0].view(q.shape))
+    for s, n in enumerate(lens):
+        for i in range(n_q):
+            seen = max(0, n - n_q + i + 1)
+            keys = np.clip(seen - page * np.arange(held), 0, page)   # of each stretch
+            add = keys * np.exp(scale * octave)
+            ref = np.zeros(d)
+            np.add.at(ref, np.arange(held) % d, add / max(add.sum(), 1e-300))
+            # A is the value itself, one key's score is at most scale * 2
+            info = (ref, 2 * scale, 1.0, seen)
+            tol = _tol(ref, info, dtype, d)
+            if seen > page * d:  # the smallest whole stretch changes its element by four tolerances and more
+                assert (add[keys == page] / add.sum() > 4 * tol[np.flatnonzero(keys == page) % d]).all()
+            R.check(got[s * n_q + i], np.broadcast_to(ref, (hq, d)), tol)
