@@ -280,3 +280,42 @@ def test_weights_and_their_gradients_of_other_types():
                                    R.f64(freq), False, pos.cpu().numpy())
     R.check(R.f64(dx), ref, R.HALF["bf16"] * np.abs(ref) + 1.01 * 96 * R.F * scale)
     R.check(R.f64(dwq), dws[0], R.HALF["bf16"] * np.abs(dws[0]) + 1.01 * 160 * R.F * dws[1])
+
+
+MANY = [
+    # more tokens than a launch has waves (768 workgroups of 4 in 16 bits, 512 in
+    # f32), so that a wave goes on to others; the last round is partly filled
+    (3500, 2, 1, 64, 64, False, True, "bf16", 5000),
+    (6201, 3, 1, 128, 128, False, True, "f16", 5000),
+    (4100, 2, 1, 80, 40, False, True, "f32", 5000),    # rotary / 2 no multiple of 8
+    (2500, 4, 2, 64, 32, True, True, "f32", 0),
+    (3300, 1, 1, 96, 96, True, True, "bf16", 0),
+    (3100, 1, 1, 512, 512, False, True, "bf16", 5000),
+]
+
+
+@pytest.mark.parametrize("case", MANY, ids=[f"t{c[0]}_h{c[1]}_{c[2]}_d{c[3]}_r{c[4]}_{c[7]}" for c in MANY])
+def test_heads_backward_over_many_tokens(case):
+    test_heads_backward(case)
+
+
+@pytest.mark.parametrize("form", ["tokens", "heads"])
+@pytest.mark.parametrize("case", MANY[:2] + MANY[3:5], ids=[f"t{c[0]}_d{c[3]}_{c[7]}" for c in MANY[:2] + MANY[3:5]])
+def test_heads_over_many_tokens(case, form):
+    test_heads(case, form)
+
+
+def test_heads_over_more_rows_than_a_launch_holds():
+    """Past 2^20 workgroups of four rows the first waves go round again."""
+    t, hq, hkv, d = (1 << 22) + 70003, 1, 1, 8
+    g = torch.Generator(device="cuda").manual_seed(16)
+    x = torch.randn((t, 3 * d), generator=g, device="cuda").to(torch.bfloat16)
+    wq, wk = (torch.randn(d, generator=g, device="cuda") for _ in range(2))
+    freq = _freq(d)
+    q, k, v = (torch.full((t, d), float("nan"), device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    ea.heads(R.rel(x), R.rel(q), R.rel(k), R.rel(v), d_head=d, wq=R.rel(wq), wk=R.rel(wk), eps=EPS, inv_freq=freq)
+    assert torch.equal(v, x[:, 2 * d:]) and torch.isfinite(q).all() and torch.isfinite(k).all()
+    rows = np.r_[0:40, (1 << 22) - 40:(1 << 22) + 40, t - 40:t]
+    ref, err = R.heads(R.f64(x[rows]), hq, hkv, d, R.f64(wq), R.f64(wk), EPS, R.f64(freq), False, rows)
+    for got, r, e in zip((q, k), ref, err):
+        R.check(R.f64(got[rows]).reshape(len(rows), 1, d), r, R.heads_tol(r, e, "bf16"))
