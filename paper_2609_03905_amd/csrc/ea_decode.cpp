@@ -324,10 +324,19 @@ int plan_paged(const ea_relation* q, const ea_relation* k, const ea_paged* b, bo
   const int64_t cols = (int64_t)mq->t * (mq->h / hkv);
   plan_pass(&p->shared, true, 0, b->n_group, cols, hkv, d);
   plan_pass(&p->own, false, b->n_group, b->n_seq, cols, hkv, d);
-  // without groups, where the arrival counters suffice and a tile has not more
-  // than 64 parts, the last one to arrive joins them and no second launch follows
+  // Without groups, and where the arrival counters suffice, the last part of a
+  // tile to arrive can join them, four at a time, and no second launch follows.
+  // That pays for tiles of few parts: where a table row has at most 12 steps of
+  // 128 keys (one sequence, 32 heads over 8: 1000 keys 10.1 us and 10.7 with the
+  // launch, 1536 keys 11.0 and 10.9, 2048 keys 12.0 and 10.9; 8 of 4K keys, 4
+  // over 1, 16.5 and 11.0), or where there are so many tiles that one has two
+  // parts on the average (64 sequences of 2K keys, 32 over 8, 96 and 99).  A
+  // sequence that outweighs its batch has more: 128K keys beside 63 times 200, 32
+  // over 8, 118 and 115, beside 511 times 200, 4 over 1, 62 and 45; with fewer
+  // tiles than the rule asks for (beside 7 short ones, 4 over 1) 90 and 30.
+  const int64_t steps = (b->stride * k->shape[2] + kPagedStep - 1) / kPagedStep;
   p->own.fused = b->n_group == 0 && p->own.cols <= 32 && p->own.tiles <= kWsCounterBytes / 4 &&
-                 p->own.tiles * 64 >= p->own.grid;
+                 (steps <= 12 || p->own.tiles * 2 >= p->own.grid);
   p->seg = kWsCounterBytes;
   int64_t at = p->seg + align256((b->n_seq + b->n_group) * (int64_t)sizeof(PagedSeg));
   int i = 0;

@@ -110,7 +110,8 @@ LONG = [
     ([20000, 3], [], 1, 4, 1, 128),
     ([30010, 30001, 29990], [(0, 3, 29984)], 1, 4, 1, 128),            # shared and own parts
     ([9000 + i for i in range(12)], [(0, 12, 8960)], 1, 8, 1, 64),
-    ([131072, 5, 900, 1, 70, 300, 64, 2], [], 1, 4, 1, 128),           # the last to arrive joins hundreds of parts
+    ([131072, 5, 900, 1, 70, 300, 64, 2], [], 1, 4, 1, 128),
+    ([131072] + [3] * 299, [], 1, 4, 1, 128),                          # the last to arrive joins hundreds of parts
     ([32000 - 100 * i for i in range(8)], [], 1, 4, 1, 64),
     ([40000, 17], [], 12, 4, 1, 128),                                  # 48 columns a sequence
 ]
