@@ -39,9 +39,9 @@
 //
 // Measured (bf16 or fp16, 32 query heads over 8, D = 128): 48 sequences of up to
 // 8K keys 148 us, 5.4 TB/s (5.1 is a large copy's rate); 64 sequences that share
-// 8K keys 40 + 8 us (walk, join), 32 that share 64K 84 + 8 us, where the bytes
-// take 20 and 66; one sequence of 1000 keys 10.3 us.  With every column tile
-// reading the shared keys for itself the last two took 92 and 213 us.
+// 8K keys 42 + 8 us (walk, join), 32 that share 64K 91 + 8 us, where the bytes
+// take 20 and 66; one sequence of 1000 keys 10.1 us.  With every column tile
+// reading the shared keys for itself those of shared keys took 92 and 213 us.
 #include "ea_decode.h"
 #include "ea_device.h"
 
@@ -82,8 +82,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // half a step of the type (2^-8 of the weight in bf16, 2^-11 in fp16), as much
 // as the output's own store; the two by half a step of half a step (2^-16 and
 // 2^-22; in fp16 also by half the smallest step, see kRaise).  The sum takes the
-// weights as they are.  Twice the products with V: 64 sequences that share 8K keys 47 to
-// 48.5 us, 32 that share 64K 90 to 97; without shared keys no change.
+// weights as they are.  Twice the products with V: 64 sequences that share 8K
+// keys 46 to 47.5 us, 32 that share 64K 90 to 98; without shared keys no change.
 template <bool BF>
 __device__ __forceinline__ void split_p(float a, float b, uint32_t& hi, uint32_t& lo) {
   hi = pack2<BF>(a, b);
@@ -738,7 +738,10 @@ __device__ __forceinline__ void walk_few(const PagedArgs& a, const PagedPass& ps
 // step of 64 keys is fetched once for the workgroup, straight into shared
 // memory (one instruction 1 KiB, a lane 16 bytes, each from its own key row),
 // while the step before is computed; two workgroups share a CU, so that one's
-// softmax runs beside the other's products.
+// softmax runs beside the other's products.  (The schedule takes 28 bytes of
+// shared memory a segment beside the 66 KiB of the walk at D = 128: from about
+// 510 sequences and groups on only one fits.  Groups of 8 that share 2K keys: 504
+// segments 4.0 TB/s, 513 segments 2.9.)
 //   S^T = K Q^T on 32x32x16: a lane holds one column's scores of 16 keys in 32
 //   O^T += V^T P^T: V^T through transposing reads; the product's k index 8 g + e
 //   stands for key 16 hh + 4 g + e (e < 4) or 16 hh + 8 + 4 g + e - 4, as the
