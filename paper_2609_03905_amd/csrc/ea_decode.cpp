@@ -78,7 +78,7 @@ int64_t page_bytes(const ea_relation* r) {
 }
 
 bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-  return a && b && (const char*)a < (const char*)b + nb && (const char*)b < (const char*)a + na;
+  return a && b && na > 0 && nb > 0 && (const char*)a < (const char*)b + nb && (const char*)b < (const char*)a + na;
 }
 bool overlap(const ea_relation* a, const ea_relation* b) {
   return a && b && overlap(a->data, a->nbytes, b->data, b->nbytes);

@@ -388,3 +388,17 @@ def test_arrays_and_workspaces_over_other_memory():
     assert select(ws=A + (7 << 20)) == ARG
     for bad in (0, 1, 2, 5, 6, 7, 8):
         assert extend(ws=A + (bad << 20)) == ARG
+
+
+def test_nothing_overlaps_an_empty_array():
+    """No new tokens are asked for, or no element is rotated: where the empty
+    array points does not matter."""
+    s = state(out_table=A)
+    run = lambda slots, pos: ea.lib().ea_pages_extend(ctypes.byref(s), A + (7 << 20), slots, pos, 0, 256, 100, None)
+    assert run(A + 8, A + (6 << 20) + 4) == CAPACITY and run(A + (7 << 20) + 4, A + (7 << 20) + 4) == CAPACITY
+    x, dq, dx = fake([9, 512]), fake([9, 256]), fake([9, 512])
+    at = _at(dx) + 256
+    prm = E._HeadsParams(64, 1e-6, 0, 0, at, None, None)
+    w, dk = [fake([64], "f32") for _ in range(4)], [fake([9, 128]) for _ in range(2)]
+    assert ea.lib().ea_heads_backward(x._h, w[0]._h, w[1]._h, dq._h, dk[0]._h, dk[1]._h, dx._h, w[2]._h, w[3]._h,
+                                      ctypes.byref(prm), 1 << 50, 1000, None) == CAPACITY
