@@ -205,7 +205,8 @@ class LlamaBlockDecode:
         # (how the columns are tiled depends on the number of groups: fewer may need more)
         need = [ea.attention_paged_workspace(self.q, cache.k[layer], n_seq, g) for g in range(most + 1)]
         if self.x.data.is_cuda:
-            need += [ea.joinagg_workspace(*args, **kw) for args, kw in self._joinaggs.values()]
+            with torch.cuda.device(self.x.data.device):
+                need += [ea.joinagg_workspace(*args, **kw) for args, kw in self._joinaggs.values()]
         self.workspace = ea.new_workspace(max(need), device=device)
 
     def stages(self, slots, positions, q_start=None, group_start=None, group_shared=None):
