@@ -93,6 +93,11 @@ extern "C" {
 #define EA_F32 0
 #define EA_BF16 1
 #define EA_F16 2
+/* Eight bits: what a cache's codes are held in (ea_pages_write).  Relations of
+   them are taken by the calls that say so and by repartition; others refuse them
+   (EA_ERR_DTYPE). */
+#define EA_E4M3 3 /* 4 exponent and 3 mantissa bits: up to 448, NaN, no infinity */
+#define EA_E5M2 4 /* 5 and 2: up to 57344, infinities, NaN                       */
 
 /* ---- join operations (the concrete operator f run on each tuple) ------ */
 /* Generic einsum join: the scalar join of the inputs' elements.            */
@@ -532,6 +537,51 @@ typedef struct ea_paged {
 int ea_attention_paged_workspace(const ea_relation* q, const ea_relation* k, const ea_paged* batch, int64_t* ws_bytes);
 int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_relation* v, ea_relation* out,
                        const ea_paged* batch, void* workspace, int64_t ws_bytes, void* stream);
+
+/* ---- a cache in 8 bits ----------------------------------------------------
+   Codes [pages, Hkv, page_size, d] in EA_E4M3 or EA_E5M2, one block a page (K and
+   V each), and f32 scales [pages, Hkv, page_size / B] of one block: a code c in
+   head h and row r of page p stands for c * scale[p][h][r / B].  B, the rows of
+   a scale's block, divides page_size. */
+typedef struct ea_page_rows {
+  int32_t n_seq;
+  int32_t stride;
+  const int32_t* q_start; /* [n_seq + 1] ascending first rows; NULL: one a sequence */
+  const int32_t* lengths; /* [n_seq] keys, the rows among them                      */
+  const int32_t* table;   /* [n_seq][stride] pages                                  */
+} ea_page_rows;
+/* Quantises rows into the cache.  Rows q_start[s] .. q_start[s+1]-1 of xk and xv
+   are the last of sequence s's lengths[s] keys (as in ea_attention_paged).  For
+   every head and block that rows go to, K and V apart: the scale is the least
+   power of two, from 2^-120 to 2^120, under which the largest finite new |x| is
+   no larger than the largest code.  A block whose first row is among the new
+   ones is begun anew; another keeps its scale if that is larger, and where the
+   scale grows the codes of its rows before the new ones are rounded again.
+   Codes are rounded to nearest, ties to even; NaN is kept, an infinity is one
+   in EA_E5M2 and NaN in EA_E4M3.  Rows behind the new ones stay as they are and
+   stand for nothing.  A row whose page lies outside the cache, or that has no
+   key (more rows than keys), is not written.  Pages that several sequences
+   share, or a block's rows given twice, must not be among those written.
+   xk, xv: [T, Hkv d], or [.., Hkv, T, d] (forms and partitions as ea_heads' q),
+   f32, bf16 or f16; d a multiple of 16 from 16 to 512; (stride + 1) * page_size < 2^31 - 1024,
+   n_seq <= EA_PAGED_MAX_SEQ.  Lengths are taken as at most a table row's keys.
+   Outputs must not overlap anything else.  Asynchronous on `stream`: no plan, no
+   workspace, never allocates; results do not depend on timing.  Errors:
+   EA_ERR_ARG, EA_ERR_DTYPE, EA_ERR_UNSUPPORTED, EA_ERR_HIP. */
+int ea_pages_write(const ea_relation* xk, const ea_relation* xv, ea_relation* k, ea_relation* v, ea_relation* k_scale,
+                   ea_relation* v_scale, const ea_page_rows* rows, void* stream);
+/* The same rows back: xk and xv get c * scale, rounded once.  Rows of a sequence
+   without a key, or whose page lies outside the cache, get zeros; rows of no
+   sequence stay as they were. */
+int ea_pages_read(const ea_relation* k, const ea_relation* v, const ea_relation* k_scale, const ea_relation* v_scale,
+                  ea_relation* xk, ea_relation* xv, const ea_page_rows* rows, void* stream);
+/* ea_attention_paged over such a cache, of keys and values code * scale (any
+   finite scales).  q and out are bf16 or f16; the weights' products with V take
+   them as two bf16 values.  Everything else, the workspace and its size's call
+   among it, is as there. */
+int ea_attention_paged8(const ea_relation* q, const ea_relation* k, const ea_relation* v, const ea_relation* k_scale,
+                        const ea_relation* v_scale, ea_relation* out, const ea_paged* batch, void* workspace,
+                        int64_t ws_bytes, void* stream);
 
 /* ---- the page table of a cache --------------------------------------------
    State, in device int32 arrays: table[n_seq][stride], lengths[n_seq] and

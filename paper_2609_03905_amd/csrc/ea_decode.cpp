@@ -72,6 +72,8 @@ int check_cache(const ea_relation* r, const char* what, bool need_data, int plan
   return EA_OK;
 }
 
+bool is_code(int32_t dtype) { return dtype == EA_E4M3 || dtype == EA_E5M2; }
+
 int64_t page_bytes(const ea_relation* r) {
   const int p = r->rank - 4;
   return align256(r->shape[p + 1] * r->shape[p + 2] * r->shape[p + 3] * dtype_size(r->dtype));
@@ -110,6 +112,23 @@ int check_weights(const ea_relation* w, int32_t d, const char* what) {
   if (e) return e;
   if (w->rank != 1 || w->shape[0] != d) return fail(EA_ERR_ARG, "%s is not [%d]", what, d);
   if (w->nb[0] != 1) return fail(EA_ERR_UNSUPPORTED, "%s is split", what);
+  if (is_code(w->dtype)) return fail(EA_ERR_DTYPE, "%s is held in 8 bits", what);
+  return EA_OK;
+}
+
+// The scales of a cache k and of its counterpart: [pages, heads, blocks of a page].
+int check_scales(const ea_relation* k, const ea_relation* ks, const ea_relation* vs) {
+  for (const ea_relation* r : {ks, vs}) {
+    const char* what = r == ks ? "k_scale" : "v_scale";
+    const int e = check_rel(r, what, true);
+    if (e) return e;
+    if (r->dtype != EA_F32) return fail(EA_ERR_DTYPE, "%s is not f32", what);
+    if (r->rank != 3 || r->shape[0] != k->shape[0] || r->shape[1] != k->shape[1] || k->shape[2] % r->shape[2])
+      return fail(EA_ERR_ARG, "%s is not [%lld, %lld, blocks of a page of %lld]", what, (long long)k->shape[0],
+                  (long long)k->shape[1], (long long)k->shape[2]);
+    if (r->nblocks != 1) return fail(EA_ERR_UNSUPPORTED, "%s is split", what);
+    if (r->shape[2] != ks->shape[2]) return fail(EA_ERR_ARG, "k_scale and v_scale differ in shape");
+  }
   return EA_OK;
 }
 
@@ -134,6 +153,7 @@ int check_heads(const ea_relation* x, const ea_relation* wq, const ea_relation* 
   if (wq && !(p->eps >= 0.0f && std::isfinite(p->eps))) return fail(EA_ERR_ARG, "eps is negative or not finite");
   for (const ea_relation* r : {q, k, v})
     if (r->dtype != x->dtype) return fail(EA_ERR_DTYPE, "q, k, v and qkv are of different dtypes");
+  if (is_code(x->dtype)) return fail(EA_ERR_DTYPE, "head rows are f32, bf16 or f16 (ea_pages_write quantises)");
   if (x->rank != 2) return fail(EA_ERR_ARG, "qkv has rank %d, not 2", x->rank);
   if ((e = row_map(x, d, "qkv", mx)) || (e = row_map(q, d, "q", mq))) return e;
   int32_t hkv;
@@ -312,8 +332,12 @@ int plan_paged(const ea_relation* q, const ea_relation* k, const ea_paged* b, bo
   int e;
   if ((e = check_rel(q, "q", need_data)) || (e = check_cache(k, "k", need_data, 0))) return e;
   const int64_t d = k->shape[3], hkv = k->shape[1];
-  if (k->dtype != EA_BF16 && k->dtype != EA_F16) return fail(EA_ERR_DTYPE, "the cache is neither bf16 nor f16");
-  if (q->dtype != k->dtype) return fail(EA_ERR_DTYPE, "q and the cache are of different dtypes");
+  if (is_code(k->dtype)) {
+    if (q->dtype != EA_BF16 && q->dtype != EA_F16) return fail(EA_ERR_DTYPE, "q is neither bf16 nor f16");
+  } else {
+    if (k->dtype != EA_BF16 && k->dtype != EA_F16) return fail(EA_ERR_DTYPE, "the cache is neither bf16 nor f16");
+    if (q->dtype != k->dtype) return fail(EA_ERR_DTYPE, "q and the cache are of different dtypes");
+  }
   if (d != 64 && d != 128) return fail(EA_ERR_UNSUPPORTED, "head width %lld is neither 64 nor 128", (long long)d);
   if ((e = row_map(q, (int32_t)d, "q", mq))) return e;
   if (mq->h % hkv) return fail(EA_ERR_ARG, "%d query heads over %lld key-value heads", mq->h, (long long)hkv);
@@ -366,17 +390,26 @@ int ea_attention_paged_workspace(const ea_relation* q, const ea_relation* k, con
   return ok();
 }
 
-int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_relation* v, ea_relation* out,
-                       const ea_paged* batch, void* workspace, int64_t ws_bytes, void* stream) {
+}  // extern "C"
+
+namespace {
+
+// Both forms of the call: over a cache in 16 bits (no scales) or in 8.
+int attention_paged(const ea_relation* q, const ea_relation* k, const ea_relation* v, const ea_relation* ks,
+                    const ea_relation* vs, bool codes, ea_relation* out, const ea_paged* batch, void* workspace,
+                    int64_t ws_bytes, void* stream) {
   PagedArgs a{};
   PagedPlan p;
   int e = plan_paged(q, k, batch, true, &a.q, &p);
   if (e) return e;
   if ((e = check_cache(v, "v", true, 0)) || (e = check_rel(out, "out", true))) return e;
-  if (v->dtype != k->dtype || out->dtype != k->dtype)
-    return fail(EA_ERR_DTYPE, "q, k, v and out are of different dtypes");
+  if (codes != is_code(k->dtype))
+    return fail(EA_ERR_DTYPE, codes ? "the cache is not held in 8 bits" : "a cache in 8 bits: ea_attention_paged8 takes it");
+  if (v->dtype != k->dtype || out->dtype != q->dtype)
+    return fail(EA_ERR_DTYPE, "k and v, or q and out, are of different dtypes");
   for (int i = 0; i < 4; ++i)
     if (v->shape[i] != k->shape[i]) return fail(EA_ERR_ARG, "k and v caches differ in shape");
+  if (codes && (e = check_scales(k, ks, vs))) return e;
   const int32_t d = (int32_t)k->shape[3];
   if ((e = row_map(out, d, "out", &a.o))) return e;
   if (a.o.t != a.q.t || a.o.h != a.q.h) return fail(EA_ERR_ARG, "out and q differ in rows or heads");
@@ -395,7 +428,7 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
                   (long long)(b.stride * k->shape[2]));
   }
   if (!b.q_start && a.q.t < b.n_seq) return fail(EA_ERR_ARG, "%d query rows for %d sequences", a.q.t, b.n_seq);
-  for (const ea_relation* r : {q, k, v})
+  for (const ea_relation* r : {q, k, v, ks, vs})
     if (overlap(out, r)) return fail(EA_ERR_ARG, "out overlaps an input");
   const int64_t need = p.bytes;
   if (!workspace || (uintptr_t)workspace % 256) return fail(EA_ERR_ARG, "workspace missing or not 256-byte aligned");
@@ -407,7 +440,7 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
                     b.n_group ? ints(b.group_start, b.n_group + (int64_t)1) : Span{nullptr, 0},
                     b.n_group ? ints(b.group_shared, b.n_group) : Span{nullptr, 0}}))
       return fail(EA_ERR_ARG, "out or the workspace overlaps an array of the batch");
-  if (overlap(Span{workspace, need}, {span(q), span(k), span(v), span(out)}))
+  if (overlap(Span{workspace, need}, {span(q), span(k), span(v), span(ks), span(vs), span(out)}))
     return fail(EA_ERR_ARG, "the workspace overlaps a relation");
   a.pq = (const char*)q->data;
   a.pk = (const char*)k->data;
@@ -438,8 +471,119 @@ int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_rela
     s->part_ml = (float*)(ws + p.ml[i]);
     s->part_o = (float*)(ws + p.o[i++]);
   }
-  EA_HIP_TRY(launch_paged(a, p.shared, p.own, d, k->dtype, (hipStream_t)stream));
+  if (codes) {
+    a.ks = (const float*)ks->data;
+    a.vs = (const float*)vs->data;
+    a.n_blocks = (int32_t)ks->shape[2];
+    a.block = fast_div((uint32_t)(a.page_size / a.n_blocks));
+    EA_HIP_TRY((k->dtype == EA_E4M3 ? launch_paged8_e4m3 : launch_paged8_e5m2)(a, p.shared, p.own, d, q->dtype,
+                                                                               (hipStream_t)stream));
+  } else {
+    EA_HIP_TRY(launch_paged(a, p.shared, p.own, d, k->dtype, (hipStream_t)stream));
+  }
   return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+int ea_attention_paged(const ea_relation* q, const ea_relation* k, const ea_relation* v, ea_relation* out,
+                       const ea_paged* batch, void* workspace, int64_t ws_bytes, void* stream) {
+  return attention_paged(q, k, v, nullptr, nullptr, false, out, batch, workspace, ws_bytes, stream);
+}
+
+int ea_attention_paged8(const ea_relation* q, const ea_relation* k, const ea_relation* v, const ea_relation* k_scale,
+                        const ea_relation* v_scale, ea_relation* out, const ea_paged* batch, void* workspace,
+                        int64_t ws_bytes, void* stream) {
+  return attention_paged(q, k, v, k_scale, v_scale, true, out, batch, workspace, ws_bytes, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+// Both directions between rows and a cache in 8 bits.
+int cache8(const ea_relation* xk, const ea_relation* xv, const ea_relation* k, const ea_relation* v,
+           const ea_relation* ks, const ea_relation* vs, const ea_page_rows* rows, bool write, void* stream) {
+  if (!rows) return fail(EA_ERR_ARG, "NULL rows");
+  Cache8Args a{};
+  int e;
+  if ((e = check_rel(xk, "xk", true)) || (e = check_rel(xv, "xv", true)) || (e = check_cache(k, "k", true, 0)) ||
+      (e = check_cache(v, "v", true, 0)))
+    return e;
+  if (!is_code(k->dtype) || v->dtype != k->dtype)
+    return fail(EA_ERR_DTYPE, "the caches are not both held in e4m3, or both in e5m2");
+  if (is_code(xk->dtype) || xv->dtype != xk->dtype)
+    return fail(EA_ERR_DTYPE, "xk and xv are not both f32, both bf16 or both f16");
+  for (int i = 0; i < 4; ++i)
+    if (v->shape[i] != k->shape[i]) return fail(EA_ERR_ARG, "k and v caches differ in shape");
+  if ((e = check_scales(k, ks, vs))) return e;
+  const int64_t d = k->shape[3], hkv = k->shape[1], page = k->shape[2];
+  if (d < 16 || d > 512 || d % 16)
+    return fail(EA_ERR_UNSUPPORTED, "head width %lld is no multiple of 16 in [16, 512]", (long long)d);
+  if ((e = row_map(xk, (int32_t)d, "xk", &a.xk)) || (e = row_map(xv, (int32_t)d, "xv", &a.xv))) return e;
+  if (a.xk.h != hkv || a.xv.h != hkv || a.xk.t != a.xv.t)
+    return fail(EA_ERR_ARG, "xk has %d rows of %d heads, xv %d of %d, the caches %lld heads", a.xk.t, a.xk.h, a.xv.t,
+                a.xv.h, (long long)hkv);
+  const ea_page_rows& b = *rows;
+  if (b.n_seq < 1 || b.stride < 1) return fail(EA_ERR_ARG, "n_seq %d, table stride %d", b.n_seq, b.stride);
+  if (b.n_seq > EA_PAGED_MAX_SEQ)
+    return fail(EA_ERR_UNSUPPORTED, "%d sequences, at most %d", b.n_seq, EA_PAGED_MAX_SEQ);
+  if ((b.stride + (int64_t)1) * page > INT32_MAX - 1024)
+    return fail(EA_ERR_UNSUPPORTED, "a table row of 2^31 keys or more");
+  if (hkv > 1 << 20) return fail(EA_ERR_UNSUPPORTED, "%lld heads", (long long)hkv);
+  if (!b.lengths || !b.table) return fail(EA_ERR_ARG, "NULL lengths or table");
+  if (!b.q_start && a.xk.t < b.n_seq) return fail(EA_ERR_ARG, "%d rows for %d sequences", a.xk.t, b.n_seq);
+  const ea_relation* const outs_w[] = {k, v, ks, vs};
+  const ea_relation* const outs_r[] = {xk, xv};
+  const ea_relation* const all[] = {xk, xv, k, v, ks, vs};
+  for (int i = 0; i < (write ? 4 : 2); ++i) {
+    const ea_relation* o = write ? outs_w[i] : outs_r[i];
+    for (const ea_relation* r : all)
+      if (r != o ? overlap(o, r) : false) return fail(EA_ERR_ARG, "an output overlaps another relation");
+    if (overlap(span(o), {ints(b.q_start, b.n_seq + (int64_t)1), ints(b.lengths, b.n_seq),
+                          ints(b.table, b.n_seq * (int64_t)b.stride)}))
+      return fail(EA_ERR_ARG, "an output overlaps q_start, lengths or the table");
+  }
+  if (write ? k == v || ks == vs : xk == xv) return fail(EA_ERR_ARG, "K and V are one relation");
+  a.pxk = (const char*)xk->data;
+  a.pxv = (const char*)xv->data;
+  a.pk = (char*)k->data;
+  a.pv = (char*)v->data;
+  a.ks = (float*)ks->data;
+  a.vs = (float*)vs->data;
+  a.q_start = b.q_start;
+  a.len = b.lengths;
+  a.table = b.table;
+  a.n_seq = b.n_seq;
+  a.stride = b.stride;
+  a.n_pages = (int32_t)k->shape[0];
+  a.page_size = (int32_t)page;
+  a.rows = a.xk.t;
+  a.hkv = (int32_t)hkv;
+  a.d = (int32_t)d;
+  a.n_blocks = (int32_t)ks->shape[2];
+  a.block_rows = a.page_size / a.n_blocks;
+  a.page = fast_div((uint32_t)a.page_size);
+  a.block = fast_div((uint32_t)a.block_rows);
+  a.page_bytes = page_bytes(k);
+  EA_HIP_TRY(launch_cache8(a, xk->dtype, k->dtype, write, (hipStream_t)stream));
+  return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+int ea_pages_write(const ea_relation* xk, const ea_relation* xv, ea_relation* k, ea_relation* v, ea_relation* k_scale,
+                   ea_relation* v_scale, const ea_page_rows* rows, void* stream) {
+  return cache8(xk, xv, k, v, k_scale, v_scale, rows, true, stream);
+}
+
+int ea_pages_read(const ea_relation* k, const ea_relation* v, const ea_relation* k_scale, const ea_relation* v_scale,
+                  ea_relation* xk, ea_relation* xv, const ea_page_rows* rows, void* stream) {
+  return cache8(xk, xv, k, v, k_scale, v_scale, rows, false, stream);
 }
 
 }  // extern "C"

@@ -127,9 +127,37 @@ struct PagedArgs {
   int64_t page_bytes;
   float scale;       // of the scores, log2 domain
   PagedSeg* seg;     // groups, then sequences
+  // a cache in 8 bits: scales [pages][heads][blocks of a page]
+  const float *ks, *vs;
+  FastDiv block;     // by rows of a scale's block
+  int32_t n_blocks;
 };
 hipError_t launch_paged(const PagedArgs& a, const PagedPass& shared, const PagedPass& own, int32_t d, int32_t dtype,
                         hipStream_t s);
+// The same over codes; dtype is that of q and out.
+hipError_t launch_paged8_e4m3(const PagedArgs& a, const PagedPass& shared, const PagedPass& own, int32_t d,
+                              int32_t dtype, hipStream_t s);
+hipError_t launch_paged8_e5m2(const PagedArgs& a, const PagedPass& shared, const PagedPass& own, int32_t d,
+                              int32_t dtype, hipStream_t s);
+// The join of a call's partial results, where the walk does not do it itself.
+hipError_t launch_paged_join(const PagedArgs& a, const PagedPass& shared, const PagedPass& own, int32_t d,
+                             int32_t dtype, hipStream_t s);
+
+// ---- a cache in 8 bits ---------------------------------------------------------
+constexpr int kScaleExp = 120;  // scales that a write gives are 2^-120 to 2^120
+
+struct Cache8Args {
+  RowMap xk, xv;              // rows
+  const char *pxk, *pxv;      // read by the write, written by the read
+  char *pk, *pv;              // codes
+  float *ks, *vs;             // scales [pages][heads][blocks of a page]
+  const int32_t *q_start, *len, *table;
+  int32_t n_seq, stride, n_pages, page_size, rows, hkv, d;
+  int32_t block_rows, n_blocks;  // rows of a scale's block, blocks of a page
+  FastDiv page, block;
+  int64_t page_bytes;
+};
+hipError_t launch_cache8(const Cache8Args& a, int32_t dtype, int32_t code, bool write, hipStream_t s);
 
 // ---- the page table -------------------------------------------------------------
 struct PagesArgs {

@@ -54,6 +54,8 @@ int dtype_size(int32_t dt) {
     case EA_F32: return 4;
     case EA_BF16: return 2;
     case EA_F16: return 2;
+    case EA_E4M3: return 1;
+    case EA_E5M2: return 1;
     default: return EA_ERR_DTYPE;
   }
 }
@@ -747,7 +749,7 @@ int classify(const Spec& sp, int32_t join_op, int32_t agg_op, const ea_relation*
   std::string out_letters(sp.let[out], sp.let[out] + sp.rank[out]);
   *oi = OpInfo();
   for (int i = 0; i <= n_in; ++i)
-    if (!is_float_dtype(ops[i]->dtype)) return fail(EA_ERR_DTYPE, "operand %d has an unknown dtype", i);
+    if (!is_float_dtype(ops[i]->dtype)) return fail(EA_ERR_DTYPE, "operand %d is neither f32, bf16 nor f16", i);
   switch (join_op) {
     case EA_JOIN_MUL:
     case EA_JOIN_ADD: {

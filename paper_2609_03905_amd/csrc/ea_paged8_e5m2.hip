@@ -1,0 +1,11 @@
+// ea_paged8_e5m2.hip -- attention over a paged cache of e5m2 codes.
+#include "ea_paged8.h"
+
+namespace ea {
+
+hipError_t launch_paged8_e5m2(const PagedArgs& a, const PagedPass& sh, const PagedPass& own, int32_t d, int32_t dt,
+                              hipStream_t s) {
+  return run_code<true>(a, sh, own, d, dt, s);
+}
+
+}  // namespace ea

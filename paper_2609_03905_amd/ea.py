@@ -24,9 +24,9 @@ ERR_NAMES = {-1: "EA_ERR_ARG", -2: "EA_ERR_DTYPE", -3: "EA_ERR_PARTITION", -4: "
              -9: "EA_ERR_NOPLAN"}
 ERR_ARG, ERR_CAPACITY, ERR_NOPLAN = -1, -4, -9
 WS_COUNTER_BYTES = 262144  # EA_WS_COUNTER_BYTES: the counter area at the start of a workspace
-F32, BF16, F16 = 0, 1, 2
-DTYPES = {"f32": F32, "bf16": BF16, "f16": F16}
-ELEM_SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+F32, BF16, F16, E4M3, E5M2 = 0, 1, 2, 3, 4
+DTYPES = {"f32": F32, "bf16": BF16, "f16": F16, "e4m3": E4M3, "e5m2": E5M2}
+ELEM_SIZE = {"f32": 4, "bf16": 2, "f16": 2, "e4m3": 1, "e5m2": 1}
 JOIN_MUL, JOIN_ADD = 0, 1
 OP_RMSNORM, OP_SOFTMAX, OP_ATTENTION, OP_SWIGLU = 16, 17, 18, 19
 AGG_NONE, AGG_SUM, AGG_MAX, AGG_LSE = 0, 1, 2, 3
@@ -55,6 +55,11 @@ class _Paged(ctypes.Structure):
     _fields_ = [("scale", ctypes.c_float), ("n_seq", ctypes.c_int32), ("q_start", ctypes.c_void_p),
                 ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("stride", ctypes.c_int32),
                 ("n_group", ctypes.c_int32), ("group_start", ctypes.c_void_p), ("group_shared", ctypes.c_void_p)]
+
+
+class _PageRows(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("stride", ctypes.c_int32), ("q_start", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p)]
 
 
 class _Pages(ctypes.Structure):
@@ -107,6 +112,9 @@ def lib() -> ctypes.CDLL:
         L.ea_heads_backward.argtypes = [vp] * 9 + [P(_HeadsParams), vp, i64, vp]
         L.ea_attention_paged_workspace.argtypes = [vp, vp, P(_Paged), P(i64)]
         L.ea_attention_paged.argtypes = [vp] * 4 + [P(_Paged), vp, i64, vp]
+        L.ea_attention_paged8.argtypes = [vp] * 6 + [P(_Paged), vp, i64, vp]
+        L.ea_pages_write.argtypes = [vp] * 6 + [P(_PageRows), vp]
+        L.ea_pages_read.argtypes = [vp] * 6 + [P(_PageRows), vp]
         L.ea_pages_workspace.argtypes = [i32, i32, P(i64)]
         L.ea_pages_extend.argtypes = [P(_Pages), vp, vp, vp, i32, vp, i64, vp]
         L.ea_pages_select.argtypes = [i32, P(vp), P(_Pages), vp, vp, i64, vp]
@@ -519,7 +527,8 @@ def attention_paged_workspace(q: Relation, k: Relation, n_seq: int, n_group: int
 
 def attention_paged(q: Relation, k: Relation, v: Relation, out: Relation, *, scale: float, table: torch.Tensor,
                     lengths: torch.Tensor, q_start: torch.Tensor | None = None,
-                    group_start: torch.Tensor | None = None, group_shared: torch.Tensor | None = None, stream=None,
+                    group_start: torch.Tensor | None = None, group_shared: torch.Tensor | None = None,
+                    k_scale: Relation | None = None, v_scale: Relation | None = None, stream=None,
                     workspace: torch.Tensor | None = None) -> None:
     """Attention of each sequence's newest tokens over a paged cache: ``k`` and
     ``v`` [pages, Hkv, page_size, d], one block a page; sequence s has
@@ -527,14 +536,54 @@ def attention_paged(q: Relation, k: Relation, v: Relation, out: Relation, *, sca
     q_start[s + 1] - 1 of ``q`` (None: row s), the last of which sees all keys
     and each one before it one less.  Groups of sequences group_start[g] ..
     group_start[g + 1] - 1 share their first group_shared[g] keys, which are
-    read once.  The arrays are read when the kernels run."""
-    _on_device(q, k, v, out)
+    read once.  The arrays are read when the kernels run.  A cache in 8 bits
+    ("e4m3", "e5m2", see pages_write) comes with its scales."""
+    _on_device(q, k, v, out, k_scale, v_scale)
+    if (k_scale is None) != (v_scale is None):
+        raise EAError(ERR_ARG, "k_scale and v_scale: both or neither")
     b = _paged(scale, table, lengths, q_start, group_start, group_shared)
     s = _stream(stream)
     need = ctypes.c_int64()
     _check(lib().ea_attention_paged_workspace(q._h, k._h, ctypes.byref(b), ctypes.byref(need)))
     ws, n = _workspace(need.value, workspace, s)
-    _check(lib().ea_attention_paged(q._h, k._h, v._h, out._h, ctypes.byref(b), ws, n, s))
+    if k_scale is None:
+        _check(lib().ea_attention_paged(q._h, k._h, v._h, out._h, ctypes.byref(b), ws, n, s))
+    else:
+        _check(lib().ea_attention_paged8(q._h, k._h, v._h, k_scale._h, v_scale._h, out._h, ctypes.byref(b), ws, n, s))
+
+
+def _page_rows(table, lengths, q_start):
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise EAError(ERR_ARG, "table is no [sequences, pages] tensor")
+    n, stride = table.shape
+    return _PageRows(n, stride, _device_array(q_start, "q_start", (n + 1,), optional=True),
+                     _device_array(lengths, "lengths", (n,)), _device_array(table, "table", (n, stride)))
+
+
+def pages_write(xk: Relation, xv: Relation, k: Relation, v: Relation, *, k_scale: Relation, v_scale: Relation,
+                table: torch.Tensor, lengths: torch.Tensor, q_start: torch.Tensor | None = None, stream=None) -> None:
+    """Rows quantised into a cache in 8 bits.  Rows q_start[s] .. q_start[s + 1]
+    - 1 (None: row s) of ``xk`` and ``xv`` ([T, Hkv d] or [.., Hkv, T, d]) are
+    the last of sequence s's lengths[s] keys, which lie in the pages table[s] of
+    ``k`` and ``v``: codes [pages, Hkv, page_size, d], "e4m3" or "e5m2", one
+    block a page.  Every head and block of page_size / n rows has a scale, a
+    power of two, in ``k_scale`` and ``v_scale`` ("f32" [pages, Hkv, n]): the
+    least under which the largest new element has a code, or the one that the
+    block has from earlier rows, if that is larger; where it grows those rows are
+    rounded again.  A block whose first row is written is begun anew.  The arrays
+    are read when the kernel runs."""
+    _on_device(xk, xv, k, v, k_scale, v_scale)
+    rows = _page_rows(table, lengths, q_start)
+    _check(lib().ea_pages_write(xk._h, xv._h, k._h, v._h, k_scale._h, v_scale._h, ctypes.byref(rows), _stream(stream)))
+
+
+def pages_read(k: Relation, v: Relation, xk: Relation, xv: Relation, *, k_scale: Relation, v_scale: Relation,
+               table: torch.Tensor, lengths: torch.Tensor, q_start: torch.Tensor | None = None, stream=None) -> None:
+    """The rows that pages_write puts into a cache, read back into ``xk`` and
+    ``xv``: code times scale, rounded once (zeros where a row has no key)."""
+    _on_device(xk, xv, k, v, k_scale, v_scale)
+    rows = _page_rows(table, lengths, q_start)
+    _check(lib().ea_pages_read(k._h, v._h, k_scale._h, v_scale._h, xk._h, xv._h, ctypes.byref(rows), _stream(stream)))
 
 
 def _pages(table, lengths, refs, page_size, out_table, out_lengths, out_refs, status):

@@ -1,0 +1,162 @@
+"""What the calls on a cache in 8 bits refuse, host only: every check precedes HIP."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+ea = pytest.importorskip("paper_2609_03905_amd")
+from paper_2609_03905_amd import ea as E  # noqa: E402
+from test_decode_cpu import cache, fake, heads, paged  # noqa: E402
+import cache8_ref as C  # noqa: E402
+
+OK, ARG, DTYPE, CAPACITY, UNSUPPORTED = 0, -1, -2, -4, -7
+NODATA = object()
+
+
+def scales(pages=30, h=2, n=4, dtype="f32", part=None):
+    return fake([pages, h, n], dtype, part)
+
+
+def bare(shape, dtype, part=None):
+    return ea.Relation(shape, dtype, part or E.whole_partition(shape), allocate=False)
+
+
+def rows(call, **change):
+    a = dict(xk=fake([9, 2 * 64]), xv=fake([2, 9, 64]), k=cache(30, 2, 16, 64, "e4m3"), v=cache(30, 2, 16, 64, "e4m3"),
+             ks=scales(), vs=scales(), n_seq=3, stride=5, start=256, lengths=512, table=1024)
+    a.update({n: v() if callable(v) else v for n, v in change.items()})
+    b = E._PageRows(a["n_seq"], a["stride"], a["start"], a["lengths"], a["table"])
+    h = lambda r: None if r is None else r._h
+    order = ("xk", "xv", "k", "v", "ks", "vs") if call == "write" else ("k", "v", "ks", "vs", "xk", "xv")
+    return getattr(ea.lib(), "ea_pages_" + call)(*[h(a[x]) for x in order], None if a.get("no_rows") else ctypes.byref(b),
+                                                 None)
+
+
+@pytest.mark.parametrize("call", ["write", "read"])
+@pytest.mark.parametrize("code,change", [
+    (ARG, dict(no_rows=True)), (ARG, dict(xk=None)), (ARG, dict(xv=None)), (ARG, dict(k=None)), (ARG, dict(v=None)),
+    (ARG, dict(ks=None)), (ARG, dict(vs=None)),
+    (ARG, dict(xk=lambda: bare([9, 128], "bf16"))), (ARG, dict(ks=lambda: bare([30, 2, 4], "f32"))),
+    (ARG, dict(n_seq=0)), (ARG, dict(stride=0)), (UNSUPPORTED, dict(n_seq=2049)), (UNSUPPORTED, dict(stride=2 ** 27)),
+    (ARG, dict(lengths=None)), (ARG, dict(table=None)), (ARG, dict(n_seq=10, start=None)),
+    (DTYPE, dict(k=lambda: cache(30, 2, 16, 64), v=lambda: cache(30, 2, 16, 64))),   # not in 8 bits
+    (DTYPE, dict(v=lambda: cache(30, 2, 16, 64, "e5m2"))),
+    (DTYPE, dict(xv=lambda: fake([9, 128], "f16"))),
+    (DTYPE, dict(xk=lambda: fake([9, 128], "e4m3"), xv=lambda: fake([9, 128], "e4m3"))),
+    (DTYPE, dict(ks=lambda: scales(dtype="bf16"))),
+    (ARG, dict(v=lambda: cache(31, 2, 16, 64, "e4m3"))),
+    (UNSUPPORTED, dict(k=lambda: fake([30, 2, 16, 64], "e4m3"))),                    # a block that is not one page
+    (ARG, dict(ks=lambda: scales(pages=31))), (ARG, dict(ks=lambda: scales(h=1))), (ARG, dict(ks=lambda: scales(n=3))),
+    (ARG, dict(ks=lambda: scales(n=32))), (ARG, dict(vs=lambda: scales(n=8))), (ARG, dict(ks=lambda: fake([30, 8], "f32"))),
+    (UNSUPPORTED, dict(ks=lambda: scales(part=[[0, 15, 30], [0, 2], [0, 4]]))),
+    (UNSUPPORTED, dict(k=lambda: cache(30, 2, 16, 8, "e4m3"), v=lambda: cache(30, 2, 16, 8, "e4m3"))),
+    (UNSUPPORTED, dict(k=lambda: cache(30, 2, 16, 24, "e4m3"), v=lambda: cache(30, 2, 16, 24, "e4m3"))),
+    (UNSUPPORTED, dict(k=lambda: cache(30, 2, 16, 528, "e4m3"), v=lambda: cache(30, 2, 16, 528, "e4m3"))),
+    (ARG, dict(xk=lambda: fake([9, 64]))), (ARG, dict(xk=lambda: fake([8, 128]))), (ARG, dict(xv=lambda: fake([9, 100]))),
+    (UNSUPPORTED, dict(xk=lambda: fake([9, 128], "bf16", [[0, 9], [0, 32, 128]]))),
+])
+def test_rows_refusals(call, code, change):
+    assert rows(call, **change) == code, ea.lib().ea_last_error()
+
+
+def _at(r, address):
+    assert ea.lib().ea_relation_set_data(r.handle, ctypes.c_void_p(address), r.nbytes) == OK
+    return r
+
+
+BASE = 1 << 44  # addresses that no other relation of these tests has
+
+
+def test_rows_overlap():
+    xk, xv = (_at(bare([9, 128], "bf16"), BASE + i * (1 << 20)) for i in range(2))
+    for call, bad in (("write", "k"), ("write", "v"), ("write", "ks"), ("write", "vs")):
+        r = bare([30, 2, 4], "f32") if bad in ("ks", "vs") else \
+            bare([30, 2, 16, 64], "e4m3", [range(31), [0, 2], [0, 16], [0, 64]])
+        assert rows(call, xk=xk, xv=xv, **{bad: _at(r, BASE)}) == ARG
+        at = BASE + (1 << 24)
+        for array in ("start", "lengths", "table"):
+            assert rows(call, **{bad: _at(r, at), array: at + r.nbytes - 4}) == ARG
+    for bad in ("xk", "xv"):
+        x = _at(bare([9, 128], "bf16"), BASE + (1 << 25))
+        for array in ("start", "lengths", "table"):
+            assert rows("read", **{bad: x, array: BASE + (1 << 25)}) == ARG
+        assert rows("read", **{bad: x}, ks=_at(bare([30, 2, 4], "f32"), BASE + (1 << 25) + 256)) == ARG
+    same = fake([9, 128])
+    assert rows("read", xk=same, xv=same) == ARG
+    k, s = cache(30, 2, 16, 64, "e4m3"), scales()
+    assert rows("write", k=k, v=k) == ARG and rows("write", ks=s, vs=s) == ARG
+
+
+def paged8(ws=256, n=None, **change):
+    a = dict(q=fake([5, 8 * 128]), k=cache(30, 2, 16, 128, "e4m3"), v=cache(30, 2, 16, 128, "e4m3"), ks=scales(),
+             vs=scales(), out=fake([8, 5, 128]), scale=0.1, n_seq=5, lengths=256, table=256, stride=4)
+    a.update({x: v() if callable(v) else v for x, v in change.items()})
+    b = E._Paged(a["scale"], a["n_seq"], None, a["lengths"], a["table"], a["stride"], 0, None, None)
+    h = lambda r: None if r is None else r._h
+    if n is None:
+        need = ctypes.c_int64()
+        rc = ea.lib().ea_attention_paged_workspace(h(a["q"]), h(a["k"]), ctypes.byref(b), ctypes.byref(need))
+        n = need.value if rc == OK else 0
+    return ea.lib().ea_attention_paged8(*[h(a[x]) for x in ("q", "k", "v", "ks", "vs", "out")], ctypes.byref(b), ws, n,
+                                        None)
+
+
+@pytest.mark.parametrize("code,change", [
+    (ARG, dict(ks=None)), (ARG, dict(vs=None)), (ARG, dict(scale=0.0)), (ARG, dict(ws=None)), (CAPACITY, dict(n=4096)),
+    (DTYPE, dict(k=lambda: cache(30, 2, 16, 128), v=lambda: cache(30, 2, 16, 128))),
+    (DTYPE, dict(q=lambda: fake([5, 1024], "f32"))), (DTYPE, dict(out=lambda: fake([5, 1024], "f16"))),
+    (DTYPE, dict(q=lambda: fake([5, 1024], "e4m3"))),
+    (DTYPE, dict(v=lambda: cache(30, 2, 16, 128, "e5m2"))), (DTYPE, dict(vs=lambda: scales(dtype="f16"))),
+    (ARG, dict(ks=lambda: scales(n=5))), (ARG, dict(vs=lambda: scales(n=2))),
+    (UNSUPPORTED, dict(k=lambda: cache(30, 2, 16, 96, "e4m3"), v=lambda: cache(30, 2, 16, 96, "e4m3"))),
+])
+def test_attention_refusals(code, change):
+    assert paged8(**change) == code, ea.lib().ea_last_error()
+
+
+def test_attention_overlap():
+    q = fake([5, 1024])
+    assert paged8(q=q, out=q) == ARG
+    s = _at(bare([30, 2, 4], "f32"), BASE)
+    assert paged8(ks=s, out=_at(bare([5, 1024], "bf16"), BASE + 256)) == ARG
+    assert paged8(vs=s, ws=BASE + 256) == ARG
+
+
+def test_other_calls_refuse_eight_bits():
+    assert paged(k=cache(30, 2, 16, 128, "e4m3"), v=cache(30, 2, 16, 128, "e4m3")) == DTYPE  # no scales
+    eight = lambda *s: fake(list(s), "e5m2")
+    assert heads(x=eight(9, 512), q=eight(9, 256), k=eight(9, 128), v=eight(2, 9, 64)) == DTYPE
+    assert heads(wq=fake([64], "e4m3")) == DTYPE and heads(wk=fake([64], "e4m3")) == DTYPE
+    for dtype in ("e4m3", "e5m2"):
+        assert ea.lib().ea_dtype_size(E.DTYPES[dtype]) == 1
+        a, b, c = (fake([256, 256], dtype) for _ in range(3))
+        for op, agg, ins, spec in ((E.JOIN_MUL, E.AGG_SUM, [a, b], "ij,jk->ik"), (E.JOIN_ADD, E.AGG_NONE, [a, b], "ij,ij->ij"),
+                                   (E.OP_SOFTMAX, E.AGG_LSE, [a], "ij->ij")):
+            with pytest.raises(E.EAError) as e:
+                E.joinagg(spec, op, agg, ins, c)
+            assert e.value.code == DTYPE
+        with pytest.raises(E.EAError) as e:  # an output, a residual
+            E.joinagg("ij,jk->ik", E.JOIN_MUL, E.AGG_SUM, [fake([256, 256]), fake([256, 256])], c)
+        assert e.value.code == DTYPE
+
+
+def test_binding_refuses():
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    k = cache(30, 2, 16, 64, "e4m3")
+    with pytest.raises(E.EAError, match="both or neither"):
+        E.attention_paged(fake([3, 256]), k, k, fake([3, 256]), scale=1.0, table=i(3, 5), lengths=i(3), k_scale=scales())
+    for bad in (dict(table=i(3)), dict(table=i(3, 5)), dict(lengths=None)):
+        with pytest.raises(E.EAError):  # a table of one dim; arrays that are not on a GPU
+            E.pages_write(fake([9, 128]), fake([9, 128]), k, k, k_scale=scales(), v_scale=scales(),
+                          **{"table": i(3, 5), "lengths": i(3), **bad})
+
+
+@pytest.mark.parametrize("code", ["e4m3", "e5m2"])
+def test_the_reference_rounds_as_the_type_does(code):
+    x = torch.from_numpy(np.random.default_rng(1).standard_normal(50000) * 10.0 ** np.linspace(-8, 5, 50000)).float()
+    x = x[x.abs() <= C.TOP[code]]
+    C.same(x.to(C.TORCH[code]).float().numpy(), C.rounded(x.double().numpy(), code))
+    for top in (448, 57344, 1, 1.75, 1.76, 3.5, 2.0 ** -130, 0):
+        s = C.least_scale(np.array([top, -np.inf, np.nan]), code)
+        assert top <= C.TOP[code] * s and (s == 2.0 ** C.LEAST or top > C.TOP[code] * s / 2)

@@ -1,0 +1,306 @@
+"""Attention over a paged cache in 8 bits against the 64-bit definition: both
+codes, both query types, scales of one row to a page, with and without shared
+prefixes, whatever the rows and scales hold that nothing sees."""
+import numpy as np
+import pytest
+import torch
+
+import cache8_ref as C
+import decode_ref as R
+from paper_2609_03905_amd import ea
+
+pytestmark = pytest.mark.gpu
+
+
+def _batch(lens, groups, page, block, hkv, d, code, seed, spare=3, spread=2):
+    """Codes and scales of K and V, and the page table; groups is a list of
+    (first, last + 1, keys shared)."""
+    rng = np.random.default_rng(seed)
+    n = len(lens)
+    own = [-(-max(x, 0) // page) for x in lens]
+    table = np.full((n, max(1, max(own)) + 1), -1, np.int64)
+    total = sum(own) + spare
+    ids = list(rng.permutation(total))
+    prefix = {}
+    for first, _, keys in groups:
+        prefix[first] = [ids.pop() for _ in range(keys // page)]
+    for s in range(n):
+        g = next((f for f, e, _ in groups if f <= s < e), None)
+        mine = list(prefix.get(g, []))[:own[s]]
+        mine += [ids.pop() for _ in range(own[s] - len(mine))]
+        table[s, :own[s]] = mine
+    kv = []
+    for _ in range(2):
+        x = rng.standard_normal((total, hkv, page, d)) * C.TOP[code] / 5
+        x = np.clip(x, -C.TOP[code], C.TOP[code])
+        # keys of about 1, whatever the code's reach; scales up to 2^spread apart
+        scale = 2.0 ** rng.integers(-spread, spread + 1, (total, hkv, page // block)) * 5 / C.TOP[code]
+        kv.append((C.rounded(x, code), np.float32(scale).astype(np.float64)))
+    return kv, table, rng
+
+
+def _run(q, dev, table, lens, q_start, groups, scale, out=None, form="tokens", **more):
+    t, hq, d = q.shape
+    src = q.reshape(t, hq * d) if form == "tokens" else q.transpose(0, 1).contiguous()
+    out = torch.full_like(src, float("nan")) if out is None else out
+    kw = dict(more)
+    if groups:
+        kw |= {"group_start": R.i32([g[0] for g in groups] + [groups[-1][1]]),
+               "group_shared": R.i32([g[2] for g in groups])}
+    ea.attention_paged(C.rel(src), dev[0].rel, dev[1].rel, C.rel(out), scale=scale, table=R.i32(table),
+                       lengths=R.i32(lens), q_start=None if q_start is None else R.i32(q_start),
+                       k_scale=dev[0].scale_rel, v_scale=dev[1].scale_rel, **kw)
+    return out.view(t, hq, d) if form == "tokens" else out.transpose(0, 1)
+
+
+def _check(q, kv, table, lens, q_start, groups, code, dtype, scale=None, form="tokens", dev=None):
+    t, hq, d = q.shape
+    page = kv[0][0].shape[2]
+    scale = d ** -0.5 if scale is None else scale
+    dev = dev or [C.Cache(codes, s, code) for codes, s in kv]
+    got = _run(q, dev, table, lens, q_start, groups, scale, form=form)
+    starts = list(range(len(lens) + 1)) if q_start is None else q_start
+    ref, info = R.attention(R.f64(q), C.values(*kv[0]), C.values(*kv[1]), table, lens, page, starts, scale)
+    n = starts[-1]
+    R.check(R.f64(got)[:n], ref[:n], C.attention_tol(ref, info, dtype, d)[:n])
+    return got
+
+
+CASES = [
+    # lens, groups, n_q, hq, hkv, d, page, block, code, dtype
+    ([1], [], 1, 1, 1, 64, 16, 16, "e4m3", "bf16"),
+    ([0], [], 1, 4, 1, 128, 16, 4, "e5m2", "f16"),
+    ([0, 3, 0, 128, 129, 1], [], 1, 4, 2, 128, 16, 16, "e4m3", "bf16"),
+    ([700], [], 1, 8, 2, 128, 64, 64, "e4m3", "f16"),
+    ([333, 17, 1, 64], [], 1, 6, 2, 64, 20, 5, "e5m2", "f16"),
+    ([31, 32, 33, 127], [], 1, 5, 1, 128, 1, 1, "e4m3", "bf16"),
+    ([90, 45], [], 1, 40, 1, 64, 7, 1, "e4m3", "f16"),               # more heads a group than a tile's columns
+    ([90, 145], [], 1, 24, 1, 128, 16, 8, "e5m2", "bf16"),           # two column tiles
+    ([200, 210, 205], [(0, 3, 192)], 1, 4, 1, 128, 16, 16, "e4m3", "bf16"),
+    ([128, 128], [(0, 2, 128)], 1, 4, 1, 64, 16, 2, "e5m2", "f16"),  # nothing of their own
+    ([50, 300, 310, 290, 12], [(1, 4, 288)], 1, 8, 2, 128, 32, 32, "e5m2", "bf16"),
+    ([130, 140, 150, 60, 70], [(0, 3, 128), (3, 5, 48)], 1, 3, 3, 64, 16, 8, "e4m3", "bf16"),
+    ([40, 41, 42, 43], [(0, 2, 0), (2, 4, 40)], 1, 4, 2, 64, 8, 8, "e4m3", "f16"),  # a group that shares nothing
+    ([64, 100, 64], [(0, 3, 64)], 5, 8, 2, 64, 16, 16, "e4m3", "bf16"),  # drafts that end in the shared keys
+    ([3, 9, 1], [], 4, 4, 1, 128, 16, 16, "e4m3", "bf16"),           # more tokens than keys: rows that see none
+    ([300, 90], [], 30, 8, 2, 128, 16, 4, "e4m3", "f16"),            # many columns, nothing shared
+    ([300, 290], [(0, 2, 256)], 20, 8, 1, 128, 64, 16, "e5m2", "f16"),  # and both
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=[f"n{len(c[0])}_g{len(c[1])}_q{c[2]}_h{c[3]}_{c[4]}_d{c[5]}_p{c[6]}_b{c[7]}_"
+                                             f"{c[8]}_{c[9]}" for c in CASES])
+def test_paged8(case):
+    lens, groups, n_q, hq, hkv, d, page, block, code, dtype = case
+    kv, table, rng = _batch(lens, groups, page, block, hkv, d, code, 1)
+    q = torch.from_numpy(rng.standard_normal((len(lens) * n_q, hq, d))).to(R.TORCH[dtype]).cuda()
+    starts = None if n_q == 1 else [n_q * i for i in range(len(lens) + 1)]
+    _check(q, kv, table, lens, starts, groups, code, dtype)
+
+
+@pytest.mark.parametrize("code,dtype", [("e4m3", "bf16"), ("e5m2", "f16")])
+def test_ragged_query_rows_and_rows_behind(code, dtype):
+    """0, 1, 7 and 40 newest tokens a sequence; rows behind the last sequence
+    stay as they were; head-major q and out."""
+    lens, starts = [30, 5, 260, 40], [0, 0, 1, 41, 48]
+    kv, table, rng = _batch(lens, [], 16, 8, 2, 128, code, 2)
+    q = torch.from_numpy(rng.standard_normal((53, 4, 128))).to(R.TORCH[dtype]).cuda()
+    got = _check(q, kv, table, lens, starts, [], code, dtype, form="heads")
+    assert torch.isnan(got[48:].float()).all()
+
+
+@pytest.mark.parametrize("shared", [0, 6000])
+def test_long_walks_and_repeatable(shared):
+    """Long walks over many workgroups: against the definition, and the same
+    bits on every run."""
+    n, page, hkv, hq, d = 5, 16, 2, 8, 128
+    lens = [6000 + 40 * i + 1 for i in range(n)]
+    groups = [(0, n, shared)] if shared else []
+    kv, table, rng = _batch(lens, groups, page, page, hkv, d, "e4m3", 3)
+    q = torch.from_numpy(rng.standard_normal((n, hq, d))).bfloat16().cuda()
+    dev = [C.Cache(codes, s, "e4m3") for codes, s in kv]
+    got = _check(q, kv, table, lens, None, groups, "e4m3", "bf16", dev=dev)
+    for _ in range(3):
+        assert torch.equal(_run(q, dev, table, lens, None, groups, d ** -0.5), got)
+
+
+@pytest.mark.parametrize("big", [-100, -60, 60, 100])
+def test_scales_far_apart(big):
+    """V's scales near the ends of their range and 2^24 apart, K's so that the
+    scores stay in reach: the output is as large."""
+    lens, page, block, d = [70, 300], 16, 4, 64
+    kv, table, rng = _batch(lens, [], page, block, 1, d, "e4m3", 4, spread=12)
+    (kc, ks), (vc, vs) = kv
+    ks[...] = 2.0 ** rng.integers(-14, -8, ks.shape)
+    vs[...] = 2.0 ** (big + rng.integers(-12, 12, vs.shape))
+    q = torch.from_numpy(rng.standard_normal((2, 4, d))).bfloat16().cuda()
+    _check(q, kv, table, lens, None, [], "e4m3", "bf16")
+
+
+def _garbage(kv, table, lens, code, seed, number):
+    """NaN codes in all rows that nothing sees, and `number` for scales of
+    blocks without a row that is seen."""
+    (kc, ks), (vc, vs) = kv
+    page, block = kc.shape[2], kc.shape[2] // ks.shape[2]
+    seen = np.zeros((len(kc), page), bool)
+    for s, n in enumerate(lens):
+        for j in range(n):
+            seen[table[s, j // page], j % page] = True
+    blocks = seen.reshape(len(kc), -1, block).any(-1)
+    dirty = []
+    for codes, scale in kv:
+        c, s = codes.copy(), scale.copy()
+        c[np.broadcast_to(~seen[:, None, :, None], c.shape)] = np.nan
+        s[np.broadcast_to(~blocks[:, None], s.shape)] = number
+        dirty.append(C.Cache(c, s, code))
+    return dirty
+
+
+@pytest.mark.parametrize("number", [float("nan"), float("inf"), 3e38])
+@pytest.mark.parametrize("case", [0, 1, 2])
+def test_what_nothing_sees_does_not_matter(case, number):
+    lens, groups, n_q, hq, hkv, d, page, block, code, dtype = [
+        ([33, 1, 150], [], 1, 4, 2, 128, 16, 4, "e4m3", "bf16"),
+        ([70, 90, 80], [(0, 3, 64)], 5, 8, 2, 64, 16, 8, "e5m2", "f16"),
+        ([300, 90], [], 30, 8, 2, 128, 20, 1, "e4m3", "bf16"),
+    ][case]
+    kv, table, rng = _batch(lens, groups, page, block, hkv, d, code, 5, spare=6)
+    table[0, -1] = 10 ** 6  # behind the keys: not read
+    q = torch.from_numpy(rng.standard_normal((len(lens) * n_q, hq, d))).to(R.TORCH[dtype]).cuda()
+    starts = [n_q * i for i in range(len(lens) + 1)]
+    _check(q, kv, table, lens, starts, groups, code, dtype, dev=_garbage(kv, table, lens, code, 6, number))
+
+
+@pytest.mark.parametrize("walk", ["few", "many", "both"])
+@pytest.mark.parametrize("code", ["e4m3", "e5m2"])
+def test_what_one_row_sees_another_does_not(walk, code):
+    """The last key of a draft, seen by the last row alone: NaN in an element of
+    its V, in its V's scale, in its K, infinities in V (e5m2): the other rows are
+    as without; the last row's element, or row, shows them."""
+    n_q, hq, d, page = {"few": 3, "many": 20, "both": 5}[walk], 4, 128, 16
+    lens = [200, 170]
+    groups = [(0, 2, 160)] if walk == "both" else []
+    if walk == "both":  # the last shared key is the last that a first draft sees
+        lens = [160, 170]
+    kv, table, rng = _batch(lens, groups, page, 1, 1, d, code, 7)
+    q = torch.from_numpy(rng.standard_normal((2 * n_q, hq, d))).bfloat16().cuda()
+    starts = [0, n_q, 2 * n_q]
+    clean = _check(q, kv, table, lens, starts, groups, code, "bf16")
+    last = lens[0] - 1
+    pg, row = table[0, last // page], last % page
+    # (shared pages are the other sequence's too: its rows all see that key)
+    others = [i for i in range(2 * n_q) if i != n_q - 1 and (walk != "both" or i < n_q)]
+    for what in ["code", "scale", "key"] + (["inf"] if code == "e5m2" else []):
+        dev = []
+        for i, (codes, scale) in enumerate(kv):
+            c, s = codes.copy(), scale.copy()
+            if what == "code" and i == 1:
+                c[pg, 0, row, 9] = np.nan
+            if what == "inf" and i == 1:
+                c[pg, 0, row, 9] = -np.inf
+            if what == "scale" and i == 1:
+                s[pg, 0, row] = np.nan
+            if what == "key" and i == 0:
+                c[pg, 0, row, 3] = np.nan
+            dev.append(C.Cache(c, s, code))
+        got = _run(q, dev, table, lens, starts, groups, d ** -0.5)
+        assert torch.equal(got[others], clean[others]), what
+        mine = got[n_q - 1].float()
+        if what == "code":
+            assert mine[:, 9].isnan().all() and torch.equal(got[n_q - 1, :, 10:], clean[n_q - 1, :, 10:])
+        elif what == "inf":
+            assert (mine[:, 9] == -float("inf")).all() and torch.equal(got[n_q - 1, :, :9], clean[n_q - 1, :, :9])
+        else:
+            assert mine.isnan().all()
+
+
+def test_pages_outside_the_cache_are_invisible():
+    lens, page = [100, 64], 16
+    kv, table, rng = _batch(lens, [], page, 16, 2, 64, "e4m3", 8)
+    table[0, 2], table[1, 0] = -5, len(kv[0][0])
+    q = torch.from_numpy(rng.standard_normal((2, 4, 64))).bfloat16().cuda()
+    _check(q, kv, table, lens, None, [], "e4m3", "bf16")
+    _check(q, kv, table, [10 ** 9, -3], None, [], "e4m3", "bf16")  # a table row's keys; none
+
+
+def test_as_sixteen_bits():
+    """Codes and scales of a bf16 cache's values exactly: both calls agree within
+    what they may each be off."""
+    lens, page, hq, hkv, d = [500, 77, 1300], 32, 8, 2, 128
+    kv, table, rng = _batch(lens, [], page, page, hkv, d, "e4m3", 9)
+    for i, (codes, scale) in enumerate(kv):
+        scale[...] = 2.0 ** -8
+    q = torch.from_numpy(rng.standard_normal((3, hq, d))).bfloat16().cuda()
+    got = _check(q, kv, table, lens, None, [], "e4m3", "bf16")
+    wide = [R.pages_rel(torch.from_numpy(C.values(*x)).bfloat16().cuda()) for x in kv]
+    src, out = q.reshape(3, -1), torch.empty(3, hq * d, dtype=torch.bfloat16, device="cuda")
+    ea.attention_paged(R.rel(src), *wide, R.rel(out), scale=d ** -0.5, table=R.i32(table), lengths=R.i32(lens))
+    ref, info = R.attention(R.f64(q), C.values(*kv[0]), C.values(*kv[1]), table, lens, page, [0, 1, 2, 3], d ** -0.5)
+    assert np.all(np.abs(R.f64(got) - R.f64(out).reshape(ref.shape)) <= 2 * C.attention_tol(ref, info, "bf16", d))
+
+
+def test_codes_past_four_gib():
+    """Pages at both ends of caches of more than 2^32 bytes."""
+    page, hkv, d, pages = 64, 8, 128, 66000
+    lens = [300, 40]
+    kv, table, rng = _batch(lens, [], page, 16, hkv, d, "e4m3", 10)
+    n = len(kv[0][0])
+    where = np.array([pages - 1 - i if i % 2 else i for i in range(n)])
+    part = [range(pages + 1), [0, hkv], [0, page], [0, d]]
+    rels, scales = [], []
+    for codes, scale in kv:
+        r = ea.Relation((pages, hkv, page, d), "e4m3", part)
+        assert r.nbytes > 2 ** 32
+        r.data.view(pages, -1)[torch.from_numpy(where).cuda()] = C.code_tensor(codes, "e4m3").view(torch.uint8).view(n, -1)
+        s = torch.zeros(pages, hkv, page // 16, device="cuda")
+        s[torch.from_numpy(where).cuda()] = torch.from_numpy(scale).float().cuda()
+        rels.append(r)
+        scales.append(C.rel(s))
+    q = torch.from_numpy(rng.standard_normal((2, 2 * hkv, d))).bfloat16().cuda()
+    out = torch.empty_like(q)
+    far = np.where(table >= 0, where[np.maximum(table, 0)], -1)
+    ea.attention_paged(C.rel(q.view(2, -1)), *rels, C.rel(out.view(2, -1)), scale=0.1, table=R.i32(far),
+                       lengths=R.i32(lens), k_scale=scales[0], v_scale=scales[1])
+    ref, info = R.attention(R.f64(q), C.values(*kv[0]), C.values(*kv[1]), table, lens, page, [0, 1, 2], 0.1)
+    R.check(R.f64(out), ref, C.attention_tol(ref, info, "bf16", d))
+
+
+def test_captured_calls_follow_lengths_with_workspaces_of_their_own():
+    """Two captured calls on two streams, replayed together while lengths grow:
+    the bits of eager calls, every replay."""
+    lens, page, hq, hkv, d = [[500, 3, 40], [7, 2000, 64]], 16, 8, 2, 128
+    sets = []
+    for i in range(2):
+        kv, table, rng = _batch([n + 40 for n in lens[i]], [], page, 8, hkv, d, ["e4m3", "e5m2"][i], 11 + i)
+        dev = [C.Cache(codes, s, ["e4m3", "e5m2"][i]) for codes, s in kv]
+        q = torch.from_numpy(rng.standard_normal((3, hq, d))).bfloat16().cuda().view(3, -1)
+        out = torch.empty_like(q)
+        at = R.i32(lens[i])
+        ws = ea.new_workspace(ea.attention_paged_workspace(C.rel(q), dev[0].rel, 3))
+        sets.append((dev, q, out, at, R.i32(table), ws, [C.rel(q), dev[0].rel, dev[1].rel, C.rel(out)]))
+
+    def call(s, out=None, ws=None):
+        dev, q, o, at, table, w, rels = s
+        rels = rels if out is None else rels[:3] + [C.rel(out)]
+        ea.attention_paged(*rels, scale=0.1, table=table, lengths=at, k_scale=dev[0].scale_rel, v_scale=dev[1].scale_rel,
+                           workspace=w if ws is None else ws)
+
+    streams, graphs = [torch.cuda.Stream() for _ in sets], []
+    torch.cuda.synchronize()
+    for s, st in zip(sets, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            s[3].add_(1)
+            call(s)
+        graphs.append(g)
+    for _ in range(6):
+        torch.cuda.synchronize()
+        for st, g in zip(streams, graphs):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        for s in sets:
+            want = torch.empty_like(s[2])
+            call(s, want, ea.new_workspace(s[5].numel()))
+            assert torch.equal(s[2], want) and want.isfinite().all()
+            assert not s[5][:ea.WS_COUNTER_BYTES].any()
