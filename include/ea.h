@@ -575,9 +575,10 @@ int ea_pages_write(const ea_relation* xk, const ea_relation* xv, ea_relation* k,
    sequence stay as they were. */
 int ea_pages_read(const ea_relation* k, const ea_relation* v, const ea_relation* k_scale, const ea_relation* v_scale,
                   ea_relation* xk, ea_relation* xv, const ea_page_rows* rows, void* stream);
-/* ea_attention_paged over such a cache, of keys and values code * scale (any
-   finite scales).  q and out are bf16 or f16; the weights' products with V take
-   them as two bf16 values.  Everything else, the workspace and its size's call
+/* ea_attention_paged over such a cache, of keys and values code * scale.  Scales
+   are powers of two, as ea_pages_write gives them; any other stands for NaN.
+   q and out are bf16 or f16; the weights' products with V take them as two bf16
+   values.  Everything else, the workspace and its size's call
    among it, is as there. */
 int ea_attention_paged8(const ea_relation* q, const ea_relation* k, const ea_relation* v, const ea_relation* k_scale,
                         const ea_relation* v_scale, ea_relation* out, const ea_paged* batch, void* workspace,

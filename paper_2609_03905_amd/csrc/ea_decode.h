@@ -95,6 +95,7 @@ hipError_t launch_heads_grad(const HeadsGradArgs& a, int32_t dtype, hipStream_t 
 constexpr int kPagedCols = 16;      // query columns of a matrix tile
 constexpr int kPagedStep = 128;     // keys that a workgroup takes at a time
 constexpr int kPagedWideStep = 64;  // and with many columns
+constexpr int kPaged8Step = 256;    // a cache in 8 bits, few columns
 
 struct PagedSeg {  // what the join needs of a segment
   int32_t r0, r1;       // query rows

@@ -104,12 +104,6 @@ __device__ __forceinline__ Segment segment(const PagedArgs& a, int i) {
   return s;
 }
 
-// Keys of a step of a walk over tiles of COLS columns.
-template <int COLS>
-__device__ __forceinline__ constexpr int step_keys() {
-  return COLS <= 32 ? kPagedStep : kPagedWideStep;
-}
-
 // A segment as the walk needs it, kept in shared memory (one more at the end
 // holds the totals).
 struct Seg {
@@ -141,9 +135,9 @@ __device__ __forceinline__ int tiles_of(int rows, int g, int cols) {
 
 // Every segment's first step and tile, by the whole workgroup: the groups' (none
 // where SHARED is 0) and the sequences', whose loads are one round trip.  *to and
-// *ts: the steps of all; none where there are more tiles than the rows can have,
+// *ts: the steps (of OWN_KEYS and SHARED_KEYS keys) of all; none where there are more tiles than the rows can have,
 // that is, where the sequences' rows overlap.
-template <int OWN, int SHARED>
+template <int OWN, int OWN_KEYS, int SHARED, int SHARED_KEYS>
 __device__ __forceinline__ void schedule(const PagedArgs& a, const PagedPass& own, const PagedPass& shared, Seg* seg_o,
                                          Seg* seg_s, int* to, int* ts) {
   constexpr int N = SHARED ? 4 : 2;  // steps and tiles of the sequences, and of the groups
@@ -156,7 +150,7 @@ __device__ __forceinline__ void schedule(const PagedArgs& a, const PagedPass& ow
   for (int i = i0; i < i1; ++i) {
     const bool g = SHARED && i < ng;
     const Segment s = segment(a, i);
-    const int keys = g ? step_keys<SHARED>() : step_keys<OWN>(), cols = g ? SHARED : OWN;
+    const int keys = g ? SHARED_KEYS : OWN_KEYS, cols = g ? SHARED : OWN;
     const int steps = steps_of(s.k0, s.k1, keys);
     const int64_t tiles = steps ? (((int64_t)(s.r1 - s.r0) * a.g + cols - 1) / cols) * a.hkv : 0;
     Seg x;

@@ -79,6 +79,12 @@ __device__ __forceinline__ void add_odd(uint32_t w, float& lo, float& hi) {
   hi += __builtin_isfinite(b) ? 0.0f : b;
 }
 
+// Keys of a step of a walk over tiles of COLS columns.
+template <int COLS>
+__device__ __forceinline__ constexpr int step_keys() {
+  return COLS <= 32 ? kPagedStep : kPagedWideStep;
+}
+
 // Shared memory of the two walks.
 template <int D>
 struct __attribute__((aligned(16))) FewShared {
@@ -773,7 +779,7 @@ __global__ __launch_bounds__(kThreads, COLS == 32 && D == 128 ? 1 : 2) void page
   extern __shared__ __attribute__((aligned(16))) char dyn[];
   Seg* seg = reinterpret_cast<Seg*>(dyn);
   int total;
-  schedule<COLS, 0>(a, ps, ps, seg, nullptr, &total, nullptr);
+  schedule<COLS, step_keys<COLS>(), 0, 1>(a, ps, ps, seg, nullptr, &total, nullptr);
   const int parts = min(ps.grid, total);
   if (ps.fused) clear_empty<D>(a, ps, seg);
   else publish<COLS, step_keys<COLS>()>(a, ps, seg, total, parts, blockIdx.x, gridDim.x);
@@ -802,7 +808,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_both_kernel(const PagedArgs
   } sh;
   constexpr int KO = step_keys<OWN>(), KS = step_keys<SHARED>();
   int to, ts;
-  schedule<OWN, SHARED>(a, own, shared, seg_o, seg_s, &to, &ts);
+  schedule<OWN, KO, SHARED, KS>(a, own, shared, seg_o, seg_s, &to, &ts);
   const int n = gridDim.x;
   // by the bytes that the walks read (with the measured times of their steps and
   // of beginning and ending a walk instead: 8K prefix 43 us against 40); in

@@ -2,10 +2,13 @@
 // ea_paged.hip).  With codes c and scales k_j, v_j of a key's blocks,
 //   O = sum_j w_j v_j cv_j / sum_j w_j,   w_j = 2^(s_j - m),
 //   s_j = scale log2(e) k_j q.ck_j
-// Codes are exact in bf16 and in fp16: they are widened on their way to the
-// matrix cores, K's to q's type, V's to bf16, and the scales, one a key, enter in
-// f32: k_j a score, v_j a weight.  The weights w_j v_j, whose exponents are as far
-// apart as f32's, go to the product as two bf16 values.
+// Codes are widened on their way to the matrix cores, K's to q's type, V's to bf16.
+// A scale is a power of two, and a code has at most four significant bits: c s is
+// exact in bf16, so that there the widening instruction applies the scale.  Where
+// it does not, the scales enter in f32: k_j a score (fp16 queries), v_j a weight
+// (the walk over few columns, which widens the codes of two keys at once).  The
+// weights, whose exponents may be as far apart as f32's, go to the product with V
+// as two bf16 values.
 #pragma once
 
 #include "ea_paged.h"
@@ -16,18 +19,28 @@ namespace {
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
-// Two codes of a word, the lower or the upper, as two values of a type.
+// Two codes of a word, the lower or the upper, times a power of two, as two values
+// of a type.  (The instruction takes the scale's exponent alone; NaN gives NaN.
+// Every code times every power from 2^-120 to 2^120 was compared: exact, bf16's
+// subnormal numbers among them, which the matrix cores take as they are.)
 template <bool BF, bool E5, bool UP>
-__device__ __forceinline__ uint32_t widen2(uint32_t w) {
-  if constexpr (BF && E5) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, UP));
-  else if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, UP));
-  else if constexpr (E5) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w, 1.0f, UP));
-  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, UP));
+__device__ __forceinline__ uint32_t widen2(uint32_t w, float s) {
+  if constexpr (BF && E5) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, UP));
+  else if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, UP));
+  else if constexpr (E5) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w, s, UP));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, UP));
 }
 template <bool BF, bool E5>
-__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b) {
-  return make_uint4(widen2<BF, E5, false>(a), widen2<BF, E5, true>(a), widen2<BF, E5, false>(b),
-                    widen2<BF, E5, true>(b));
+__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b, float s) {
+  return make_uint4(widen2<BF, E5, false>(a, s), widen2<BF, E5, true>(a, s), widen2<BF, E5, false>(b, s),
+                    widen2<BF, E5, true>(b, s));
+}
+
+// A scale, NaN where it is no power of two of its range: what such a scale stands
+// for shows in every row that sees it.
+__device__ __forceinline__ float power_of_two(float s) {
+  const uint32_t b = __float_as_uint(s);
+  return (b & 0x807fffffu) == 0 && b - 0x00800000u < 0x7f000000u ? s : NAN;
 }
 
 // 0 V is no number where V is not finite, and a column that does not see a value
@@ -59,8 +72,8 @@ __device__ __forceinline__ void add_odd4(uint32_t w, float (&x)[4]) {
 // Shared memory of the two walks.
 template <int D>
 struct __attribute__((aligned(16))) Few8Shared {
-  int64_t off[kWaves][2][32];
-  float scale[kWaves][2][32];  // of a step's keys: K's, V's
+  int64_t off[kWaves][2][kPaged8Step / kWaves];
+  float scale[kWaves][2][kPaged8Step / kWaves];  // of a step's keys: K's, V's
   float o[kWaves][kPagedCols][D + 4];
   float ml[kWaves][kPagedCols][2];
   int last;
@@ -69,37 +82,40 @@ template <int D>
 struct __attribute__((aligned(1024))) Many8Shared {
   uint16_t kv[2][2 * kPagedWideStep * D];  // two steps' buffers: K, then V
   int64_t off[2][kPagedWideStep];
-  float scale[2][2][kPagedWideStep];
-  int odd[2][kWaves];
+  float ks[2][kPagedWideStep];   // K's scales (fp16 queries)
+  int no_vs[2][kPagedWideStep];  // whether a V row's scale is none
+  int odd[2][kWaves];            // whether a wave found such a scale, or codes that are not finite
 };
 
-// Few columns: each wave walks its own 32 keys of a step of 128, codes from the
+// Few columns: each wave walks its own 64 keys of a step of 256, codes from the
 // pages to registers.
 //   S^T = K Q^T     (16x16x32: A = 16 keys x 32 d, B = 32 d x 16 columns)
 //   O^T += V^T P^T  (A = 16 d x 32 keys, B = 32 keys x 16 columns)
 // A lane's 16 bytes of a K row are two steps' k indices, Q's are taken alike.  A V
-// row's lane has D / 16 neighbouring codes of each of the eight keys whose scores
-// its column's accumulators hold; a byte permutation puts two keys' codes of one d
-// side by side, and widening them gives the operand.
+// row's lane has D / 16 neighbouring codes of each of the sixteen keys whose
+// scores its column's accumulators hold; a byte permutation puts two keys' codes of
+// one d side by side, and widening them gives the operand.
 template <int D, bool BF, bool E5, int COLS>
 __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& ps, const Seg* seg, Few8Shared<D>& sh,
                                           int total, int parts, int block) {
   constexpr int NC = COLS / kPagedCols;
-  constexpr int VE = D / 16;  // codes a lane holds of a V row
-  constexpr int KL = D / 64;  // loads of 16 codes of a K row
-  auto& s_off = sh.off;
+  constexpr int VE = D / 16;                // codes a lane holds of a V row
+  constexpr int KL = D / 64;                // loads of 16 codes of a K row
+  constexpr int NK = kPaged8Step / kWaves;  // keys of a wave's step
+  constexpr int NT = NK / 16;               // and tiles of 16 of them
 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g4 = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int w = xcd_part(block, parts);
   int at = (int)((int64_t)total * w / parts);
   const int end = (int)((int64_t)total * (w + 1) / parts);
+  static_assert(NK == 64, "a lane a key");
 
   auto next_piece = [&]() {
     Piece p;
     p.si = find_segment(seg, ps.n, at);
     p.s = seg[p.si];
-    p.n = steps_of(p.s.k0, p.s.k1, kPagedStep);
+    p.n = steps_of(p.s.k0, p.s.k1, kPaged8Step);
     const int tiles = tiles_of(p.s.rows, a.g, COLS);
     const int local = at - p.s.step, step = local % p.n;
     p.it = local / p.n;
@@ -107,34 +123,35 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
     p.tile = p.it - p.h * tiles;
     const int walk = min(p.n - step, end - at);
     p.whole = walk == p.n && p.s.k0 == 0;
-    p.ka = p.s.k0 + step * kPagedStep;
-    p.kb = (int)min((int64_t)p.s.k1, (int64_t)p.ka + (int64_t)walk * kPagedStep);
+    p.ka = p.s.k0 + step * kPaged8Step;
+    p.kb = (int)min((int64_t)p.s.k1, (int64_t)p.ka + (int64_t)walk * kPaged8Step);
     p.pages = a.table + (int64_t)p.s.seq * a.stride;
     p.head_off = (int64_t)p.h * a.page_size * D;
     at += walk;
     return p;
   };
-  // a wave's step is 32 keys; lane i looks after key i, its row's place and K's
-  // scale, lane i + 32 after V's
-  const int kl = lane & 31;
-  const float* scales = lane < 32 ? a.ks : a.vs;
-  auto entry = [&](const Piece& p, int k) { return k + kl < p.kb ? p.pages[div_fast(k + kl, a.page)] : -1; };
-  auto place = [&](const Piece& p, int slot, int k, int pg) {  // the rows' offsets (-1: no such row); the scale
-    const int key = k + kl, in = key - div_fast(key, a.page) * a.page_size;
-    const bool there = (uint32_t)pg < (uint32_t)a.n_pages;
-    const int64_t off = there ? pg * a.page_bytes + (int64_t)in * D : -1;
-    if (lane < 32) s_off[wid][slot][kl] = off;
-    __builtin_amdgcn_wave_barrier();
-    return there ? scales[((int64_t)pg * a.hkv + p.h) * a.n_blocks + div_fast(in, a.block)] : 0.0f;
+  // What a step's lane knows of its key: the row's place goes to shared memory
+  // (any row's, if the key has none), the scales follow a step later.
+  struct Keys {
+    uint64_t there;  // keys that have a row
+    float ks, vs;    // this lane's key's scales
   };
-  uint4 kr[2][KL];
-  uint32_t vr[8][VE / 4];
+  auto entry = [&](const Piece& p, int k) { return k + lane < p.kb ? p.pages[div_fast(k + lane, a.page)] : -1; };
+  auto place = [&](const Piece& p, int slot, int k, int pg) {
+    const int key = k + lane, in = key - div_fast(key, a.page) * a.page_size;
+    const bool there = (uint32_t)pg < (uint32_t)a.n_pages;
+    sh.off[wid][slot][lane] = there ? pg * a.page_bytes + (int64_t)in * D : 0;
+    __builtin_amdgcn_wave_barrier();
+    const int64_t i = there ? ((int64_t)pg * a.hkv + p.h) * a.n_blocks + div_fast(in, a.block) : 0;
+    return Keys{__ballot(there), a.ks[i], a.vs[i]};
+  };
+  uint4 kr[NT][KL];
+  uint32_t vr[4 * NT][VE / 4];
   auto load_k = [&](const Piece& pc, int slot) {
     const char* base = a.pk + pc.head_off + g4 * 16;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int64_t off = s_off[wid][slot][16 * t + c];
-      const char* p = base + (off < 0 ? 0 : off);
+    for (int t = 0; t < NT; ++t) {
+      const char* p = base + sh.off[wid][slot][16 * t + c];
 #pragma unroll
       for (int i = 0; i < KL; ++i) kr[t][i] = *reinterpret_cast<const uint4*>(p + i * 64);
     }
@@ -142,9 +159,8 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
   auto load_v = [&](const Piece& pc, int slot) {
     const char* base = a.pv + pc.head_off + c * VE;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t off = s_off[wid][slot][16 * (i >> 2) + 4 * g4 + (i & 3)];
-      const char* p = base + (off < 0 ? 0 : off);
+    for (int i = 0; i < 4 * NT; ++i) {
+      const char* p = base + sh.off[wid][slot][16 * (i >> 2) + 4 * g4 + (i & 3)];
       if constexpr (VE == 8) {
         const uint2 x = *reinterpret_cast<const uint2*>(p);
         vr[i][0] = x.x, vr[i][1] = x.y;
@@ -168,9 +184,9 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
   // The loads of a step are on their way while the step before is computed, also
   // from one piece to the next.
   Piece next = next_piece();
-  int slot = 0, next_pg = entry(next, next.ka + wid * 32);
+  int slot = 0, next_pg = entry(next, next.ka + wid * NK);
   load_q(next);
-  float next_scale = place(next, 0, next.ka + wid * 32, next_pg);
+  Keys keys = place(next, 0, next.ka + wid * NK, next_pg);
   load_k(next, 0);
   load_v(next, 0);
   bool have = true;
@@ -204,67 +220,86 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
 #pragma unroll
       for (int j = 0; j < VE; ++j) acc[t][j] = f32x4_t{};
     }
-    int k = cur.ka + wid * 32;
-    next_pg = entry(cur, k + kPagedStep);
-    for (bool again = true; again; k += kPagedStep) {
-      again = k + kPagedStep < kb;
+    int k = cur.ka + wid * NK;
+    next_pg = entry(cur, k + kPaged8Step);
+    for (bool again = true; again; k += kPaged8Step) {
+      again = k + kPaged8Step < kb;
+      const uint64_t there = keys.there;
       // every key of the step has a row and is seen by every column
-      const bool full = __all(s_off[wid][slot][kl] >= 0) && k + 32 <= lim_min;
-      sh.scale[wid][lane >> 5][kl] = next_scale;
+      const bool full = there == ~uint64_t(0) && k + NK <= lim_min;
+      sh.scale[wid][0][lane] = power_of_two(keys.ks);
+      sh.scale[wid][1][lane] = power_of_two(keys.vs);
       __builtin_amdgcn_wave_barrier();
       if (again) {
-        next_scale = place(cur, slot ^ 1, k + kPagedStep, next_pg);
-        next_pg = entry(cur, k + 2 * kPagedStep);
+        keys = place(cur, slot ^ 1, k + kPaged8Step, next_pg);
+        next_pg = entry(cur, k + 2 * kPaged8Step);
       } else if (have) {
-        next_scale = place(next, slot ^ 1, next.ka + wid * 32, entry(next, next.ka + wid * 32));
+        keys = place(next, slot ^ 1, next.ka + wid * NK, entry(next, next.ka + wid * NK));
       }
-      f32x4_t sc[NC][2];
+      f32x4_t sc[NC][NT];
 #pragma unroll
-      for (int t = 0; t < NC; ++t) sc[t][0] = sc[t][1] = f32x4_t{};
+      for (int u = 0; u < NT; ++u) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+        for (int t = 0; t < NC; ++t) sc[t][u] = f32x4_t{};
+        const float ks = BF ? sh.scale[wid][0][16 * u + c] : 1.0f;
 #pragma unroll
         for (int i = 0; i < KL; ++i) {
-          const uint4 k0 = widen8<BF, E5>(kr[u][i].x, kr[u][i].y), k1 = widen8<BF, E5>(kr[u][i].z, kr[u][i].w);
+          const uint4 k0 = widen8<BF, E5>(kr[u][i].x, kr[u][i].y, ks), k1 = widen8<BF, E5>(kr[u][i].z, kr[u][i].w, ks);
 #pragma unroll
           for (int t = 0; t < NC; ++t) {
             sc[t][u] = mfma16<BF>(k0, q[t][2 * i], sc[t][u]);
             sc[t][u] = mfma16<BF>(k1, q[t][2 * i + 1], sc[t][u]);
           }
         }
+      }
       if (again) load_k(cur, slot ^ 1);
       else if (have) load_k(next, slot ^ 1);
-      f32x4_t vs[2];
+      if constexpr (!BF) {  // (a scaled code may be out of fp16's reach)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&sh.scale[wid][0][16 * u + 4 * g4]);
-        vs[u] = *reinterpret_cast<const f32x4_t*>(&sh.scale[wid][1][16 * u + 4 * g4]);
+        for (int u = 0; u < NT; ++u) {
+          const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&sh.scale[wid][0][16 * u + 4 * g4]);
 #pragma unroll
-        for (int t = 0; t < NC; ++t)
+          for (int t = 0; t < NC; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sc[t][u][i] *= ks[i];
+            for (int i = 0; i < 4; ++i) sc[t][u][i] *= ks[i];
+        }
       }
+      uint32_t odd = 0;
       if (!full) {
+        const uint64_t mine = there >> (4 * g4);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int kk = 16 * (i >> 2) + 4 * g4 + (i & 3);
-          const bool row_there = s_off[wid][slot][kk] >= 0;
+        for (int i = 0; i < 4 * NT; ++i) {
+          const bool row_there = mine >> (16 * (i >> 2) + (i & 3)) & 1;
 #pragma unroll
           for (int t = 0; t < NC; ++t) {
             const float x = sc[t][i >> 2][i & 3];
-            sc[t][i >> 2][i & 3] = row_there && k + kk < lim[t] ? x : -INFINITY;
+            sc[t][i >> 2][i & 3] = row_there && k + 16 * (i >> 2) + 4 * g4 + (i & 3) < lim[t] ? x : -INFINITY;
           }
           // a row that is not there was read elsewhere: it may hold anything
 #pragma unroll
           for (int j = 0; j < VE / 4; ++j) vr[i][j] = row_there ? vr[i][j] : 0u;
         }
       }
-      uint4 p[NC], p2[NC];
+      // (where every column sees every key, NaN times its weight is right as it
+      // is, but an infinity's second weight may be 0)
+      if (E5 || !full) {
+#pragma unroll
+        for (int i = 0; i < 4 * NT; ++i)
+#pragma unroll
+          for (int j = 0; j < VE / 4; ++j) odd |= odd_codes<E5>(vr[i][j]);
+        if (__builtin_expect(__any(odd != 0), 0)) {
+#pragma unroll
+          for (int i = 0; i < 4 * NT; ++i)
+#pragma unroll
+            for (int j = 0; j < VE / 4; ++j) vr[i][j] = even_codes<E5>(vr[i][j]);
+        }
+      }
+      uint4 p[NC][NT / 2], p2[NC][NT / 2];
 #pragma unroll
       for (int t = 0; t < NC; ++t) {
         float mx = sc[t][0][0];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) mx = fmaxf(mx, sc[t][i >> 2][i & 3]);
+        for (int i = 1; i < 4 * NT; ++i) mx = fmaxf(mx, sc[t][i >> 2][i & 3]);
         mx = fmaxf(mx, other16(mx));
         mx = fmaxf(mx, other32(mx)) * a.scale;
         const float m_new = mx > m[t] + kLazyMax || m[t] == -INFINITY ? fmaxf(mx, m[t]) : m[t];
@@ -276,58 +311,57 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
           for (int j = 0; j < VE; ++j) acc[t][j] *= alpha;
         }
         m[t] = m_new;
-        float x[8];
+        float x[4 * NT];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i >> 2][i & 3], a.scale, -m_use));
-        l[t] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-        if (full) {
+        for (int i = 0; i < 4 * NT; ++i)
+          x[i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i >> 2][i & 3], a.scale, -m_use));
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] *= vs[i >> 2][i & 3];
-        } else {  // (the scale of a key that is not seen may be anything)
+        for (int i = 0; i < 4 * NT; i += 4) l[t] += (x[i] + x[i + 1]) + (x[i + 2] + x[i + 3]);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = x[i] == 0.0f ? 0.0f : x[i] * vs[i >> 2][i & 3];
+        for (int u = 0; u < NT; ++u) {
+          const f32x4_t vs = *reinterpret_cast<const f32x4_t*>(&sh.scale[wid][1][16 * u + 4 * g4]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[4 * u + i] *= vs[i];
         }
-        split_p<true>(x[0], x[1], p[t].x, p2[t].x);
-        split_p<true>(x[2], x[3], p[t].y, p2[t].y);
-        split_p<true>(x[4], x[5], p[t].z, p2[t].z);
-        split_p<true>(x[6], x[7], p[t].w, p2[t].w);
-      }
-      uint32_t odd = 0;
+        if (!full) {  // (the scale of a key that is not seen may be anything)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < 4 * NT; ++i) x[i] = sc[t][i >> 2][i & 3] == -INFINITY ? 0.0f : x[i];
+        }
 #pragma unroll
-        for (int j = 0; j < VE / 4; ++j) odd |= odd_codes<E5>(vr[i][j]);
-      if (__builtin_expect(__any(odd != 0), 0)) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int j = 0; j < VE / 4; ++j) vr[i][j] = even_codes<E5>(vr[i][j]);
-      }
-#pragma unroll
-      for (int j = 0; j < VE; j += 2) {
-        // d j and j + 1 of two keys a word
-        const uint32_t sel = j & 2 ? 0x07030602u : 0x05010400u;
-        uint32_t x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_perm(vr[2 * i + 1][j / 4], vr[2 * i][j / 4], sel);
-        const uint4 v0 = make_uint4(widen2<true, E5, false>(x[0]), widen2<true, E5, false>(x[1]),
-                                    widen2<true, E5, false>(x[2]), widen2<true, E5, false>(x[3]));
-        const uint4 v1 = make_uint4(widen2<true, E5, true>(x[0]), widen2<true, E5, true>(x[1]),
-                                    widen2<true, E5, true>(x[2]), widen2<true, E5, true>(x[3]));
-#pragma unroll
-        for (int t = 0; t < NC; ++t) {
-          acc[t][j] = mfma16<true>(v0, p[t], acc[t][j]);
-          acc[t][j] = mfma16<true>(v0, p2[t], acc[t][j]);
-          acc[t][j + 1] = mfma16<true>(v1, p[t], acc[t][j + 1]);
-          acc[t][j + 1] = mfma16<true>(v1, p2[t], acc[t][j + 1]);
+        for (int u = 0; u < NT / 2; ++u) {
+          split_p<true>(x[8 * u], x[8 * u + 1], p[t][u].x, p2[t][u].x);
+          split_p<true>(x[8 * u + 2], x[8 * u + 3], p[t][u].y, p2[t][u].y);
+          split_p<true>(x[8 * u + 4], x[8 * u + 5], p[t][u].z, p2[t][u].z);
+          split_p<true>(x[8 * u + 6], x[8 * u + 7], p[t][u].w, p2[t][u].w);
         }
       }
+#pragma unroll
+      for (int j = 0; j < VE; j += 2)
+#pragma unroll
+        for (int u = 0; u < NT / 2; ++u) {
+          // d j and j + 1 of two keys a word
+          const uint32_t sel = j & 2 ? 0x07030602u : 0x05010400u;
+          uint32_t x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[i] = __builtin_amdgcn_perm(vr[8 * u + 2 * i + 1][j / 4], vr[8 * u + 2 * i][j / 4], sel);
+          const uint4 v0 = make_uint4(widen2<true, E5, false>(x[0], 1.0f), widen2<true, E5, false>(x[1], 1.0f),
+                                      widen2<true, E5, false>(x[2], 1.0f), widen2<true, E5, false>(x[3], 1.0f));
+          const uint4 v1 = make_uint4(widen2<true, E5, true>(x[0], 1.0f), widen2<true, E5, true>(x[1], 1.0f),
+                                      widen2<true, E5, true>(x[2], 1.0f), widen2<true, E5, true>(x[3], 1.0f));
+#pragma unroll
+          for (int t = 0; t < NC; ++t) {
+            acc[t][j] = mfma16<true>(v0, p[t][u], acc[t][j]);
+            acc[t][j + 1] = mfma16<true>(v1, p[t][u], acc[t][j + 1]);
+            acc[t][j] = mfma16<true>(v0, p2[t][u], acc[t][j]);
+            acc[t][j + 1] = mfma16<true>(v1, p2[t][u], acc[t][j + 1]);
+          }
+        }
       if (__builtin_expect(__any(odd != 0), 0)) {
 #pragma unroll 1
-        for (int kk = 0; kk < 32; ++kk) {
-          const int64_t off = s_off[wid][slot][kk];
-          if (off < 0) continue;
-          const char* row = a.pv + cur.head_off + off;
+        for (int kk = 0; kk < NK; ++kk) {
+          if (!(there >> kk & 1)) continue;
+          const char* row = a.pv + cur.head_off + sh.off[wid][slot][kk];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -402,7 +436,7 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
       const int64_t off = there ? pg * a.page_bytes + (int64_t)in * D : -1;
       if (lane < 16) s_off[b][my] = off;
       __builtin_amdgcn_wave_barrier();
-      return there ? scales[((int64_t)pg * a.hkv + h) * a.n_blocks + div_fast(in, a.block)] : 0.0f;
+      return there ? scales[((int64_t)pg * a.hkv + h) * a.n_blocks + div_fast(in, a.block)] : 1.0f;
     };
     uint4 kr[LPW], vr[LPW];
     float scale;
@@ -419,23 +453,28 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
     auto land = [&](int b) {
       uint16_t* sK = sKV + b * BUF;
       uint16_t* sV = sK + KEYS * D;
-      uint32_t odd = 0;
-      if (lane < 32) sh.scale[b][lane >> 4][my] = scale;
+      scale = power_of_two(scale);
+      const bool none = scale != scale;
+      uint32_t odd = none && lane >= 16 && lane < 32;
+      if (!BF && lane < 16) sh.ks[b][my] = scale;
+      if (lane >= 16 && lane < 32) sh.no_vs[b][my] = none;
 #pragma unroll
       for (int i = 0; i < LPW; ++i) {
-        const int r = (wid * LPW + i) * RPI + lane / LPR, pc = 2 * (lane % LPR);
+        const int row = i * RPI + lane / LPR, r = wid * 16 + row, pc = 2 * (lane % LPR);
+        const float ks = BF ? __shfl(scale, row) : 1.0f, vs = __shfl(scale, 16 + row);
         uint4* tk = reinterpret_cast<uint4*>(sK + r * D);
         uint4* tv = reinterpret_cast<uint4*>(sV + r * D);
-        tk[pc ^ swz_k<D>(r)] = widen8<BF, E5>(kr[i].x, kr[i].y);
-        tk[(pc + 1) ^ swz_k<D>(r)] = widen8<BF, E5>(kr[i].z, kr[i].w);
+        tk[pc ^ swz_k<D>(r)] = widen8<BF, E5>(kr[i].x, kr[i].y, ks);
+        tk[(pc + 1) ^ swz_k<D>(r)] = widen8<BF, E5>(kr[i].z, kr[i].w, ks);
         uint4 v = vr[i];
-        if (s_off[b][r] < 0) v = make_uint4(0, 0, 0, 0);
+        if (s_off[b][r] < 0 || vs != vs) v = make_uint4(0, 0, 0, 0);
         const uint32_t o = odd_codes<E5>(v.x) | odd_codes<E5>(v.y) | odd_codes<E5>(v.z) | odd_codes<E5>(v.w);
         odd |= o;
         if (__builtin_expect(__any(o != 0), 0))
           v = make_uint4(even_codes<E5>(v.x), even_codes<E5>(v.y), even_codes<E5>(v.z), even_codes<E5>(v.w));
-        tv[pc ^ swz_v<D>(r)] = widen8<true, E5>(v.x, v.y);
-        tv[(pc + 1) ^ swz_v<D>(r)] = widen8<true, E5>(v.z, v.w);
+        const float use = vs != vs ? 1.0f : vs;
+        tv[pc ^ swz_v<D>(r)] = widen8<true, E5>(v.x, v.y, use);
+        tv[(pc + 1) ^ swz_v<D>(r)] = widen8<true, E5>(v.z, v.w, use);
       }
       const bool any = __any(odd != 0);
       if (lane == 0) sh.odd[b][wid] = any;
@@ -484,14 +523,16 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
         for (int t = 0; t < KT; ++t) sc[t] = mfma32<BF>(x[t], q[i], sc[t]);
       }
       __builtin_amdgcn_s_setprio(0);
+      if constexpr (!BF) {  // (a scaled code may be out of fp16's reach)
 #pragma unroll
-      for (int t = 0; t < KT; ++t)
+        for (int t = 0; t < KT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&sh.scale[b][0][32 * (wk * KT + t) + 8 * r + 4 * g]);
+          for (int r = 0; r < 4; ++r) {
+            const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&sh.ks[b][32 * (wk * KT + t) + 8 * r + 4 * g]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[t][4 * r + e] *= ks[e];
-        }
+            for (int e = 0; e < 4; ++e) sc[t][4 * r + e] *= ks[e];
+          }
+      }
       if (!full) {
 #pragma unroll
         for (int t = 0; t < KT; ++t)
@@ -526,27 +567,13 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
       for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
-          float x[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            x[i] = sc[t][8 * hh + i];
-            l += x[i];
-          }
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const f32x4_t vs =
-                *reinterpret_cast<const f32x4_t*>(&sh.scale[b][1][32 * (wk * KT + t) + 16 * hh + 8 * r + 4 * g]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float& y = x[4 * r + e];
-              y = full || y != 0.0f ? y * vs[e] : 0.0f;  // (the scale of a key that is not seen may be anything)
-            }
-          }
           uint4 p, p2;
-          split_p<true>(x[0], x[1], p.x, p2.x);
-          split_p<true>(x[2], x[3], p.y, p2.y);
-          split_p<true>(x[4], x[5], p.z, p2.z);
-          split_p<true>(x[6], x[7], p.w, p2.w);
+          split_p<true>(sc[t][8 * hh], sc[t][8 * hh + 1], p.x, p2.x);
+          split_p<true>(sc[t][8 * hh + 2], sc[t][8 * hh + 3], p.y, p2.y);
+          split_p<true>(sc[t][8 * hh + 4], sc[t][8 * hh + 5], p.z, p2.z);
+          split_p<true>(sc[t][8 * hh + 6], sc[t][8 * hh + 7], p.w, p2.w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) l += sc[t][8 * hh + i];
           const int k0 = 32 * (wk * KT + t) + 16 * hh + 4 * (gq >> 1) + (li >> 2);
           uint4 y[ND];
 #pragma unroll
@@ -570,13 +597,14 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
           const int64_t off = s_off[b][kk];
           if (off < 0) continue;
           const char* vrow = a.pv + head_off + off + 4 * g;
+          const bool none = sh.no_vs[b][kk];  // (NaN in all of the row)
 #pragma unroll
           for (int i = 0; i < ND; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const uint32_t v = *reinterpret_cast<const uint32_t*>(vrow + 32 * i + 8 * r);
               float x[4] = {acc[i][4 * r], acc[i][4 * r + 1], acc[i][4 * r + 2], acc[i][4 * r + 3]};
-              if (k + kk < lim) add_odd4<E5>(v, x);
+              if (k + kk < lim) add_odd4<E5>(none ? 0x7f7f7f7fu : v, x);
 #pragma unroll
               for (int e = 0; e < 4; ++e) acc[i][4 * r + e] = x[e];
             }
@@ -661,6 +689,12 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
   }
 }
 
+// Keys of a step of a walk over tiles of COLS columns.
+template <int COLS>
+__device__ __forceinline__ constexpr int step_keys() {
+  return COLS <= 32 ? kPaged8Step : kPagedWideStep;
+}
+
 // The sequences' own keys alone.
 template <int D, bool BF, bool E5, int COLS>
 __global__ __launch_bounds__(kThreads, COLS == 32 && D == 128 ? 1 : 2) void paged8_kernel(const PagedArgs a,
@@ -668,7 +702,7 @@ __global__ __launch_bounds__(kThreads, COLS == 32 && D == 128 ? 1 : 2) void page
   extern __shared__ __attribute__((aligned(16))) char dyn[];
   Seg* seg = reinterpret_cast<Seg*>(dyn);
   int total;
-  schedule<COLS, 0>(a, ps, ps, seg, nullptr, &total, nullptr);
+  schedule<COLS, step_keys<COLS>(), 0, 1>(a, ps, ps, seg, nullptr, &total, nullptr);
   const int parts = min(ps.grid, total);
   if (ps.fused) clear_empty<D>(a, ps, seg);
   else publish<COLS, step_keys<COLS>()>(a, ps, seg, total, parts, blockIdx.x, gridDim.x);
@@ -696,7 +730,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged8_both_kernel(const PagedArg
   } sh;
   constexpr int KO = step_keys<OWN>(), KS = step_keys<SHARED>();
   int to, ts;
-  schedule<OWN, SHARED>(a, own, shared, seg_o, seg_s, &to, &ts);
+  schedule<OWN, KO, SHARED, KS>(a, own, shared, seg_o, seg_s, &to, &ts);
   const int n = gridDim.x;
   const double ws = (double)ts * KS, wo = (double)to * KO;
   const int ns = ts == 0 ? 0 : to == 0 ? n : min(max((int)(n * ws / (ws + wo) + 4.0) / 8 * 8, 8), n - 8);

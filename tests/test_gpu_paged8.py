@@ -34,8 +34,8 @@ def _batch(lens, groups, page, block, hkv, d, code, seed, spare=3, spread=2):
         x = rng.standard_normal((total, hkv, page, d)) * C.TOP[code] / 5
         x = np.clip(x, -C.TOP[code], C.TOP[code])
         # keys of about 1, whatever the code's reach; scales up to 2^spread apart
-        scale = 2.0 ** rng.integers(-spread, spread + 1, (total, hkv, page // block)) * 5 / C.TOP[code]
-        kv.append((C.rounded(x, code), np.float32(scale).astype(np.float64)))
+        one = {"e4m3": -7, "e5m2": -14}[code]
+        kv.append((C.rounded(x, code), 2.0 ** (one + rng.integers(-spread, spread + 1, (total, hkv, page // block)))))
     return kv, table, rng
 
 
@@ -156,7 +156,7 @@ def _garbage(kv, table, lens, code, seed, number):
     return dirty
 
 
-@pytest.mark.parametrize("number", [float("nan"), float("inf"), 3e38])
+@pytest.mark.parametrize("number", [float("nan"), float("inf"), 3e38, -1.0, 0.0])
 @pytest.mark.parametrize("case", [0, 1, 2])
 def test_what_nothing_sees_does_not_matter(case, number):
     lens, groups, n_q, hq, hkv, d, page, block, code, dtype = [
@@ -190,7 +190,7 @@ def test_what_one_row_sees_another_does_not(walk, code):
     pg, row = table[0, last // page], last % page
     # (shared pages are the other sequence's too: its rows all see that key)
     others = [i for i in range(2 * n_q) if i != n_q - 1 and (walk != "both" or i < n_q)]
-    for what in ["code", "scale", "key"] + (["inf"] if code == "e5m2" else []):
+    for what in ["code", "scale", "half", "key"] + (["inf"] if code == "e5m2" else []):
         dev = []
         for i, (codes, scale) in enumerate(kv):
             c, s = codes.copy(), scale.copy()
@@ -200,6 +200,8 @@ def test_what_one_row_sees_another_does_not(walk, code):
                 c[pg, 0, row, 9] = -np.inf
             if what == "scale" and i == 1:
                 s[pg, 0, row] = np.nan
+            if what == "half" and i == 0:
+                s[pg, 0, row] = 1.5  # no power of two: no number
             if what == "key" and i == 0:
                 c[pg, 0, row, 3] = np.nan
             dev.append(C.Cache(c, s, code))
