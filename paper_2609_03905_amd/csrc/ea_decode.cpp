@@ -532,7 +532,7 @@ int cache8(const ea_relation* xk, const ea_relation* xv, const ea_relation* k, c
     return fail(EA_ERR_UNSUPPORTED, "%d sequences, at most %d", b.n_seq, EA_PAGED_MAX_SEQ);
   if ((b.stride + (int64_t)1) * page > INT32_MAX - 1024)
     return fail(EA_ERR_UNSUPPORTED, "a table row of 2^31 keys or more");
-  if (hkv > 1 << 20) return fail(EA_ERR_UNSUPPORTED, "%lld heads", (long long)hkv);
+  if (2 * hkv * a.xk.t > INT32_MAX) return fail(EA_ERR_UNSUPPORTED, "2^30 rows and heads or more");
   if (!b.lengths || !b.table) return fail(EA_ERR_ARG, "NULL lengths or table");
   if (!b.q_start && a.xk.t < b.n_seq) return fail(EA_ERR_ARG, "%d rows for %d sequences", a.xk.t, b.n_seq);
   const ea_relation* const outs_w[] = {k, v, ks, vs};
@@ -567,6 +567,8 @@ int cache8(const ea_relation* xk, const ea_relation* xv, const ea_relation* k, c
   a.block_rows = a.page_size / a.n_blocks;
   a.page = fast_div((uint32_t)a.page_size);
   a.block = fast_div((uint32_t)a.block_rows);
+  a.pieces = fast_div((uint32_t)a.d / 8);
+  a.sides = fast_div(2 * (uint32_t)a.hkv);
   a.page_bytes = page_bytes(k);
   EA_HIP_TRY(launch_cache8(a, xk->dtype, k->dtype, write, (hipStream_t)stream));
   return ok();

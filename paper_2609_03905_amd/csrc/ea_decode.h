@@ -156,6 +156,7 @@ struct Cache8Args {
   int32_t n_seq, stride, n_pages, page_size, rows, hkv, d;
   int32_t block_rows, n_blocks;  // rows of a scale's block, blocks of a page
   FastDiv page, block;
+  FastDiv pieces, sides;  // by 8-code pieces of a row, by K's and V's heads
   int64_t page_bytes;
 };
 hipError_t launch_cache8(const Cache8Args& a, int32_t dtype, int32_t code, bool write, hipStream_t s);

@@ -109,16 +109,18 @@ def test_read(case):
         C.same(C.f64(get(r)), want)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("code", ["e4m3", "e5m2"])
-def test_every_value_is_rounded_as_defined(code):
-    """All fp16 values: each as a row of its own scale 2^0, the ties and the
-    subnormal codes among them."""
-    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.float16)
-    x = bits[bits.float().abs() <= C.TOP[code]].cuda()
+def test_every_value_is_rounded_as_defined(code, dtype):
+    """All values of 16 bits that a code reaches under the scale 1, the ties and
+    the subnormal codes among them (f32: those of fp16)."""
+    t = R.TORCH[dtype]
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16 if dtype == "bf16" else torch.float16)
+    x = bits[bits.float().abs() <= C.TOP[code]].cuda().to(t)
     d = 512
     n = -(-len(x) // (d - 1))
-    rows = torch.zeros(n, 1, d, dtype=torch.float16, device="cuda")
-    flat = torch.zeros(n * (d - 1), dtype=torch.float16, device="cuda")
+    rows = torch.zeros(n, 1, d, dtype=t, device="cuda")
+    flat = torch.zeros(n * (d - 1), dtype=t, device="cuda")
     flat[:len(x)] = x
     rows[:, 0, 1:] = flat.view(n, d - 1)
     rows[:, 0, 0] = C.TOP[code]  # so the scale is 1
@@ -127,17 +129,20 @@ def test_every_value_is_rounded_as_defined(code):
     assert (dev[0].scale[table[0, 0]] == 1).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("code", ["e4m3", "e5m2"])
-def test_scales_at_their_borders(code):
+def test_scales_at_their_borders(code, dtype):
     """The largest element at, just above and far below a code's reach, zero,
-    the smallest numbers, infinities and NaN: a row each, a scale each."""
+    the smallest numbers, infinities and NaN: a row each, a scale each; and with
+    a number of about a third beside it."""
     top = C.TOP[code]
-    tops = [top, np.nextafter(np.float32(top), np.float32(np.inf)), top * 2, top / 2, 1.0, 1.75, 1.7500001, 0.0, -0.0,
-            2.0 ** -149, 2.0 ** -126, 2.0 ** -112, 2.0 ** -111, 3e38, 2.0 ** 127, -top * 1.01, np.inf, -np.inf, np.nan]
+    tops = [top, np.nextafter(np.float32(top), np.float32(np.inf)), top * 1.0078125, top * 2, top / 2, 1.0, 1.75,
+            1.7500001, 1.7578125, 0.0, -0.0, 2.0 ** -149, 2.0 ** -133, 2.0 ** -126, 2.0 ** -112, 2.0 ** -111, 2.0 ** -24,
+            2.0 ** -14, 65504.0, 3e38, 2.0 ** 127, -top * 1.01, np.inf, -np.inf, np.nan]
     x = np.zeros((len(tops), 1, 16), np.float32)
     x[:, 0, 5] = tops
     x[:, 0, 7] = np.float32(0.3) * np.where(np.isfinite(tops), tops, 1)
-    x = torch.from_numpy(x).cuda()
+    x = torch.from_numpy(x).to(R.TORCH[dtype]).cuda()
     kv, table, lens, starts, _ = _state([0], [len(tops)], 4, 1, 1, 16, code, 4)
     _check_write(kv, [x, -x], table, lens, starts, code)
 
