@@ -81,7 +81,7 @@ struct __attribute__((aligned(16))) Few8Shared {
 template <int D>
 struct __attribute__((aligned(1024))) Many8Shared {
   uint16_t kv[2][2 * kPagedWideStep * D];  // two steps' buffers: K, then V
-  int64_t off[2][kPagedWideStep];
+  int64_t off[3][kPagedWideStep];
   float ks[2][kPagedWideStep];   // K's scales (fp16 queries)
   int no_vs[2][kPagedWideStep];  // whether a V row's scale is none
   int odd[2][kWaves];            // whether a wave found such a scale, or codes that are not finite
@@ -265,7 +265,8 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
         }
       }
       uint32_t odd = 0;
-      if (!full) {
+      if (__builtin_expect(!full, 0)) {
+        asm volatile("" ::: "memory");
         const uint64_t mine = there >> (4 * g4);
 #pragma unroll
         for (int i = 0; i < 4 * NT; ++i) {
@@ -305,6 +306,7 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
         const float m_new = mx > m[t] + kLazyMax || m[t] == -INFINITY ? fmaxf(mx, m[t]) : m[t];
         const float m_use = m_new == -INFINITY ? 0.0f : m_new;
         if (__any(m_new != m[t])) {
+          asm volatile("" ::: "memory");
           const float alpha = __builtin_amdgcn_exp2f(m[t] - m_use);
           l[t] *= alpha;
 #pragma unroll
@@ -430,27 +432,27 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
     const int my = wid * 16 + (lane & 15);
     const float* scales = lane & 16 ? a.vs : a.ks;
     auto entry = [&](int k) { return k + my < kb ? pages[div_fast(k + my, a.page)] : -1; };
-    auto place = [&](int b, int k, int pg) {
+    auto place = [&](int slot, int k, int pg) {  // the rows' offsets, -1: no such row; the scale
       const int key = k + my, in = key - div_fast(key, a.page) * a.page_size;
       const bool there = (uint32_t)pg < (uint32_t)a.n_pages;
       const int64_t off = there ? pg * a.page_bytes + (int64_t)in * D : -1;
-      if (lane < 16) s_off[b][my] = off;
+      if (lane < 16) s_off[slot][my] = off;
       __builtin_amdgcn_wave_barrier();
       return there ? scales[((int64_t)pg * a.hkv + h) * a.n_blocks + div_fast(in, a.block)] : 1.0f;
     };
     uint4 kr[LPW], vr[LPW];
     float scale;
-    auto fetch = [&](int b) {
+    auto fetch = [&](int slot) {
 #pragma unroll
       for (int i = 0; i < LPW; ++i) {
-        const int64_t off = s_off[b][(wid * LPW + i) * RPI + lane / LPR];
+        const int64_t off = s_off[slot][(wid * LPW + i) * RPI + lane / LPR];
         kr[i] = *reinterpret_cast<const uint4*>(kbase + (off < 0 ? 0 : off));
         vr[i] = *reinterpret_cast<const uint4*>(vbase + (off < 0 ? 0 : off));
       }
     };
     // widened to buffer b; zeros in the place of values whose rows do not exist and
     // of codes that stand for no number, which sh.odd tells of
-    auto land = [&](int b) {
+    auto land = [&](int b, int slot) {
       uint16_t* sK = sKV + b * BUF;
       uint16_t* sV = sK + KEYS * D;
       scale = power_of_two(scale);
@@ -467,7 +469,7 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
         tk[pc ^ swz_k<D>(r)] = widen8<BF, E5>(kr[i].x, kr[i].y, ks);
         tk[(pc + 1) ^ swz_k<D>(r)] = widen8<BF, E5>(kr[i].z, kr[i].w, ks);
         uint4 v = vr[i];
-        if (s_off[b][r] < 0 || vs != vs) v = make_uint4(0, 0, 0, 0);
+        if (s_off[slot][r] < 0 || vs != vs) v = make_uint4(0, 0, 0, 0);
         const uint32_t o = odd_codes<E5>(v.x) | odd_codes<E5>(v.y) | odd_codes<E5>(v.z) | odd_codes<E5>(v.w);
         odd |= o;
         if (__builtin_expect(__any(o != 0), 0))
@@ -504,23 +506,31 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
     for (int i = 0; i < ND; ++i) acc[i] = f32x16_t{};
     float m = -INFINITY, l = 0.0f;
 
-    auto compute = [&](int b, int k, bool full) {
+    auto compute = [&](int b, int slot, int k) {
+      // every key of the step has a row and is seen by every column of the wave
+      const uint64_t there = __ballot(s_off[slot][lane] >= 0);
+      const bool full = there == ~uint64_t(0) && k + KEYS <= lim_min;
       const uint16_t* sK = sKV + b * BUF;
       const uint16_t* sV = sK + KEYS * D;
       f32x16_t sc[KT];
 #pragma unroll
       for (int t = 0; t < KT; ++t) sc[t] = f32x16_t{};
       __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        uint4 x[KT];
+      uint4 x[2][KT];
+      auto read_k = [&](int i) {
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
           const int r = 32 * (wk * KT + t) + lq;
-          x[t] = *reinterpret_cast<const uint4*>(sK + r * D + 8 * ((2 * i + g) ^ swz_k<D>(r)));
+          x[i & 1][t] = *reinterpret_cast<const uint4*>(sK + r * D + 8 * ((2 * i + g) ^ swz_k<D>(r)));
         }
+      };
+      read_k(0);
 #pragma unroll
-        for (int t = 0; t < KT; ++t) sc[t] = mfma32<BF>(x[t], q[i], sc[t]);
+      for (int i = 0; i < NS; ++i) {
+        if (i + 1 < NS) read_k(i + 1);
+        __builtin_amdgcn_sched_barrier(0);  // (the next operand on its way before this one's products)
+#pragma unroll
+        for (int t = 0; t < KT; ++t) sc[t] = mfma32<BF>(x[i & 1][t], q[i], sc[t]);
       }
       __builtin_amdgcn_s_setprio(0);
       if constexpr (!BF) {  // (a scaled code may be out of fp16's reach)
@@ -533,13 +543,16 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
             for (int e = 0; e < 4; ++e) sc[t][4 * r + e] *= ks[e];
           }
       }
-      if (!full) {
+      if (__builtin_expect(!full, 0)) {
+        asm volatile("" ::: "memory");  // a branch: the masks would be a third of a step's instructions
+        const uint64_t mine = there >> (32 * wk * KT + 4 * g);
+        const int seen = lim - k - 32 * wk * KT - 4 * g;
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int kk = 32 * (wk * KT + t) + 8 * (r >> 2) + 4 * g + (r & 3);
-            sc[t][r] = s_off[b][kk] >= 0 && k + kk < lim ? sc[t][r] : -INFINITY;
+            const int kk = 32 * t + 8 * (r >> 2) + (r & 3);
+            sc[t][r] = (mine >> kk & 1) && kk < seen ? sc[t][r] : -INFINITY;
           }
       }
       float mx = sc[0][0];
@@ -551,6 +564,7 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
       const float m_new = mx > m + kLazyMax || m == -INFINITY ? fmaxf(mx, m) : m;
       const float m_use = m_new == -INFINITY ? 0.0f : m_new;
       if (__any(m_new != m)) {
+        asm volatile("" ::: "memory");  // a branch: most steps leave the maximum where it is
         const float alpha = __builtin_amdgcn_exp2f(m - m_use);
         l *= alpha;
 #pragma unroll
@@ -594,7 +608,7 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
       if (__builtin_expect(sh.odd[b][0] | sh.odd[b][1] | sh.odd[b][2] | sh.odd[b][3], 0)) {
 #pragma unroll 1
         for (int kk = 32 * wk * KT; kk < 32 * (wk + 1) * KT; ++kk) {
-          const int64_t off = s_off[b][kk];
+          const int64_t off = s_off[slot][kk];
           if (off < 0) continue;
           const char* vrow = a.pv + head_off + off + 4 * g;
           const bool none = sh.no_vs[b][kk];  // (NaN in all of the row)
@@ -612,18 +626,28 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
       }
     };
 
-    land(0);
+    // A step's codes are fetched two steps ahead and land, widened, one step ahead,
+    // before the products of the step between: their loads had a whole step's time.
+    land(0, 0);
+    if (ka + KEYS < kb) {
+      scale = place(1, ka + KEYS, next_pg);
+      next_pg = entry(ka + 2 * KEYS);
+      fetch(1);
+    }
     __syncthreads();
-    int b = 0;
+    int b = 0, slot = 0;
     for (int k = ka; k < kb; k += KEYS, b ^= 1) {
-      const bool more = k + KEYS < kb;
-      if (more) {
-        scale = place(b ^ 1, k + KEYS, next_pg);
-        next_pg = entry(k + 2 * KEYS);
-        fetch(b ^ 1);
+      const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
+      if (k + KEYS < kb) {
+        land(b ^ 1, slot1);
+        if (k + 2 * KEYS < kb) {
+          scale = place(slot2, k + 2 * KEYS, next_pg);
+          next_pg = entry(k + 3 * KEYS);
+          fetch(slot2);
+        }
       }
-      if (!idle) compute(b, k, k + KEYS <= lim_min && __all(s_off[b][lane] >= 0));
-      if (more) land(b ^ 1);
+      if (!idle) compute(b, slot, k);
+      slot = slot1;
       __syncthreads();
     }
     l += other32(l);
