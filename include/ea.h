@@ -629,7 +629,16 @@ int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages*
    (out_lengths is not written); out_table and out_refs may be table and refs. */
 int ea_pages_compact(int32_t n_cache, ea_relation* const* caches, const ea_pages* state, void* workspace,
                      int64_t ws_bytes, void* stream);
-/* Workspace of the three: 256-byte aligned, over no argument; behind its
+/* The two over caches in 8 bits: scales[i] are cache i's, f32 [pages, Hkv, n] of
+   one block or [planes, pages, Hkv, n] of one block a plane, NULL where the cache
+   is not held in 8 bits (the calls without scales take no cache that is).  A block's
+   scale moves with the first of its rows. */
+int ea_pages_select_scaled(int32_t n_cache, ea_relation* const* caches, ea_relation* const* scales,
+                           const ea_pages* state, const int32_t* parent, void* workspace, int64_t ws_bytes,
+                           void* stream);
+int ea_pages_compact_scaled(int32_t n_cache, ea_relation* const* caches, ea_relation* const* scales,
+                            const ea_pages* state, void* workspace, int64_t ws_bytes, void* stream);
+/* Workspace of these: 256-byte aligned, over no argument; behind its
    counter area (which stays untouched) no initial value is needed. */
 int ea_pages_workspace(int32_t n_seq, int32_t n_pages, int64_t* ws_bytes);
 

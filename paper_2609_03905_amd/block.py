@@ -135,9 +135,14 @@ class LlamaBlockShare:
         return dict(d_head=self.d_head, wq=self.qn, wk=self.kn, eps=self.eps, inv_freq=self.inv_freq,
                     interleaved=self.interleaved, positions=positions)
 
-    def store(self, cache: KVCache, slots: torch.Tensor, layer: int = 0):
+    def store(self, cache: KVCache, slots: torch.Tensor | None, layer: int = 0, q_start: torch.Tensor | None = None):
         """The last forward's keys and values to the cache: token t to slot
-        slots[t] (queries are written again, as they are)."""
+        slots[t] (queries are written again, as they are).  A cache in 8 bits takes
+        tokens q_start[s] .. q_start[s + 1] - 1 as the newest of its sequence s
+        (None: token s) instead."""
+        if cache.scales is not None:
+            cache.write(layer, self.k, self.v, q_start)
+            return
         ea.heads(self.qkv, self.q, cache.k[layer], cache.v[layer], slots=slots, **self.head_options(self.positions))
 
     def forward(self):
@@ -170,7 +175,9 @@ class LlamaBlockDecode:
     """The newest tokens of the cache's sequences through a share's weights:
     ``rows`` tokens a step (x: [rows, hidden], sequence by sequence), their
     slots and positions from cache.extend, at most ``groups`` shared prefixes
-    (None: as many as sequences).  The calls' plans are made and their workspace
+    (None: as many as sequences).  Over a cache in 8 bits the head rows go through
+    rows of the step's own, and are written to the sequences' newest places
+    (q_start, not slots, says whose they are).  The calls' plans are made and their workspace
     is allocated here, so a step can be captured at once, and steps of several
     decoders may overlap in time (steps of one may not: its activations and its
     workspace are one step's)."""
@@ -186,6 +193,9 @@ class LlamaBlockDecode:
         self.h1 = R((rows, s.hidden), [pt, ph])
         self.qkv = R((rows, s.wqkv.shape[1]), [pt, pqkv])
         self.q = R((rows, s.hd), [pt, phd])
+        if cache.scales is not None:
+            wide = s.heads_kv * s.d_head
+            self.kr, self.vr = R((rows, wide), [[0, rows], [0, wide]]), R((rows, wide), [[0, rows], [0, wide]])
         self.attn = R((rows, s.hd), [pt, phd])
         self.x2 = R((rows, s.hidden), [pt, ph])
         self.h2 = R((rows, s.hidden), [pt, ph])
@@ -217,13 +227,19 @@ class LlamaBlockDecode:
             args, kw = self._joinaggs[name]
             return name, lambda: ea.joinagg(*args, workspace=ws, **kw)
 
+        if c.scales is None:
+            heads = [("heads", lambda: ea.heads(self.qkv, self.q, k, v, slots=slots, **s.head_options(positions)))]
+        else:
+            heads = [("heads", lambda: ea.heads(self.qkv, self.q, self.kr, self.vr, **s.head_options(positions))),
+                     ("write", lambda: c.write(self.layer, self.kr, self.vr, q_start))]
         return [
             joinagg("rmsnorm1"),
             joinagg("qkv_gemm"),
-            ("heads", lambda: ea.heads(self.qkv, self.q, k, v, slots=slots, **s.head_options(positions))),
+            *heads,
             ("attention", lambda: ea.attention_paged(self.q, k, v, self.attn, scale=s.scale, table=c.table,
                                                      lengths=c.lengths, q_start=q_start, group_start=group_start,
-                                                     group_shared=group_shared, workspace=ws)),
+                                                     group_shared=group_shared, k_scale=c.k_scale[self.layer],
+                                                     v_scale=c.v_scale[self.layer], workspace=ws)),
             joinagg("o_gemm_residual"),
             joinagg("rmsnorm2"),
             joinagg("swiglu_gemm"),

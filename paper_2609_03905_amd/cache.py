@@ -16,10 +16,14 @@ class KVCache:
     arrays, replaced by every select (captured calls keep the arrays they were
     given).  The first element of ``status`` says what became of the last call
     (ea.PAGES_OK, or why nothing was done), the second how many pages are free;
-    it is on the device, so that asking is the caller's choice."""
+    it is on the device, so that asking is the caller's choice.
+
+    With ``dtype`` "e4m3" or "e5m2" the cache is held in 8 bits: k_scale[layer]
+    and v_scale[layer] are the scales of every head's blocks of ``block`` keys
+    (None: a page), and rows go in by write and come back by read."""
 
     def __init__(self, layers: int, pages: int, heads_kv: int, page_size: int, d_head: int, sequences: int,
-                 max_pages: int, dtype: str = "bf16", device="cuda"):
+                 max_pages: int, dtype: str = "bf16", device="cuda", block: int | None = None):
         self.page_size = page_size
         shape = (2 * layers, pages, heads_kv, page_size, d_head)
         one = [[0, heads_kv], [0, page_size], [0, d_head]]
@@ -27,6 +31,19 @@ class KVCache:
         plane = self.data.block(pages)[2] if layers else 0  # bytes from plane to plane
         views = [self.data.view(i * plane, shape[1:], dtype, [range(pages + 1)] + one) for i in range(2 * layers)]
         self.k, self.v = views[0::2], views[1::2]
+        self.scales = None
+        self.k_scale = self.v_scale = [None] * layers
+        if dtype in ("e4m3", "e5m2"):
+            block = page_size if block is None else block
+            if block < 1 or page_size % block:
+                raise ea.EAError(ea.ERR_ARG, f"blocks of {block} keys in pages of {page_size}")
+            shape = (2 * layers, pages, heads_kv, page_size // block)
+            whole = ea.whole_partition(shape[1:])
+            self.scales = ea.Relation(shape, "f32", [range(2 * layers + 1)] + whole, device=device)
+            views = [self.scales.view(self.scales.block(i)[2], shape[1:], "f32", whole) for i in range(2 * layers)]
+            self.k_scale, self.v_scale = views[0::2], views[1::2]
+        elif block is not None:
+            raise ea.EAError(ea.ERR_ARG, f"a {dtype} cache has no scales")
         zeros = lambda *n: torch.zeros(n, dtype=torch.int32, device=device)
         self.table, self.lengths, self.refs = zeros(sequences, max_pages), zeros(sequences), zeros(pages)
         self._other = (zeros(sequences, max_pages), zeros(sequences), zeros(pages))
@@ -43,15 +60,30 @@ class KVCache:
                         slots=slots, positions=positions, workspace=self._workspace)
         return slots, positions
 
+    def write(self, layer: int, xk: ea.Relation, xv: ea.Relation, q_start: torch.Tensor | None = None):
+        """Rows q_start[s] .. q_start[s + 1] - 1 (None: row s) of keys and values
+        quantised into the newest places of sequence s (8 bits: ea.pages_write)."""
+        ea.pages_write(xk, xv, self.k[layer], self.v[layer], **self._rows(layer, q_start))
+
+    def read(self, layer: int, xk: ea.Relation, xv: ea.Relation, q_start: torch.Tensor | None = None):
+        """The same rows back (8 bits: ea.pages_read)."""
+        ea.pages_read(self.k[layer], self.v[layer], xk, xv, **self._rows(layer, q_start))
+
+    def _rows(self, layer, q_start):
+        if self.scales is None:
+            raise ea.EAError(ea.ERR_ARG, f"a {self.data.dtype} cache is written by ea.heads")
+        return dict(k_scale=self.k_scale[layer], v_scale=self.v_scale[layer], table=self.table, lengths=self.lengths,
+                    q_start=q_start)
+
     def select(self, parent: torch.Tensor):
         """Sequence i becomes a copy of sequence parent[i] (-1: empty)."""
         table, lengths, refs = self._other
         ea.pages_select([self.data], parent, self.table, self.lengths, self.refs, out_table=table, out_lengths=lengths,
-                        out_refs=refs, status=self.status, workspace=self._workspace)
+                        out_refs=refs, status=self.status, scales=[self.scales], workspace=self._workspace)
         self._other = (self.table, self.lengths, self.refs)
         self.table, self.lengths, self.refs = table, lengths, refs
 
     def compact(self):
         """Move the used pages to the first places."""
-        ea.pages_compact([self.data], self.table, self.lengths, self.refs, status=self.status,
+        ea.pages_compact([self.data], self.table, self.lengths, self.refs, status=self.status, scales=[self.scales],
                          workspace=self._workspace)

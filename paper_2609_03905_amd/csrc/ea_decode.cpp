@@ -634,7 +634,8 @@ bool meets_state(const ea_pages* s, const void* p, int64_t bytes) {
          overlap(p, bytes, s->out_refs, nr) || overlap(p, bytes, s->status, 8);
 }
 
-int check_caches(int32_t n, ea_relation* const* caches, const ea_pages* p, const int32_t* parent, PagesCopyArgs* c) {
+int check_caches(int32_t n, ea_relation* const* caches, ea_relation* const* scales, const ea_pages* p,
+                 const int32_t* parent, PagesCopyArgs* c) {
   if (n < 0 || n > kPagesMaxCaches || (n && !caches))
     return fail(EA_ERR_ARG, "n_cache %d outside [0, %d] or NULL caches", n, kPagesMaxCaches);
   c->n_cache = n;
@@ -657,6 +658,27 @@ int check_caches(int32_t n, ea_relation* const* caches, const ea_pages* p, const
       return fail(EA_ERR_UNSUPPORTED, "a page of 2 GiB or more");
     c->c[i] = {(char*)r->data, page_bytes(r) * p->n_pages, page_bytes(r), row, (int32_t)(q ? r->shape[0] : 1),
                (int32_t)r->shape[q + 1]};
+    const ea_relation* z = scales ? scales[i] : nullptr;
+    if (is_code(r->dtype) != (z != nullptr))
+      return fail(EA_ERR_DTYPE, z ? "cache %d is not held in 8 bits: it has no scales" : "cache %d is held in 8 bits: its scales move with it", i);
+    if (!z) continue;
+    const int ez = check_rel(z, "a scale", true);
+    if (ez) return ez;
+    if (z->dtype != EA_F32) return fail(EA_ERR_DTYPE, "scales of cache %d are not f32", i);
+    bool fits = z->rank == r->rank - 1 && p->page_size % z->shape[q + 2] == 0;
+    for (int d = 0; fits && d < q + 2; ++d) fits = z->shape[d] == r->shape[d];
+    if (!fits) return fail(EA_ERR_ARG, "scales of cache %d are not its planes, pages, heads and blocks of a page", i);
+    for (int d = 0; d < z->rank; ++d)
+      if (z->nb[d] != (d < q ? z->shape[d] : 1))
+        return fail(EA_ERR_UNSUPPORTED, "scales of cache %d: a block is not one plane", i);
+    for (int j = 0; j < n; ++j)
+      if (overlap(z, caches[j]) || (j < i && overlap(z, scales[j]))) return fail(EA_ERR_ARG, "scales overlap a cache or others");
+    if (meets_state(p, z->data, z->nbytes) || overlap(span(z), {ints(parent, p->n_seq)}))
+      return fail(EA_ERR_ARG, "scales overlap an array of the state");
+    const int64_t words = z->shape[q + 1] * z->shape[q + 2];
+    if (words > INT32_MAX) return fail(EA_ERR_UNSUPPORTED, "2^31 scales of a page or more");
+    c->s[c->n_scales++] = {(char*)z->data, align256(p->n_pages * words * 4), c->c[i].planes, (int32_t)words,
+                           (int32_t)z->shape[q + 2], (int32_t)(p->page_size / z->shape[q + 2])};
   }
   return EA_OK;
 }
@@ -668,13 +690,14 @@ int64_t pages_bytes(int32_t n_seq, int32_t n_pages) {
 }
 
 int check_pages_ws(const ea_pages* p, std::initializer_list<Span> more, int32_t n_cache, ea_relation* const* caches,
-                   void* ws, int64_t bytes, PagesArgs* a, PagesCopyArgs* c) {
+                   ea_relation* const* scales, void* ws, int64_t bytes, PagesArgs* a, PagesCopyArgs* c) {
   if (!ws || (uintptr_t)ws % 256) return fail(EA_ERR_ARG, "workspace missing or not 256-byte aligned");
   const int64_t need = pages_bytes(p->n_seq, p->n_pages);
   if (bytes < need)
     return fail(EA_ERR_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)bytes, (long long)need);
   bool meets = meets_state(p, ws, need) || overlap(Span{ws, need}, more);
-  for (int i = 0; i < n_cache; ++i) meets = meets || overlap(Span{ws, need}, {span(caches[i])});
+  for (int i = 0; i < n_cache; ++i)
+    meets = meets || overlap(Span{ws, need}, {span(caches[i]), span(scales ? scales[i] : nullptr)});
   if (meets) return fail(EA_ERR_ARG, "the workspace overlaps an argument");
   a->work = (int32_t*)((char*)ws + kWsCounterBytes);
   c->work = a->work;
@@ -710,7 +733,7 @@ int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, i
       overlap(add, a.n_seq * (int64_t)4, a.status, 8))
     return fail(EA_ERR_ARG, "add overlaps an output");
   if ((e = check_pages_ws(state, {ints(add, a.n_seq), ints(slots, n_tokens), ints(positions, n_tokens)}, 0, nullptr,
-                          workspace, ws_bytes, &a, &c)))
+                          nullptr, workspace, ws_bytes, &a, &c)))
     return e;
   a.add = add;
   a.slots = slots;
@@ -722,11 +745,17 @@ int ea_pages_extend(const ea_pages* state, const int32_t* add, int32_t* slots, i
 
 int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages* state, const int32_t* parent,
                     void* workspace, int64_t ws_bytes, void* stream) {
+  return ea_pages_select_scaled(n_cache, caches, nullptr, state, parent, workspace, ws_bytes, stream);
+}
+
+int ea_pages_select_scaled(int32_t n_cache, ea_relation* const* caches, ea_relation* const* scales,
+                           const ea_pages* state, const int32_t* parent, void* workspace, int64_t ws_bytes,
+                           void* stream) {
   PagesArgs a{};
   PagesCopyArgs c{};
   int e = check_pages(state, &a);
   if (e) return e;
-  if ((e = check_caches(n_cache, caches, state, parent, &c))) return e;
+  if ((e = check_caches(n_cache, caches, scales, state, parent, &c))) return e;
   if (!parent || !state->out_lengths) return fail(EA_ERR_ARG, "NULL parent or out_lengths");
   if (a.out_table == a.table || a.out_len == a.len || a.out_refs == a.refs)
     return fail(EA_ERR_ARG, "select needs output arrays of their own");
@@ -734,7 +763,7 @@ int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages*
   if (overlap(parent, np, a.out_table, np * a.stride) || overlap(parent, np, a.out_len, np) ||
       overlap(parent, np, a.out_refs, a.n_pages * (int64_t)4) || overlap(parent, np, a.status, 8))
     return fail(EA_ERR_ARG, "parent overlaps an output");
-  if ((e = check_pages_ws(state, {ints(parent, a.n_seq)}, n_cache, caches, workspace, ws_bytes, &a, &c))) return e;
+  if ((e = check_pages_ws(state, {ints(parent, a.n_seq)}, n_cache, caches, scales, workspace, ws_bytes, &a, &c))) return e;
   a.parent = parent;
   EA_HIP_TRY(launch_pages_select(a, c, (hipStream_t)stream));
   return ok();
@@ -742,12 +771,17 @@ int ea_pages_select(int32_t n_cache, ea_relation* const* caches, const ea_pages*
 
 int ea_pages_compact(int32_t n_cache, ea_relation* const* caches, const ea_pages* state, void* workspace,
                      int64_t ws_bytes, void* stream) {
+  return ea_pages_compact_scaled(n_cache, caches, nullptr, state, workspace, ws_bytes, stream);
+}
+
+int ea_pages_compact_scaled(int32_t n_cache, ea_relation* const* caches, ea_relation* const* scales,
+                            const ea_pages* state, void* workspace, int64_t ws_bytes, void* stream) {
   PagesArgs a{};
   PagesCopyArgs c{};
   int e = check_pages(state, &a);
   if (e) return e;
-  if ((e = check_caches(n_cache, caches, state, nullptr, &c))) return e;
-  if ((e = check_pages_ws(state, {}, n_cache, caches, workspace, ws_bytes, &a, &c))) return e;
+  if ((e = check_caches(n_cache, caches, scales, state, nullptr, &c))) return e;
+  if ((e = check_pages_ws(state, {}, n_cache, caches, scales, workspace, ws_bytes, &a, &c))) return e;
   EA_HIP_TRY(launch_pages_compact(a, c, (hipStream_t)stream));
   return ok();
 }

@@ -181,9 +181,16 @@ struct PagesCache {
   int64_t plane_bytes, page_bytes, row_bytes;  // row: one head's one token
   int32_t planes, heads;
 };
+struct PagesScales {  // of a cache in 8 bits: [planes][pages][words]
+  char* data;
+  int64_t plane_bytes;
+  int32_t planes, words;         // words of a page: heads times its blocks
+  int32_t n_blocks, block_rows;  // blocks of a page, rows of a block
+};
 struct PagesCopyArgs {
   PagesCache c[kPagesMaxCaches];
-  int32_t n_cache, page_size;
+  PagesScales s[kPagesMaxCaches];
+  int32_t n_cache, n_scales, page_size;
   const int32_t* work;
 };
 hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s);

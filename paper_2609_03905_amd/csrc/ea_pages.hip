@@ -595,6 +595,20 @@ __global__ __launch_bounds__(kCopyThreads) void move_kernel(const PagesArgs a, c
       }
     }
   }
+  // scales: of every block that holds a row that moves
+  for (int k = 0; k < c.n_scales; ++k) {
+    const PagesScales& ps = c.s[k];
+    const int64_t items = (int64_t)count * ps.words;
+    for (int plane = blockIdx.y; plane < ps.planes; plane += gridDim.y) {
+      float* base = reinterpret_cast<float*>(ps.data + plane * ps.plane_bytes);
+      for (int64_t it = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; it < items; it += gridDim.x * kCopyThreads) {
+        const int j = (int)(it / ps.words), w = (int)(it - (int64_t)j * ps.words);
+        const int from = src[ROWS ? j : count - 1 - j];
+        if (from >= 0 && (!ROWS || w % ps.n_blocks * ps.block_rows < more[j]))
+          base[(int64_t)dst[j] * ps.words + w] = base[(int64_t)from * ps.words + w];
+      }
+    }
+  }
 }
 
 // Workgroups over pieces and planes.

@@ -119,6 +119,8 @@ def lib() -> ctypes.CDLL:
         L.ea_pages_extend.argtypes = [P(_Pages), vp, vp, vp, i32, vp, i64, vp]
         L.ea_pages_select.argtypes = [i32, P(vp), P(_Pages), vp, vp, i64, vp]
         L.ea_pages_compact.argtypes = [i32, P(vp), P(_Pages), vp, i64, vp]
+        L.ea_pages_select_scaled.argtypes = [i32, P(vp), P(vp), P(_Pages), vp, vp, i64, vp]
+        L.ea_pages_compact_scaled.argtypes = [i32, P(vp), P(vp), P(_Pages), vp, i64, vp]
         L.ea_plan_cache_size.restype = i64
         L.ea_plan_cache_clear.restype = ctypes.c_int
         _lib = L
@@ -619,10 +621,14 @@ def pages_extend(table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor,
     _check(lib().ea_pages_extend(ctypes.byref(st), a, ps, pp, n, ws, nbytes, s))
 
 
-def _page_caches(caches):
+def _page_caches(caches, scales):
     caches = list(caches)
-    _on_device(*caches)
-    return len(caches), _handles(caches), caches[0].shape[-2] if caches else None
+    scales = [None] * len(caches) if scales is None else list(scales)
+    if len(scales) != len(caches):
+        raise EAError(ERR_ARG, f"{len(scales)} scales for {len(caches)} caches")
+    _on_device(*caches, *scales)
+    given = (ctypes.c_void_p * max(1, len(scales)))(*[_h(r) for r in scales])
+    return len(caches), _handles(caches), given, caches[0].shape[-2] if caches else None
 
 
 def pages_workspace(sequences: int, pages: int) -> int:
@@ -638,33 +644,36 @@ def _pages_workspace(st, workspace, s):
 
 def pages_select(caches: Sequence[Relation], parent: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
                  refs: torch.Tensor, *, out_table: torch.Tensor, out_lengths: torch.Tensor, out_refs: torch.Tensor,
-                 status: torch.Tensor, page_size: int | None = None, stream=None,
-                 workspace: torch.Tensor | None = None) -> None:
+                 status: torch.Tensor, page_size: int | None = None, scales: Sequence[Relation | None] | None = None,
+                 stream=None, workspace: torch.Tensor | None = None) -> None:
     """Sequence i of the new state is a copy of sequence parent[i] (-1: empty):
     forks, reorders and frees.  Whole pages are shared; a partly filled last
     page is copied for all children but the first, in every plane of the caches
     ([pages, Hkv, page_size, d] or [planes, pages, Hkv, page_size, d]).
-    ``page_size`` is the caches' (needed where there are none)."""
-    n, handles, ps = _page_caches(caches)
+    ``page_size`` is the caches' (needed where there are none).  ``scales``: those
+    of caches in 8 bits ([pages, Hkv, n], or [planes, pages, Hkv, n] with one
+    block a plane), which move along; None for the others."""
+    n, handles, given, ps = _page_caches(caches, scales)
     st = _pages(table, lengths, refs, page_size or ps or 0, out_table, out_lengths, out_refs, status)
     s = _stream(stream)
     ws, nbytes = _pages_workspace(st, workspace, s)
-    _check(lib().ea_pages_select(n, handles, ctypes.byref(st), _device_array(parent, "parent", (table.shape[0],)), ws,
-                                 nbytes, s))
+    _check(lib().ea_pages_select_scaled(n, handles, given, ctypes.byref(st),
+                                        _device_array(parent, "parent", (table.shape[0],)), ws, nbytes, s))
 
 
 def pages_compact(caches: Sequence[Relation], table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, *,
                   status: torch.Tensor, out_table: torch.Tensor | None = None, out_refs: torch.Tensor | None = None,
-                  page_size: int | None = None, stream=None, workspace: torch.Tensor | None = None) -> None:
+                  page_size: int | None = None, scales: Sequence[Relation | None] | None = None, stream=None,
+                  workspace: torch.Tensor | None = None) -> None:
     """Move the used pages to the first places of the cache (the k-th lowest
     one behind them to the k-th lowest hole) and rewrite the table and the
-    counts, in place unless outputs are given."""
-    n, handles, ps = _page_caches(caches)
+    counts, in place unless outputs are given (``scales`` as for pages_select)."""
+    n, handles, given, ps = _page_caches(caches, scales)
     st = _pages(table, lengths, refs, page_size or ps or 0, table if out_table is None else out_table, None,
                 refs if out_refs is None else out_refs, status)
     s = _stream(stream)
     ws, nbytes = _pages_workspace(st, workspace, s)
-    _check(lib().ea_pages_compact(n, handles, ctypes.byref(st), ws, nbytes, s))
+    _check(lib().ea_pages_compact_scaled(n, handles, given, ctypes.byref(st), ws, nbytes, s))
 
 
 def plan_cache_size() -> int:

@@ -160,3 +160,64 @@ def test_the_reference_rounds_as_the_type_does(code):
     for top in (448, 57344, 1, 1.75, 1.76, 3.5, 2.0 ** -130, 0):
         s = C.least_scale(np.array([top, -np.inf, np.nan]), code)
         assert top <= C.TOP[code] * s and (s == 2.0 ** C.LEAST or top > C.TOP[code] * s / 2)
+
+
+# ---- pages that move with their scales ---------------------------------------------
+def moved(call, caches, given, ws=256, n=None, parent=(1 << 40) + (7 << 20), **change):
+    from test_decode_cpu import state
+
+    s, need = state(**({"out_lengths": None} if call == "compact" else {}) | change), ctypes.c_int64()
+    ea.lib().ea_pages_workspace(4, 30, ctypes.byref(need))
+    z = (ctypes.c_void_p * max(1, len(given)))(*[None if r is None else r._h for r in given])
+    args = [len(caches), E._handles(caches), z, ctypes.byref(s)] + ([parent] if call == "select" else [])
+    return getattr(ea.lib(), f"ea_pages_{call}_scaled")(*args, ws, need.value if n is None else n, None)
+
+
+def planes(p, n=4, dtype="f32", split=True):
+    return fake([p, 30, 2, n], dtype, [list(range(p + 1)) if split else [0, p], [0, 30], [0, 2], [0, n]])
+
+
+@pytest.mark.parametrize("call", ["select", "compact"])
+def test_scaled_moves_refuse(call):
+    eight, wide = cache(30, 2, 16, 64, "e4m3"), cache(30, 2, 16, 64)
+    five = cache(30, 2, 16, 64, "e5m2", planes=3)
+    bad = lambda code, caches, given, **kw: moved(call, caches, given, n=100, **kw) == code
+    assert bad(CAPACITY, [eight, wide, five], [scales(), None, planes(3)])  # all well but the workspace
+    assert bad(DTYPE, [eight], [None]) and bad(DTYPE, [wide], [scales()]) and bad(DTYPE, [eight], [scales(dtype="bf16")])
+    assert bad(ARG, [eight], [scales(pages=31)]) and bad(ARG, [eight], [scales(h=1)]) and bad(ARG, [eight], [scales(n=3)])
+    assert bad(ARG, [eight], [planes(1)]) and bad(ARG, [five], [planes(2)]) and bad(ARG, [five], [scales()])
+    assert bad(UNSUPPORTED, [five], [planes(3, split=False)])
+    assert bad(UNSUPPORTED, [eight], [scales(part=[[0, 15, 30], [0, 2], [0, 4]])])
+    z = scales()
+    assert bad(ARG, [eight, cache(30, 2, 16, 64, "e4m3")], [z, z])
+    over = _at(bare([30, 2, 4], "f32"), BASE)
+    under = _at(bare([30, 2, 16, 64], "e4m3", [range(31), [0, 2], [0, 16], [0, 64]]), BASE)
+    assert bad(ARG, [under], [over]) and bad(ARG, [eight, under], [over, scales()])
+    for array in ("table", "lengths", "refs", "status"):
+        assert bad(ARG, [eight], [over], **{array: BASE + 256})
+    if call == "select":
+        assert bad(ARG, [eight], [over], parent=BASE + 128)
+    assert moved(call, [eight], [over], ws=BASE) == ARG
+    # the calls without scales take no cache in 8 bits
+    from test_decode_cpu import compact, select
+
+    assert (select if call == "select" else compact)(caches=[eight]) == DTYPE
+
+
+def test_kv_cache_refuses():
+    from paper_2609_03905_amd.cache import KVCache
+
+    for more in (dict(dtype="e4m3", block=3), dict(dtype="e4m3", block=0), dict(dtype="bf16", block=8)):
+        with pytest.raises(E.EAError) as e:
+            KVCache(1, 4, 1, 16, 64, 2, 2, device="meta", **more)
+        assert e.value.code == ARG
+    c = KVCache(1, 4, 1, 16, 64, 2, 2, device="meta")
+    for call in (c.write, c.read):
+        with pytest.raises(E.EAError, match="ea.heads"):
+            call(0, None, None)
+    c = KVCache(3, 4, 2, 16, 64, 2, 2, dtype="e5m2", block=4, device="meta")
+    assert c.scales.shape == (6, 4, 2, 4) and c.k_scale[2].shape == (4, 2, 4) and c.k[1].dtype == "e5m2"
+    assert c.v_scale[1]._byte_offset == c.scales.block(3)[2]
+    with pytest.raises(E.EAError):  # one list entry a cache
+        E.pages_select([c.data], c.lengths, c.table, c.lengths, c.refs, out_table=c.table, out_lengths=c.lengths,
+                       out_refs=c.refs, status=c.status, scales=[])
