@@ -193,7 +193,11 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
   while (have) {
     const Piece cur = next;
     have = at < end;
-    if (have) next = next_piece();
+    int first_pg = -1;
+    if (have) {
+      next = next_piece();
+      first_pg = entry(next, next.ka + wid * NK);
+    }
     const Seg s = cur.s;
     const int tile = cur.tile, kb = cur.kb, slot_out = s.tile + cur.it + w;
 
@@ -234,7 +238,7 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
         keys = place(cur, slot ^ 1, k + kPaged8Step, next_pg);
         next_pg = entry(cur, k + 2 * kPaged8Step);
       } else if (have) {
-        keys = place(next, slot ^ 1, next.ka + wid * NK, entry(next, next.ka + wid * NK));
+        keys = place(next, slot ^ 1, next.ka + wid * NK, first_pg);
       }
       f32x4_t sc[NC][NT];
 #pragma unroll
