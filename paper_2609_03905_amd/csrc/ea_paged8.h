@@ -44,29 +44,36 @@ __device__ __forceinline__ float power_of_two(float s) {
 }
 
 // 0 V is no number where V is not finite, and a column that does not see a value
-// gives it the weight 0: codes that stand for no number are taken out of the
-// product and added to the columns that see them.
-// The top bit of a word's codes that are not finite (e4m3: all ones but the sign).
+// gives it the weight 0: codes that stand for no number, or for one past bf16's (and
+// f32's) range, are taken out of the product and added to the columns that see them.
+// Those are a scale's codes from one on, the signs aside: e4m3's NaN 0x7f, e5m2's
+// infinity 0x7c, or 2^k with 2^k times the scale 2^128.
 template <bool E5>
-__device__ __forceinline__ uint32_t odd_codes(uint32_t w) {
-  return ((w & (E5 ? 0x7c7c7c7cu : 0x7f7f7f7fu)) + (E5 ? 0x04040404u : 0x01010101u)) & 0x80808080u;
+__device__ __forceinline__ uint32_t odd_from(float scale) {  // 128 less the first, in every byte
+  // (2^k is the code 8 (k + 7), or 4 (k + 15))
+  const int k = 255 - (int)(__float_as_uint(scale) >> 23);
+  return 0x01010101u * (uint32_t)(128 - (E5 ? min(0x7c, 4 * (k + 15)) : min(0x7f, 8 * (k + 7))));
+}
+// The top bit of the word's codes that are such.
+template <bool E5>
+__device__ __forceinline__ uint32_t odd_codes(uint32_t w, uint32_t from = odd_from<E5>(1.0f)) {
+  return ((w & 0x7f7f7f7fu) + from) & 0x80808080u;
 }
 // The word with zeros in their place.
 template <bool E5>
-__device__ __forceinline__ uint32_t even_codes(uint32_t w) {
-  const uint32_t top = odd_codes<E5>(w);
+__device__ __forceinline__ uint32_t even_codes(uint32_t w, uint32_t from = odd_from<E5>(1.0f)) {
+  const uint32_t top = odd_codes<E5>(w, from);
   return w & ~(top | (top - (top >> 7)));
 }
-// What the others add to the sums x.
+// What such codes, times a scale, add to the sums x.
 template <bool E5>
-__device__ __forceinline__ void add_odd4(uint32_t w, float (&x)[4]) {
+__device__ __forceinline__ void add_odd4(uint32_t w, float scale, float (&x)[4]) {
   f32x2_t lo, hi;
   if constexpr (E5) lo = __builtin_amdgcn_cvt_pk_f32_bf8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_bf8(w, true);
   else lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-  x[0] += __builtin_isfinite(lo[0]) ? 0.0f : lo[0];
-  x[1] += __builtin_isfinite(lo[1]) ? 0.0f : lo[1];
-  x[2] += __builtin_isfinite(hi[0]) ? 0.0f : hi[0];
-  x[3] += __builtin_isfinite(hi[1]) ? 0.0f : hi[1];
+  const float v[4] = {lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] += __builtin_isfinite(v[i]) ? 0.0f : v[i];
 }
 
 // Shared memory of the two walks.
@@ -83,8 +90,9 @@ struct __attribute__((aligned(1024))) Many8Shared {
   uint16_t kv[2][2 * kPagedWideStep * D];  // two steps' buffers: K, then V
   int64_t off[3][kPagedWideStep];
   float ks[2][kPagedWideStep];   // K's scales (fp16 queries)
-  int no_vs[2][kPagedWideStep];  // whether a V row's scale is none
-  int odd[2][kWaves];            // whether a wave found such a scale, or codes that are not finite
+  float vs[2][kPagedWideStep];   // V's, NaN for none
+  int odd[2][kWaves];            // whether a wave found such a scale, or odd codes
+  int lim[kWaves];               // the keys that every column of a wave sees
 };
 
 // Few columns: each wave walks its own 64 keys of a step of 256, codes from the
@@ -94,7 +102,11 @@ struct __attribute__((aligned(1024))) Many8Shared {
 // A lane's 16 bytes of a K row are two steps' k indices, Q's are taken alike.  A V
 // row's lane has D / 16 neighbouring codes of each of the sixteen keys whose
 // scores its column's accumulators hold; a byte permutation puts two keys' codes of
-// one d side by side, and widening them gives the operand.
+// one d side by side, and widening them gives the operand.  Bound by HBM where there
+// is work for the chip: 48 ragged sequences of up to 8K keys, 4 heads over each of 8,
+// 85 us, 4.75 TB/s (a wave's step of 32 keys, its scales as f32 factors: 96); one
+// sequence alone by the chain of its round trips (1000 keys 10.3 us, as over 16 bits).
+// Two waves a SIMD: their registers hold the step's codes.
 template <int D, bool BF, bool E5, int COLS>
 __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& ps, const Seg* seg, Few8Shared<D>& sh,
                                           int total, int parts, int block) {
@@ -376,7 +388,7 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
 #pragma unroll
               for (int t = 0; t < NC; ++t) {
                 float x[4] = {acc[t][j][i], acc[t][j + 1][i], acc[t][j + 2][i], acc[t][j + 3][i]};
-                if (k + kk < lim[t]) add_odd4<E5>(v, x);
+                if (k + kk < lim[t]) add_odd4<E5>(v, 1.0f, x);
                 acc[t][j][i] = x[0], acc[t][j + 1][i] = x[1], acc[t][j + 2][i] = x[2], acc[t][j + 3][i] = x[3];
               }
             }
@@ -393,7 +405,14 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
 
 // Many columns: steps of 64 keys, widened on the way to shared memory by the
 // thread that fetched them (a wave's column tiles share the work), one step ahead
-// of the products; tiles and products as for a cache in 16 bits.
+// of the products; tiles and products as for a cache in 16 bits.  Bound by the
+// vector instructions and products of a step, about half and a third of its clocks:
+// 32 sequences that share 64K keys, 4 heads over each of 8, 97 us, as over 16 bits,
+// whose bytes are twice as many (scales as f32 factors 107).  Without a gain: widening
+// between the products of the step before (102), weights of sixteen keys computed
+// under the products of the sixteen before (98; one product and six instructions in
+// turn, forced, 116).  One fp16 weight instead of two bf16 values needs V relative to
+// a largest scale, which a key that a mask hides may set: small values would go.
 template <int D, bool BF, bool E5, int COLS>
 __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& ps, const Seg* seg, const Seg* own,
                                            Many8Shared<D>& sh, int total, int parts, int block) {
@@ -436,11 +455,13 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
     const int my = wid * 16 + (lane & 15);
     const float* scales = lane & 16 ? a.vs : a.ks;
     auto entry = [&](int k) { return k + my < kb ? pages[div_fast(k + my, a.page)] : -1; };
+    bool lacking;                                // some of the wave's rows do not exist
     auto place = [&](int slot, int k, int pg) {  // the rows' offsets, -1: no such row; the scale
       const int key = k + my, in = key - div_fast(key, a.page) * a.page_size;
       const bool there = (uint32_t)pg < (uint32_t)a.n_pages;
       const int64_t off = there ? pg * a.page_bytes + (int64_t)in * D : -1;
       if (lane < 16) s_off[slot][my] = off;
+      lacking = __ballot(!there) != 0;
       __builtin_amdgcn_wave_barrier();
       return there ? scales[((int64_t)pg * a.hkv + h) * a.n_blocks + div_fast(in, a.block)] : 1.0f;
     };
@@ -454,35 +475,60 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
         vr[i] = *reinterpret_cast<const uint4*>(vbase + (off < 0 ? 0 : off));
       }
     };
-    // widened to buffer b; zeros in the place of values whose rows do not exist and
-    // of codes that stand for no number, which sh.odd tells of
-    auto land = [&](int b, int slot) {
+    int lim_all = 0;  // the keys that every column of the workgroup sees
+    // Widened to buffer b.  Zeros in the place of values whose rows do not exist, and
+    // of odd codes where some column may not see them, which sh.odd tells of.  (Where
+    // all columns see all of the step's rows, e4m3's NaN is right as it is; an
+    // infinity's second weight may be 0.  Without the checks 64K prefix 99 us to 97.)
+    auto land = [&](int b, int slot, int k) {
       uint16_t* sK = sKV + b * BUF;
       uint16_t* sV = sK + KEYS * D;
       scale = power_of_two(scale);
       const bool none = scale != scale;
-      uint32_t odd = none && lane >= 16 && lane < 32;
+      // (a scale under which every finite code is a number in bf16)
+      const bool care = E5 || lacking || k + KEYS > lim_all || __any(!(scale < 0x1p120f));
       if (!BF && lane < 16) sh.ks[b][my] = scale;
-      if (lane >= 16 && lane < 32) sh.no_vs[b][my] = none;
+      if (lane >= 16 && lane < 32) sh.vs[b][my] = scale;
+      bool any = false;
+      uint4 v[LPW];
+      float vs[LPW];
 #pragma unroll
       for (int i = 0; i < LPW; ++i) {
         const int row = i * RPI + lane / LPR, r = wid * 16 + row, pc = 2 * (lane % LPR);
-        const float ks = BF ? __shfl(scale, row) : 1.0f, vs = __shfl(scale, 16 + row);
+        const float ks = BF ? __shfl(scale, row) : 1.0f;
+        vs[i] = __shfl(scale, 16 + row);
         uint4* tk = reinterpret_cast<uint4*>(sK + r * D);
-        uint4* tv = reinterpret_cast<uint4*>(sV + r * D);
         tk[pc ^ swz_k<D>(r)] = widen8<BF, E5>(kr[i].x, kr[i].y, ks);
         tk[(pc + 1) ^ swz_k<D>(r)] = widen8<BF, E5>(kr[i].z, kr[i].w, ks);
-        uint4 v = vr[i];
-        if (s_off[slot][r] < 0 || vs != vs) v = make_uint4(0, 0, 0, 0);
-        const uint32_t o = odd_codes<E5>(v.x) | odd_codes<E5>(v.y) | odd_codes<E5>(v.z) | odd_codes<E5>(v.w);
-        odd |= o;
-        if (__builtin_expect(__any(o != 0), 0))
-          v = make_uint4(even_codes<E5>(v.x), even_codes<E5>(v.y), even_codes<E5>(v.z), even_codes<E5>(v.w));
-        const float use = vs != vs ? 1.0f : vs;
-        tv[pc ^ swz_v<D>(r)] = widen8<true, E5>(v.x, v.y, use);
-        tv[(pc + 1) ^ swz_v<D>(r)] = widen8<true, E5>(v.z, v.w, use);
+        v[i] = vr[i];
       }
-      const bool any = __any(odd != 0);
+      if (care) {
+        asm volatile("" ::: "memory");  // a branch
+        uint32_t odd = none && lane >= 16 && lane < 32;
+#pragma unroll
+        for (int i = 0; i < LPW; ++i) {
+          if (s_off[slot][wid * 16 + i * RPI + lane / LPR] < 0 || vs[i] != vs[i]) v[i] = make_uint4(0, 0, 0, 0);
+          const uint32_t f = odd_from<E5>(vs[i]);
+          odd |= odd_codes<E5>(v[i].x, f) | odd_codes<E5>(v[i].y, f) | odd_codes<E5>(v[i].z, f) | odd_codes<E5>(v[i].w, f);
+        }
+        any = __any(odd != 0);
+        if (__builtin_expect(any, 0)) {
+#pragma unroll
+          for (int i = 0; i < LPW; ++i) {
+            const uint32_t f = odd_from<E5>(vs[i]);
+            v[i] = make_uint4(even_codes<E5>(v[i].x, f), even_codes<E5>(v[i].y, f), even_codes<E5>(v[i].z, f),
+                              even_codes<E5>(v[i].w, f));
+            if (vs[i] != vs[i]) vs[i] = 1.0f;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < LPW; ++i) {
+        const int r = wid * 16 + i * RPI + lane / LPR, pc = 2 * (lane % LPR);
+        uint4* tv = reinterpret_cast<uint4*>(sV + r * D);
+        tv[pc ^ swz_v<D>(r)] = widen8<true, E5>(v[i].x, v[i].y, vs[i]);
+        tv[(pc + 1) ^ swz_v<D>(r)] = widen8<true, E5>(v[i].z, v[i].w, vs[i]);
+      }
       if (lane == 0) sh.odd[b][wid] = any;
     };
     scale = place(0, ka, entry(ka));
@@ -504,6 +550,7 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) lim_min = min(lim_min, __shfl_xor(lim_min, o));
     lim_min = __builtin_amdgcn_readfirstlane(lim_min);
+    if (lane == 0) sh.lim[wid] = lim_min;
 
     f32x16_t acc[ND];
 #pragma unroll
@@ -615,14 +662,14 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
           const int64_t off = s_off[slot][kk];
           if (off < 0) continue;
           const char* vrow = a.pv + head_off + off + 4 * g;
-          const bool none = sh.no_vs[b][kk];  // (NaN in all of the row)
+          const float vs = sh.vs[b][kk];  // (NaN: in all of the row)
 #pragma unroll
           for (int i = 0; i < ND; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const uint32_t v = *reinterpret_cast<const uint32_t*>(vrow + 32 * i + 8 * r);
               float x[4] = {acc[i][4 * r], acc[i][4 * r + 1], acc[i][4 * r + 2], acc[i][4 * r + 3]};
-              if (k + kk < lim) add_odd4<E5>(none ? 0x7f7f7f7fu : v, x);
+              if (k + kk < lim) add_odd4<E5>(vs != vs ? 0x7f7f7f7fu : v, vs != vs ? 1.0f : vs, x);
 #pragma unroll
               for (int e = 0; e < 4; ++e) acc[i][4 * r + e] = x[e];
             }
@@ -632,18 +679,19 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
 
     // A step's codes are fetched two steps ahead and land, widened, one step ahead,
     // before the products of the step between: their loads had a whole step's time.
-    land(0, 0);
+    land(0, 0, ka);
     if (ka + KEYS < kb) {
       scale = place(1, ka + KEYS, next_pg);
       next_pg = entry(ka + 2 * KEYS);
       fetch(1);
     }
     __syncthreads();
+    lim_all = __builtin_amdgcn_readfirstlane(min(min(sh.lim[0], sh.lim[1]), min(sh.lim[2], sh.lim[3])));
     int b = 0, slot = 0;
     for (int k = ka; k < kb; k += KEYS, b ^= 1) {
       const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot1 == 2 ? 0 : slot1 + 1;
       if (k + KEYS < kb) {
-        land(b ^ 1, slot1);
+        land(b ^ 1, slot1, k + KEYS);
         if (k + 2 * KEYS < kb) {
           scale = place(slot2, k + 2 * KEYS, next_pg);
           next_pg = entry(k + 3 * KEYS);
@@ -760,6 +808,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged8_both_kernel(const PagedArg
   int to, ts;
   schedule<OWN, KO, SHARED, KS>(a, own, shared, seg_o, seg_s, &to, &ts);
   const int n = gridDim.x;
+  // Workgroups are dealt to the walks by the bytes they read.  (Own keys weighted
+  // more, up to 12 times: slower.  An equal part of both walks for every workgroup,
+  // neighbours beginning with different ones: 8K prefix 47.6 us to 60.5.)
   const double ws = (double)ts * KS, wo = (double)to * KO;
   const int ns = ts == 0 ? 0 : to == 0 ? n : min(max((int)(n * ws / (ws + wo) + 4.0) / 8 * 8, 8), n - 8);
   const int ps = min(ns, ts), po = min(n - ns, to);

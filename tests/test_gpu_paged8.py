@@ -216,6 +216,37 @@ def test_what_one_row_sees_another_does_not(walk, code):
             assert mine.isnan().all()
 
 
+@pytest.mark.parametrize("walk", ["few", "many", "both"])
+@pytest.mark.parametrize("code", ["e4m3", "e5m2"])
+def test_values_past_the_range_of_32_bits_stay_with_who_sees_them(walk, code):
+    """The last key of a draft, seen by the last row alone, has V codes up to the
+    largest under the largest scale, 2^128 and more among them: the other rows are
+    as without, and the last row has an infinity of its sign where a value is one
+    (the walk over few columns, which scales the weights: at least 2^110, or one)."""
+    n_q, hq, d, page = {"few": 3, "many": 20, "both": 5}[walk], 4, 128, 16
+    lens = [200, 170]
+    groups = [(0, 2, 160)] if walk == "both" else []
+    if walk == "both":
+        lens = [160, 170]
+    kv, table, rng = _batch(lens, groups, page, 1, 1, d, code, 12)
+    q = torch.from_numpy(rng.standard_normal((2 * n_q, hq, d))).bfloat16().cuda()
+    starts = [0, n_q, 2 * n_q]
+    clean = _check(q, kv, table, lens, starts, groups, code, "bf16")
+    last = lens[0] - 1
+    pg, row = table[0, last // page], last % page
+    (vc, vs), top = kv[1], C.TOP[code]
+    vc[pg, 0, row] = 0
+    vc[pg, 0, row, :4] = [top, -top, 1, -1]
+    vs[pg, 0, row] = 2.0 ** 120
+    got = _run(q, [C.Cache(*x, code) for x in kv], table, lens, starts, groups, d ** -0.5)
+    others = [i for i in range(2 * n_q) if i != n_q - 1 and (walk != "both" or i < n_q)]
+    assert torch.equal(got[others], clean[others])
+    mine = got[n_q - 1].float()
+    assert (mine[:, 0] > 2.0 ** 110).all() and (mine[:, 1] < -2.0 ** 110).all()
+    if walk != "few":
+        assert mine[:, :2].isinf().all()
+
+
 def test_pages_outside_the_cache_are_invisible():
     lens, page = [100, 64], 16
     kv, table, rng = _batch(lens, [], page, 16, 2, 64, "e4m3", 8)
@@ -239,6 +270,39 @@ def test_as_sixteen_bits():
     ea.attention_paged(R.rel(src), *wide, R.rel(out), scale=d ** -0.5, table=R.i32(table), lengths=R.i32(lens))
     ref, info = R.attention(R.f64(q), C.values(*kv[0]), C.values(*kv[1]), table, lens, page, [0, 1, 2, 3], d ** -0.5)
     assert np.all(np.abs(R.f64(got) - R.f64(out).reshape(ref.shape)) <= 2 * C.attention_tol(ref, info, "bf16", d))
+
+
+def test_the_most_sequences():
+    """As many sequences and groups as a call takes, most of a key or none, their
+    schedule in shared memory beside both walks' buffers."""
+    n, page, hq, hkv, d = ea.PAGED_MAX_SEQ - 4, 4, 4, 1, 128
+    rng = np.random.default_rng(13)
+    lens = [int(x) for x in rng.integers(0, 12, n)]
+    groups = []
+    for i in range(4):
+        groups.append((i * 20, (i + 1) * 20, 8 * (i + 1)))
+        for s in range(i * 20, (i + 1) * 20):
+            lens[s] += 8 * (i + 1)
+    kv, table, rng = _batch(lens, groups, page, 2, hkv, d, "e4m3", 14)
+    q = torch.from_numpy(rng.standard_normal((n, hq, d))).bfloat16().cuda()
+    _check(q, kv, table, lens, None, groups, "e4m3", "bf16")
+    _check(q, kv, table, lens, None, [], "e4m3", "bf16")
+
+
+@pytest.mark.parametrize("lens", [[4000], [4090, 1], [4200], [2000, 3900, 0, 300]])
+def test_walks_joined_by_their_last_part(lens):
+    """Table rows about as long as those whose parts the last one joins; the same
+    bits on every run, the arrival counters left at zero."""
+    hq, hkv, d, page = 8, 2, 128, 16
+    kv, table, rng = _batch(lens, [], page, 16, hkv, d, "e4m3", 15)
+    table = table[:, :max(-(-n // page) for n in lens)]
+    q = torch.from_numpy(rng.standard_normal((len(lens), hq, d))).bfloat16().cuda()
+    dev = [C.Cache(codes, s, "e4m3") for codes, s in kv]
+    got = _check(q, kv, table, lens, None, [], "e4m3", "bf16", dev=dev)
+    ws = ea.new_workspace(ea.attention_paged_workspace(C.rel(q.view(len(lens), -1)), dev[0].rel, len(lens)))
+    for _ in range(3):
+        assert torch.equal(_run(q, dev, table, lens, None, [], d ** -0.5, workspace=ws), got)
+        assert not ws[:ea.WS_COUNTER_BYTES].any()
 
 
 def test_codes_past_four_gib():
