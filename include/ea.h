@@ -560,11 +560,13 @@ typedef struct ea_page_rows {
    Codes are rounded to nearest, ties to even; NaN is kept, an infinity is one
    in EA_E5M2 and NaN in EA_E4M3.  Rows behind the new ones stay as they are and
    stand for nothing.  A row whose page lies outside the cache, or that has no
-   key (more rows than keys), is not written.  Pages that several sequences
-   share, or a block's rows given twice, must not be among those written.
+   key (more rows than keys), is not written.  A scale there that is no positive
+   number counts as none.  Pages that several sequences share, or a block's rows
+   given twice, must not be among those written.
    xk, xv: [T, Hkv d], or [.., Hkv, T, d] (forms and partitions as ea_heads' q),
-   f32, bf16 or f16; d a multiple of 16 from 16 to 512; (stride + 1) * page_size < 2^31 - 1024,
-   n_seq <= EA_PAGED_MAX_SEQ.  Lengths are taken as at most a table row's keys.
+   f32, bf16 or f16; d a multiple of 16 from 16 to 512; Hkv d < 2^26,
+   Hkv T < 2^30, (stride + 1) * page_size < 2^31 - 1024, n_seq <=
+   EA_PAGED_MAX_SEQ.  Lengths are taken as at most a table row's keys.
    Outputs must not overlap anything else.  Asynchronous on `stream`: no plan, no
    workspace, never allocates; results do not depend on timing.  Errors:
    EA_ERR_ARG, EA_ERR_DTYPE, EA_ERR_UNSUPPORTED, EA_ERR_HIP. */
@@ -578,8 +580,8 @@ int ea_pages_read(const ea_relation* k, const ea_relation* v, const ea_relation*
 /* ea_attention_paged over such a cache, of keys and values code * scale.  Scales
    are powers of two, as ea_pages_write gives them; any other stands for NaN.
    q and out are bf16 or f16; the weights' products with V take them as two bf16
-   values.  Everything else, the workspace and its size's call
-   among it, is as there. */
+   values.  Everything else, the workspace and its size's call among it, is as
+   there. */
 int ea_attention_paged8(const ea_relation* q, const ea_relation* k, const ea_relation* v, const ea_relation* k_scale,
                         const ea_relation* v_scale, ea_relation* out, const ea_paged* batch, void* workspace,
                         int64_t ws_bytes, void* stream);

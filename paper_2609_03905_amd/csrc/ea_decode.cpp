@@ -358,9 +358,13 @@ int plan_paged(const ea_relation* q, const ea_relation* k, const ea_paged* b, bo
   // sequence that outweighs its batch has more: 128K keys beside 63 times 200, 32
   // over 8, 118 and 115, beside 511 times 200, 4 over 1, 62 and 45; with fewer
   // tiles than the rule asks for (beside 7 short ones, 4 over 1) 90 and 30.
-  const int64_t steps = (b->stride * k->shape[2] + kPagedStep - 1) / kPagedStep;
+  // Over codes, in steps of 256 keys, 16 (one sequence, 32 heads over 8: 2000 keys
+  // 11.0 us and 12.5 with the launch, 4000 keys 12.6 and 13.1, 6000 keys 15.4 and
+  // 14.1; 4 over 1 11.8 and 13.3 at 4000 keys, 12.9 and 13.3 at 6000).
+  const bool codes = is_code(k->dtype);
+  const int64_t keys = codes ? kPaged8Step : kPagedStep, steps = (b->stride * k->shape[2] + keys - 1) / keys;
   p->own.fused = b->n_group == 0 && p->own.cols <= 32 && p->own.tiles <= kWsCounterBytes / 4 &&
-                 (steps <= 12 || p->own.tiles * 2 >= p->own.grid);
+                 (steps <= (codes ? 16 : 12) || p->own.tiles * 2 >= p->own.grid);
   p->seg = kWsCounterBytes;
   int64_t at = p->seg + align256((b->n_seq + b->n_group) * (int64_t)sizeof(PagedSeg));
   int i = 0;
@@ -533,6 +537,7 @@ int cache8(const ea_relation* xk, const ea_relation* xv, const ea_relation* k, c
   if ((b.stride + (int64_t)1) * page > INT32_MAX - 1024)
     return fail(EA_ERR_UNSUPPORTED, "a table row of 2^31 keys or more");
   if (2 * hkv * a.xk.t > INT32_MAX) return fail(EA_ERR_UNSUPPORTED, "2^30 rows and heads or more");
+  if (hkv * d >= 1 << 26) return fail(EA_ERR_UNSUPPORTED, "rows of 2^26 elements or more");
   if (!b.lengths || !b.table) return fail(EA_ERR_ARG, "NULL lengths or table");
   if (!b.q_start && a.xk.t < b.n_seq) return fail(EA_ERR_ARG, "%d rows for %d sequences", a.xk.t, b.n_seq);
   const ea_relation* const outs_w[] = {k, v, ks, vs};

@@ -135,8 +135,8 @@ __device__ __forceinline__ int tiles_of(int rows, int g, int cols) {
 
 // Every segment's first step and tile, by the whole workgroup: the groups' (none
 // where SHARED is 0) and the sequences', whose loads are one round trip.  *to and
-// *ts: the steps (of OWN_KEYS and SHARED_KEYS keys) of all; none where there are more tiles than the rows can have,
-// that is, where the sequences' rows overlap.
+// *ts: the steps (of OWN_KEYS and SHARED_KEYS keys) of all; none where there are
+// more tiles than the rows can have, that is, where the sequences' rows overlap.
 template <int OWN, int OWN_KEYS, int SHARED, int SHARED_KEYS>
 __device__ __forceinline__ void schedule(const PagedArgs& a, const PagedPass& own, const PagedPass& shared, Seg* seg_o,
                                          Seg* seg_s, int* to, int* ts) {

@@ -60,6 +60,19 @@ def test_rows_refusals(call, code, change):
     assert rows(call, **change) == code, ea.lib().ea_last_error()
 
 
+@pytest.mark.parametrize("call", ["write", "read"])
+def test_rows_of_more_elements_than_are_counted(call):
+    """(rows of 2^26 elements; and one head less, whose batch is then looked at)"""
+    for h, want, change in ((2 ** 20, UNSUPPORTED, {}), (2 ** 20 - 1, ARG, dict(table=None))):
+        part = [[0, 1], [0, h], [0, 1], [0, 64]]
+        got = rows(call, xk=_at(bare([3, h * 64], "bf16"), BASE), xv=_at(bare([3, h * 64], "bf16"), BASE + (1 << 32)),
+                   k=_at(bare([1, h, 1, 64], "e4m3", part), BASE + (2 << 32)),
+                   v=_at(bare([1, h, 1, 64], "e4m3", part), BASE + (3 << 32)),
+                   ks=_at(bare([1, h, 1], "f32"), BASE + (4 << 32)), vs=_at(bare([1, h, 1], "f32"), BASE + (5 << 32)),
+                   **change)
+        assert got == want, ea.lib().ea_last_error()
+
+
 def _at(r, address):
     assert ea.lib().ea_relation_set_data(r.handle, ctypes.c_void_p(address), r.nbytes) == OK
     return r
