@@ -42,6 +42,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 template <bool BF>
 __device__ __forceinline__ void split_p(float a, float b, uint32_t& hi, uint32_t& lo) {
   hi = pack2<BF>(a, b);
+  asm("" : "+v"(hi));  // (else a is rounded once more, alone, for what it leaves)
   if constexpr (BF) lo = pack2<BF>(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
   else lo = pack2<BF>(a - f16_to_f32((uint16_t)hi), b - f16_to_f32((uint16_t)(hi >> 16)));
 }

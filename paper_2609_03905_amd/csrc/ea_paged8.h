@@ -426,6 +426,14 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
   uint16_t* sKV = sh.kv[0];
   auto& s_off = sh.off;
 
+  // (one by one in scalar registers: they are too many to stay there, and the
+  // arguments' come back from a spill in eights)
+  FastDiv dpage = a.page, dblock = a.block;
+  int page_size = a.page_size, n_pages = a.n_pages;
+  int64_t page_bytes = a.page_bytes, page_scales = (int64_t)a.hkv * a.n_blocks;
+  asm("" : "+s"(dpage.d), "+s"(dpage.m), "+s"(dpage.s), "+s"(dblock.d), "+s"(dblock.m), "+s"(dblock.s));
+  asm("" : "+s"(page_size), "+s"(n_pages), "+s"(page_bytes), "+s"(page_scales));
+
   const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, g = lane >> 5;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wc = wid % CW, wk = wid / CW;  // the wave's columns, and its part of a step's keys
@@ -453,17 +461,17 @@ __device__ __forceinline__ void walk_many8(const PagedArgs& a, const PagedPass& 
     // a wave fetches 16 of a step's rows; lane i (and i + 16, ...) looks after row
     // i, the first 16 after K's scale, the next after V's
     const int my = wid * 16 + (lane & 15);
-    const float* scales = lane & 16 ? a.vs : a.ks;
-    auto entry = [&](int k) { return k + my < kb ? pages[div_fast(k + my, a.page)] : -1; };
+    const float* scales = (lane & 16 ? a.vs : a.ks) + (int64_t)h * a.n_blocks;
+    auto entry = [&](int k) { return k + my < kb ? pages[div_fast(k + my, dpage)] : -1; };
     bool lacking;                                // some of the wave's rows do not exist
     auto place = [&](int slot, int k, int pg) {  // the rows' offsets, -1: no such row; the scale
-      const int key = k + my, in = key - div_fast(key, a.page) * a.page_size;
-      const bool there = (uint32_t)pg < (uint32_t)a.n_pages;
-      const int64_t off = there ? pg * a.page_bytes + (int64_t)in * D : -1;
+      const int key = k + my, in = key - div_fast(key, dpage) * page_size;
+      const bool there = (uint32_t)pg < (uint32_t)n_pages;
+      const int64_t off = there ? pg * page_bytes + (int64_t)in * D : -1;
       if (lane < 16) s_off[slot][my] = off;
       lacking = __ballot(!there) != 0;
       __builtin_amdgcn_wave_barrier();
-      return there ? scales[((int64_t)pg * a.hkv + h) * a.n_blocks + div_fast(in, a.block)] : 1.0f;
+      return there ? scales[pg * page_scales + div_fast(in, dblock)] : 1.0f;
     };
     uint4 kr[LPW], vr[LPW];
     float scale;
