@@ -549,6 +549,9 @@ typedef struct ea_page_rows {
   const int32_t* q_start; /* [n_seq + 1] ascending first rows; NULL: one a sequence */
   const int32_t* lengths; /* [n_seq] keys, the rows among them                      */
   const int32_t* table;   /* [n_seq][stride] pages                                  */
+  const int32_t* slots;   /* NULL, or [T] the rows' slots from ea_pages_extend: a
+                             sequence whose first row's is negative has no keys for
+                             them (the call was not served)                       */
 } ea_page_rows;
 /* Quantises rows into the cache.  Rows q_start[s] .. q_start[s+1]-1 of xk and xv
    are the last of sequence s's lengths[s] keys (as in ea_attention_paged).  For
@@ -560,7 +563,7 @@ typedef struct ea_page_rows {
    Codes are rounded to nearest, ties to even; NaN is kept, an infinity is one
    in EA_E5M2 and NaN in EA_E4M3.  Rows behind the new ones stay as they are and
    stand for nothing.  A row whose page lies outside the cache, or that has no
-   key (more rows than keys), is not written.  A scale there that is no positive
+   key (more rows than keys, or its slots say so), is not written.  A scale there that is no positive
    number counts as none.  Pages that several sequences share, or a block's rows
    given twice, must not be among those written.
    xk, xv: [T, Hkv d], or [.., Hkv, T, d] (forms and partitions as ea_heads' q),

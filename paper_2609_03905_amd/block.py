@@ -139,9 +139,9 @@ class LlamaBlockShare:
         """The last forward's keys and values to the cache: token t to slot
         slots[t] (queries are written again, as they are).  A cache in 8 bits takes
         tokens q_start[s] .. q_start[s + 1] - 1 as the newest of its sequence s
-        (None: token s) instead."""
+        (None: token s); slots, if given, say whether they have places."""
         if cache.scales is not None:
-            cache.write(layer, self.k, self.v, q_start)
+            cache.write(layer, self.k, self.v, q_start, slots)
             return
         ea.heads(self.qkv, self.q, cache.k[layer], cache.v[layer], slots=slots, **self.head_options(self.positions))
 
@@ -176,11 +176,11 @@ class LlamaBlockDecode:
     ``rows`` tokens a step (x: [rows, hidden], sequence by sequence), their
     slots and positions from cache.extend, at most ``groups`` shared prefixes
     (None: as many as sequences).  Over a cache in 8 bits the head rows go through
-    rows of the step's own, and are written to the sequences' newest places
-    (q_start, not slots, says whose they are).  The calls' plans are made and their workspace
-    is allocated here, so a step can be captured at once, and steps of several
-    decoders may overlap in time (steps of one may not: its activations and its
-    workspace are one step's)."""
+    rows of the step's own, and are written to the sequences' newest places:
+    q_start says whose they are, slots (or None) only whether extend was served.
+    The calls' plans are made and their workspace is allocated here, so a step can
+    be captured at once, and steps of several decoders may overlap in time (steps
+    of one may not: its activations and its workspace are one step's)."""
 
     def __init__(self, share: LlamaBlockShare, cache: KVCache, rows: int, layer: int = 0, device="cuda",
                  groups: int | None = None):
@@ -231,7 +231,7 @@ class LlamaBlockDecode:
             heads = [("heads", lambda: ea.heads(self.qkv, self.q, k, v, slots=slots, **s.head_options(positions)))]
         else:
             heads = [("heads", lambda: ea.heads(self.qkv, self.q, self.kr, self.vr, **s.head_options(positions))),
-                     ("write", lambda: c.write(self.layer, self.kr, self.vr, q_start))]
+                     ("write", lambda: c.write(self.layer, self.kr, self.vr, q_start, slots))]
         return [
             joinagg("rmsnorm1"),
             joinagg("qkv_gemm"),

@@ -60,20 +60,23 @@ class KVCache:
                         slots=slots, positions=positions, workspace=self._workspace)
         return slots, positions
 
-    def write(self, layer: int, xk: ea.Relation, xv: ea.Relation, q_start: torch.Tensor | None = None):
+    def write(self, layer: int, xk: ea.Relation, xv: ea.Relation, q_start: torch.Tensor | None = None,
+              slots: torch.Tensor | None = None):
         """Rows q_start[s] .. q_start[s + 1] - 1 (None: row s) of keys and values
-        quantised into the newest places of sequence s (8 bits: ea.pages_write)."""
-        ea.pages_write(xk, xv, self.k[layer], self.v[layer], **self._rows(layer, q_start))
+        quantised into the newest places of sequence s (8 bits: ea.pages_write);
+        with the slots that extend gave, none where it was not served."""
+        ea.pages_write(xk, xv, self.k[layer], self.v[layer], **self._rows(layer, q_start, slots))
 
-    def read(self, layer: int, xk: ea.Relation, xv: ea.Relation, q_start: torch.Tensor | None = None):
+    def read(self, layer: int, xk: ea.Relation, xv: ea.Relation, q_start: torch.Tensor | None = None,
+             slots: torch.Tensor | None = None):
         """The same rows back (8 bits: ea.pages_read)."""
-        ea.pages_read(self.k[layer], self.v[layer], xk, xv, **self._rows(layer, q_start))
+        ea.pages_read(self.k[layer], self.v[layer], xk, xv, **self._rows(layer, q_start, slots))
 
-    def _rows(self, layer, q_start):
+    def _rows(self, layer, q_start, slots):
         if self.scales is None:
             raise ea.EAError(ea.ERR_ARG, f"a {self.data.dtype} cache is written by ea.heads")
         return dict(k_scale=self.k_scale[layer], v_scale=self.v_scale[layer], table=self.table, lengths=self.lengths,
-                    q_start=q_start)
+                    q_start=q_start, slots=slots)
 
     def select(self, parent: torch.Tensor):
         """Sequence i becomes a copy of sequence parent[i] (-1: empty)."""

@@ -181,6 +181,7 @@ __device__ __forceinline__ Place place_of(const Cache8Args& a, const int* starts
   }
   if (s >= a.n_seq || t < r0 || t >= r1 || t >= a.rows) return p;
   p.mine = true;
+  if (a.slots && a.slots[r0] < 0) return p;
   p.at = min(max(a.len[s], 0), a.stride * a.page_size) - r1 + t;
   if (p.at < 0) return p;
   const int i = div_fast(p.at, a.page);
@@ -222,6 +223,7 @@ __device__ __forceinline__ int schedule_write(const Cache8Args& a, Span* spans) 
     s.r1 = r1;
     s.end = min(max(a.len[i], 0), a.stride * a.page_size);
     s.first = max(s.end - (r1 - r0), 0);
+    if (a.slots && r1 > r0 && r0 < a.rows && a.slots[r0] < 0) s.first = s.end;  // (its length counts no such rows)
     spans[i] = s;
     if (s.end > s.first) blocks += div_fast(s.end - 1, a.block) - div_fast(s.first, a.block) + 1;
     rows += r1 - r0;

@@ -548,8 +548,8 @@ int cache8(const ea_relation* xk, const ea_relation* xv, const ea_relation* k, c
     for (const ea_relation* r : all)
       if (r != o ? overlap(o, r) : false) return fail(EA_ERR_ARG, "an output overlaps another relation");
     if (overlap(span(o), {ints(b.q_start, b.n_seq + (int64_t)1), ints(b.lengths, b.n_seq),
-                          ints(b.table, b.n_seq * (int64_t)b.stride)}))
-      return fail(EA_ERR_ARG, "an output overlaps q_start, lengths or the table");
+                          ints(b.table, b.n_seq * (int64_t)b.stride), ints(b.slots, a.xk.t)}))
+      return fail(EA_ERR_ARG, "an output overlaps q_start, lengths, the table or the slots");
   }
   if (write ? k == v || ks == vs : xk == xv) return fail(EA_ERR_ARG, "K and V are one relation");
   a.pxk = (const char*)xk->data;
@@ -561,6 +561,7 @@ int cache8(const ea_relation* xk, const ea_relation* xv, const ea_relation* k, c
   a.q_start = b.q_start;
   a.len = b.lengths;
   a.table = b.table;
+  a.slots = b.slots;
   a.n_seq = b.n_seq;
   a.stride = b.stride;
   a.n_pages = (int32_t)k->shape[0];

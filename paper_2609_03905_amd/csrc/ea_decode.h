@@ -152,7 +152,7 @@ struct Cache8Args {
   const char *pxk, *pxv;      // read by the write, written by the read
   char *pk, *pv;              // codes
   float *ks, *vs;             // scales [pages][heads][blocks of a page]
-  const int32_t *q_start, *len, *table;
+  const int32_t *q_start, *len, *table, *slots;
   int32_t n_seq, stride, n_pages, page_size, rows, hkv, d;
   int32_t block_rows, n_blocks;  // rows of a scale's block, blocks of a page
   FastDiv page, block;

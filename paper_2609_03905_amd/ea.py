@@ -59,7 +59,7 @@ class _Paged(ctypes.Structure):
 
 class _PageRows(ctypes.Structure):
     _fields_ = [("n_seq", ctypes.c_int32), ("stride", ctypes.c_int32), ("q_start", ctypes.c_void_p),
-                ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p)]
+                ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("slots", ctypes.c_void_p)]
 
 
 class _Pages(ctypes.Structure):
@@ -554,16 +554,18 @@ def attention_paged(q: Relation, k: Relation, v: Relation, out: Relation, *, sca
         _check(lib().ea_attention_paged8(q._h, k._h, v._h, k_scale._h, v_scale._h, out._h, ctypes.byref(b), ws, n, s))
 
 
-def _page_rows(table, lengths, q_start):
+def _page_rows(x, table, lengths, q_start, slots):
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise EAError(ERR_ARG, "table is no [sequences, pages] tensor")
     n, stride = table.shape
     return _PageRows(n, stride, _device_array(q_start, "q_start", (n + 1,), optional=True),
-                     _device_array(lengths, "lengths", (n,)), _device_array(table, "table", (n, stride)))
+                     _device_array(lengths, "lengths", (n,)), _device_array(table, "table", (n, stride)),
+                     _device_array(slots, "slots", x.shape[-2:][:1], optional=True))
 
 
 def pages_write(xk: Relation, xv: Relation, k: Relation, v: Relation, *, k_scale: Relation, v_scale: Relation,
-                table: torch.Tensor, lengths: torch.Tensor, q_start: torch.Tensor | None = None, stream=None) -> None:
+                table: torch.Tensor, lengths: torch.Tensor, q_start: torch.Tensor | None = None,
+                slots: torch.Tensor | None = None, stream=None) -> None:
     """Rows quantised into a cache in 8 bits.  Rows q_start[s] .. q_start[s + 1]
     - 1 (None: row s) of ``xk`` and ``xv`` ([T, Hkv d] or [.., Hkv, T, d]) are
     the last of sequence s's lengths[s] keys, which lie in the pages table[s] of
@@ -572,19 +574,22 @@ def pages_write(xk: Relation, xv: Relation, k: Relation, v: Relation, *, k_scale
     power of two, in ``k_scale`` and ``v_scale`` ("f32" [pages, Hkv, n]): the
     least under which the largest new element has a code, or the one that the
     block has from earlier rows, if that is larger; where it grows those rows are
-    rounded again.  A block whose first row is written is begun anew.  The arrays
-    are read when the kernel runs."""
+    rounded again.  A block whose first row is written is begun anew.  ``slots``
+    [T]: the rows' slots from pages_extend; a sequence whose first row's is
+    negative gets none (that call was not served).  The arrays are read when the
+    kernel runs."""
     _on_device(xk, xv, k, v, k_scale, v_scale)
-    rows = _page_rows(table, lengths, q_start)
+    rows = _page_rows(xk, table, lengths, q_start, slots)
     _check(lib().ea_pages_write(xk._h, xv._h, k._h, v._h, k_scale._h, v_scale._h, ctypes.byref(rows), _stream(stream)))
 
 
 def pages_read(k: Relation, v: Relation, xk: Relation, xv: Relation, *, k_scale: Relation, v_scale: Relation,
-               table: torch.Tensor, lengths: torch.Tensor, q_start: torch.Tensor | None = None, stream=None) -> None:
+               table: torch.Tensor, lengths: torch.Tensor, q_start: torch.Tensor | None = None,
+               slots: torch.Tensor | None = None, stream=None) -> None:
     """The rows that pages_write puts into a cache, read back into ``xk`` and
     ``xv``: code times scale, rounded once (zeros where a row has no key)."""
     _on_device(xk, xv, k, v, k_scale, v_scale)
-    rows = _page_rows(table, lengths, q_start)
+    rows = _page_rows(xk, table, lengths, q_start, slots)
     _check(lib().ea_pages_read(k._h, v._h, k_scale._h, v_scale._h, xk._h, xv._h, ctypes.byref(rows), _stream(stream)))
 
 

@@ -60,6 +60,20 @@ def test_rows_refusals(call, code, change):
     assert rows(call, **change) == code, ea.lib().ea_last_error()
 
 
+def test_rows_slots():
+    """Slots lie under no output."""
+    xk, xv = (_at(bare([9, 128], "bf16"), BASE + i * (1 << 20)) for i in range(2))
+    part = [range(31), [0, 2], [0, 16], [0, 64]]
+    k, v = (_at(bare([30, 2, 16, 64], "e4m3", part), BASE + i * (1 << 20)) for i in (2, 3))
+    ks, vs = (_at(bare([30, 2, 4], "f32"), BASE + i * (1 << 20)) for i in (4, 5))
+    for call, rels, outs in (("write", (xk, xv, k, v, ks, vs), (k, v, ks, vs)), ("read", (k, v, ks, vs, xk, xv), (xk, xv))):
+        for o in outs:
+            at = BASE + (xk, xv, k, v, ks, vs).index(o) * (1 << 20)
+            b = E._PageRows(3, 5, 256, 512, 1024, at + o.nbytes - 4)
+            assert getattr(ea.lib(), "ea_pages_" + call)(*[r._h for r in rels], ctypes.byref(b), None) == ARG
+            assert b"slots" in ea.lib().ea_last_error()
+
+
 @pytest.mark.parametrize("call", ["write", "read"])
 def test_rows_of_more_elements_than_are_counted(call):
     """(rows of 2^26 elements; and one head less, whose batch is then looked at)"""

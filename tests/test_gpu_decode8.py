@@ -169,6 +169,42 @@ def test_scales_of_blocks_behind_a_copied_row_stay():
     assert z.tolist() == [[0, 1, 2, 3], [0, 1, 2, 7], [8, 9, 10, 11], [12, 13, 14, 15]]
 
 
+def test_a_step_that_has_no_places_leaves_the_cache():
+    """extend finds too few free pages: the step that follows writes nothing, eager
+    or captured; when pages are free again, the same calls are served."""
+    w, tokens = _weights(6)
+    share = _share(PROMPT, w, tokens(PROMPT))
+    share.forward()
+    cache = KVCache(1, 8, HEADS_KV, 16, 128, 3, 8, dtype="e4m3", block=4)
+    cache.scales.bytes().view(torch.float32).fill_(0.25)
+    cache.extend(R.i32([32, 80, 10]), 1)  # 2, 5 and 1 of 8 pages
+    assert cache.status.tolist() == [ea.PAGES_OK, 0]
+    decode, one, pos = LlamaBlockDecode(share, cache, 3), R.i32([1, 1, 1]), R.i32([32, 80, 10])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        slots, _ = cache.extend(one, 3)
+        decode.step(slots, pos)
+    _set(decode.x, tokens(3))
+    whole = lambda: [x.bytes().clone() for x in (cache.data, cache.scales)]
+    was, lens = whole(), cache.lengths.tolist()
+    for run in (lambda: decode.step(cache.extend(one, 3)[0], pos), graph.replay):
+        run()
+        assert cache.status.tolist()[0] == ea.PAGES_NONE_FREE and cache.lengths.tolist() == lens
+        assert all(torch.equal(a, b) for a, b in zip(was, whole()))
+    rows = [ea.Relation((3, HEADS_KV * 128), "bf16", ea.whole_partition((3, HEADS_KV * 128))) for _ in range(2)]
+    cache.read(0, *rows, slots=slots)  # no keys for them either
+    assert not any(R.unblocked(x).any() for x in rows)
+    for bad in (R.i32([0, 0]), slots.float(), slots.cpu()):
+        with pytest.raises(ea.EAError):
+            cache.write(0, *rows, slots=bad)
+    cache.lengths.copy_(R.i32([32, 64, 10]))  # the second sequence gives its last page back
+    cache.refs[cache.table[1, 4]] = 0
+    decode.step(cache.extend(R.i32([0, 0, 1]), 3)[0], pos, q_start=R.i32([0, 0, 0, 1]))
+    assert cache.status.tolist()[0] == ea.PAGES_OK and cache.lengths.tolist() == [32, 64, 11]
+    assert not torch.equal(was[0], cache.data.bytes())
+
+
 def test_captured_steps_as_eager_ones():
     """Two decoders over caches in 8 bits, captured and replayed on two streams:
     the bits of eager steps of a third, every replay."""
