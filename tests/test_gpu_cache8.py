@@ -109,6 +109,77 @@ def test_read(case):
         C.same(C.f64(get(r)), want)
 
 
+@pytest.mark.parametrize("major", ["tokens", "heads"])
+@pytest.mark.parametrize("hb,tb", [(2, 7), (3, 1), (1, 64), (5, 6)])
+def test_partitions_of_the_rows(major, hb, tb):
+    """K's rows in blocks of hb of 5 heads and tb rows, the last ones shorter; V's
+    in one block."""
+    news, page, block, hkv, d = [40, 3, 25], 12, 6, 5, 48
+    kv, table, lens, starts, rng = _state([5, 0, 9], news, page, block, hkv, d, "e4m3", 21)
+    t = starts[-1]
+    cut = lambda n, b: list(range(0, n, b)) + [n]
+    lay = lambda x: R.blocked(x.reshape(t, hkv * d), [cut(t, tb), [i * d for i in cut(hkv, hb)]]) if major == "tokens" else \
+        R.blocked(x.transpose(0, 1).contiguous(), [cut(hkv, hb), cut(t, tb), [0, d]])
+    dense = lambda r: R.unblocked(r).view(t, hkv, d) if major == "tokens" else R.unblocked(r).transpose(0, 1)
+    xs = [_rows(rng, t, hkv, d, "bf16") for _ in range(2)]
+    dev = [C.Cache(codes, scale, "e4m3") for codes, scale in kv]
+    batch = dict(k_scale=dev[0].scale_rel, v_scale=dev[1].scale_rel, table=R.i32(table), lengths=R.i32(lens),
+                 q_start=R.i32(starts))
+    ea.pages_write(lay(xs[0]), _laid(xs[1], "tokens")[0], dev[0].rel, dev[1].rel, **batch)
+    for x, (codes, scale), c in zip(xs, kv, dev):
+        C.write(C.f64(x), codes, scale, table, lens, starts, "e4m3")
+        C.same(c.scale.cpu().numpy(), scale)
+        C.same(C.f64(c.get()), codes)
+    outs = [lay(torch.full_like(xs[0], 7.0)), _laid(torch.full_like(xs[1], 7.0), "tokens")]
+    ea.pages_read(dev[0].rel, dev[1].rel, outs[0], outs[1][0], **batch)
+    for (codes, scale), got in zip(kv, (dense(outs[0]), outs[1][1](outs[1][0]))):
+        vals, want = C.values(codes, scale), np.zeros((t, hkv, d))
+        for row, _, at, pg in C.places(table, lens, starts, page, len(codes)):
+            want[row] = vals[pg, :, at % page]
+        C.same(C.f64(got), torch.from_numpy(want).bfloat16().double().numpy())
+
+
+def test_the_most_sequences():
+    """As many sequences as a call takes, of no row to three."""
+    n = ea.PAGED_MAX_SEQ
+    rng = np.random.default_rng(22)
+    olds, news = rng.integers(0, 9, n), rng.integers(0, 4, n)
+    kv, table, lens, starts, rng = _state(list(olds), list(news), 4, 2, 1, 16, "e5m2", 23)
+    xs = [_rows(rng, starts[-1], 1, 16, "f16") for _ in range(2)]
+    dev = _check_write(kv, xs, table, lens, starts, "e5m2")
+    outs = [_laid(torch.zeros_like(xs[0]), "tokens") for _ in range(2)]
+    ea.pages_read(dev[0].rel, dev[1].rel, outs[0][0], outs[1][0], k_scale=dev[0].scale_rel, v_scale=dev[1].scale_rel,
+                  table=R.i32(table), lengths=R.i32(lens), q_start=R.i32(starts))
+    for (codes, scale), (r, get) in zip(kv, outs):
+        vals, want = C.values(codes, scale), np.zeros((starts[-1], 1, 16))
+        for row, _, at, pg in C.places(table, lens, starts, 4, len(codes)):
+            want[row] = vals[pg, :, at % 4]
+        C.same(C.f64(get(r)), torch.from_numpy(want).half().double().numpy())
+
+
+def test_rows_that_do_not_ascend_or_overlap():
+    """First rows that fall back (a sequence without rows, one that has a row twice):
+    as many rows as the call has are written by those whose they are; more are not."""
+    page, block, hkv, d = 4, 4, 2, 32
+    kv, table, lens, _, rng = _state([0, 0, 0], [5, 4, 6], page, block, hkv, d, "e4m3", 24)
+    x = _rows(rng, 12, hkv, d, "bf16")
+    # sequence 0 rows 0-4, sequence 1 none, sequence 2 rows 2-7: 11 of 12
+    dev = [C.Cache(codes, scale, "e4m3") for codes, scale in kv]
+    _write(x, x, *dev, table, lens, [0, 5, 2, 8])
+    for (codes, scale), c in zip(kv, dev):
+        want = [codes.copy(), scale.copy()]
+        C.write(C.f64(x[:5]), *want, table[:1], lens[:1], [0, 5], "e4m3")
+        C.write(C.f64(x[2:8]), *want, table[2:], lens[2:], [0, 6], "e4m3")
+        C.same(c.scale.cpu().numpy(), want[1])
+        C.same(C.f64(c.get()), want[0])
+    # 15 rows of 12: none
+    dev = [C.Cache(codes, scale, "e4m3") for codes, scale in kv]
+    _write(x, x, *dev, table, lens, [0, 9, 2, 8])
+    for (codes, scale), c in zip(kv, dev):
+        C.same(c.scale.cpu().numpy(), scale)
+        C.same(C.f64(c.get()), codes)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("code", ["e4m3", "e5m2"])
 def test_every_value_is_rounded_as_defined(code, dtype):

@@ -98,6 +98,19 @@ def test_paged8(case):
     _check(q, kv, table, lens, starts, groups, code, dtype)
 
 
+@pytest.mark.parametrize("shared", [0, 96])
+@pytest.mark.parametrize("d,code,dtype", [(64, "e4m3", "bf16"), (64, "e5m2", "f16"), (128, "e4m3", "f16"), (128, "e5m2", "bf16")])
+@pytest.mark.parametrize("n_q", [8, 9, 16, 17, 32, 33, 64, 65])
+def test_columns_about_the_tiles(n_q, d, code, dtype, shared):
+    """Twice 8 to 65 columns a sequence: either side of tiles of 16, 32, 64 and 128
+    in both walks, keys that end inside a step and a page."""
+    lens = [shared + n_q + 3, shared + 150, shared + n_q]
+    groups = [(0, 3, shared)] if shared else []
+    kv, table, rng = _batch(lens, groups, 12, 6, 1, d, code, 30 + n_q)
+    q = torch.from_numpy(rng.standard_normal((3 * n_q, 2, d))).to(R.TORCH[dtype]).cuda()
+    _check(q, kv, table, lens, [n_q * i for i in range(4)], groups, code, dtype)
+
+
 @pytest.mark.parametrize("code,dtype", [("e4m3", "bf16"), ("e5m2", "f16")])
 def test_ragged_query_rows_and_rows_behind(code, dtype):
     """0, 1, 7 and 40 newest tokens a sequence; rows behind the last sequence
