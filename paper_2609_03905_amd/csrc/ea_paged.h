@@ -74,7 +74,9 @@ __device__ __forceinline__ int shared_keys(const PagedArgs& a, int g) {
 // The group that sequence s is in, or -1: groups are [group_start[i],
 // group_start[i + 1]), ascending.
 __device__ __forceinline__ int group_of(const PagedArgs& a, int s) {
-  if (a.n_group == 0 || s < a.group_start[0] || s >= a.group_start[a.n_group]) return -1;
+  if (a.n_group == 0) return -1;
+  const int first = a.group_start[0], last = a.group_start[a.n_group];
+  if (s < first || s >= last) return -1;
   int lo = 0, hi = a.n_group;  // group_start[lo] <= s < group_start[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -95,10 +97,12 @@ __device__ __forceinline__ Segment segment(const PagedArgs& a, int i) {
     s.k1 = shared_keys(a, i);
     s.seq = min(s0, a.n_seq - 1);
   } else {
-    const int seq = i - a.n_group, g = group_of(a, seq);
+    // (loads that wait for none of the others first, so that they are one round trip)
+    const int seq = i - a.n_group, len = a.len[seq];
     s.r0 = first_row(a, seq);
     s.r1 = max(first_row(a, seq + 1), s.r0);
-    s.k1 = clampi(a.len[seq], 0, a.stride * a.page_size);
+    const int g = group_of(a, seq);
+    s.k1 = clampi(len, 0, a.stride * a.page_size);
     s.k0 = g >= 0 ? min(shared_keys(a, g), s.k1) : 0;
     s.seq = seq;
   }
@@ -116,15 +120,19 @@ struct Seg {
 
 __device__ __forceinline__ int add_most(int a, int b) { return (int)min((int64_t)a + b, (int64_t)0x7fffffff); }
 
-// Inclusive sums over a wave's lanes, no larger than 2^31 - 1.
-__device__ __forceinline__ int wave_scan(int v) {
+// Inclusive sums over a wave's lanes, no larger than 2^31 - 1, of N values side by
+// side: one's shuffles are on their way with the others'.
+template <int N>
+__device__ __forceinline__ void wave_scan(int (&v)[N]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) {
-    const int u = __shfl_up(v, o);
-    if (lane >= o) v = add_most(v, u);
+    int u[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) u[k] = __shfl_up(v[k], o);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = lane >= o ? add_most(v[k], u[k]) : v[k];
   }
-  return v;
 }
 
 __device__ __forceinline__ int steps_of(int k0, int k1, int keys) {
@@ -171,14 +179,16 @@ __device__ __forceinline__ void schedule(const PagedArgs& a, const PagedPass& ow
   }
   int sum[N];
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    sum[k] = wave_scan(mine[k]);
-    if (lane == 63) s_wave[wid][k] = sum[k];
-  }
-  __syncthreads();
+  for (int k = 0; k < N; ++k) sum[k] = mine[k];
+  wave_scan(sum);
 #pragma unroll
   for (int k = 0; k < N; ++k)
-    for (int w = 0; w < wid; ++w) sum[k] = add_most(sum[k], s_wave[w][k]);
+    if (lane == 63) s_wave[wid][k] = sum[k];
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves - 1; ++w)
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum[k] = add_most(sum[k], w < wid ? s_wave[w][k] : 0);
   if (tid == kThreads - 1) {
     seg_o[own.n].step = sum[0];
     seg_o[own.n].tile = sum[1];
