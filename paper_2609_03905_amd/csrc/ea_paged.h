@@ -76,7 +76,7 @@ __device__ __forceinline__ int shared_keys(const PagedArgs& a, int g) {
 __device__ __forceinline__ int group_of(const PagedArgs& a, int s) {
   if (a.n_group == 0) return -1;
   const int first = a.group_start[0], last = a.group_start[a.n_group];
-  if (s < first || s >= last) return -1;
+  if ((s < first) | (s >= last)) return -1;
   int lo = 0, hi = a.n_group;  // group_start[lo] <= s < group_start[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -99,9 +99,11 @@ __device__ __forceinline__ Segment segment(const PagedArgs& a, int i) {
   } else {
     // (loads that wait for none of the others first, so that they are one round trip)
     const int seq = i - a.n_group, len = a.len[seq];
-    s.r0 = first_row(a, seq);
-    s.r1 = max(first_row(a, seq + 1), s.r0);
+    int r0 = seq, r1 = seq + 1;
+    if (a.q_start) r0 = a.q_start[seq], r1 = a.q_start[seq + 1];
     const int g = group_of(a, seq);
+    s.r0 = clampi(r0, 0, a.rows);
+    s.r1 = max(clampi(r1, 0, a.rows), s.r0);
     s.k1 = clampi(len, 0, a.stride * a.page_size);
     s.k0 = g >= 0 ? min(shared_keys(a, g), s.k1) : 0;
     s.seq = seq;
