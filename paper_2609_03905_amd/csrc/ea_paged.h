@@ -55,13 +55,8 @@ __device__ __forceinline__ int xcd_part(int b, int n) {
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
-// First query row of sequence s (0 <= s <= n_seq).
-__device__ __forceinline__ int first_row(const PagedArgs& a, int s) {
-  return a.q_start ? clampi(a.q_start[s], 0, a.rows) : min(s, a.rows);
-}
-
 struct Segment {
-  int r0, r1;  // query rows
+  int r0, r1;  // query rows (of sequence s: q_start[s] to q_start[s + 1], or s)
   int k0, k1;  // keys
   int seq;     // whose table row lists the pages
 };
@@ -90,11 +85,14 @@ __device__ __forceinline__ int group_of(const PagedArgs& a, int s) {
 __device__ __forceinline__ Segment segment(const PagedArgs& a, int i) {
   Segment s;
   if (i < a.n_group) {
-    const int s0 = clampi(a.group_start[i], 0, a.n_seq), s1 = clampi(a.group_start[i + 1], s0, a.n_seq);
-    s.r0 = first_row(a, s0);
-    s.r1 = max(first_row(a, s1), s.r0);
+    const int first = a.group_start[i], last = a.group_start[i + 1], keys = shared_keys(a, i);
+    const int s0 = clampi(first, 0, a.n_seq), s1 = clampi(last, s0, a.n_seq);
+    int r0 = s0, r1 = s1;
+    if (a.q_start) r0 = a.q_start[s0], r1 = a.q_start[s1];
+    s.r0 = clampi(r0, 0, a.rows);
+    s.r1 = max(clampi(r1, 0, a.rows), s.r0);
     s.k0 = 0;
-    s.k1 = shared_keys(a, i);
+    s.k1 = keys;
     s.seq = min(s0, a.n_seq - 1);
   } else {
     // (loads that wait for none of the others first, so that they are one round trip)
@@ -155,8 +153,14 @@ __device__ __forceinline__ void schedule(const PagedArgs& a, const PagedPass& ow
   __shared__ int s_wave[kWaves][N];
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int ng = SHARED ? shared.n : 0, n = ng + own.n;
+  // segments of a thread: the groups first, or, where there are few, by the last
+  // threads, whose loads then wait beside the sequences' and not before them
   const int per = (n + kThreads - 1) / kThreads;
-  const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  int i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  if (SHARED && per == 1) {
+    i0 = tid < own.n ? ng + tid : tid >= kThreads - ng ? tid - (kThreads - ng) : n;
+    i1 = min(n, i0 + 1);
+  }
   int mine[N] = {};
   for (int i = i0; i < i1; ++i) {
     const bool g = SHARED && i < ng;
