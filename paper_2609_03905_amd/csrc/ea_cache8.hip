@@ -250,7 +250,7 @@ __device__ __forceinline__ int schedule_write(const Cache8Args& a, Span* spans) 
 // read twice): 4 and two units at a time, or 16 (f32 8) of one unit for long blocks.
 // Bound by HBM: 65 thousand tokens of 32 sequences, 8 heads of 128, blocks of 16,
 // bf16, in 88 us, 4.6 TB/s (one unit at a time, rows dealt to workgroups by position,
-// 150 us); 8192 tokens of one sequence, blocks of 64, in 13.8 us, 3.6 TB/s, of which
+// 150 us); 8192 tokens of one sequence, blocks of 64, in 14.2 us, 3.5 TB/s, of which
 // 7 are the launch and the first rows' round trips; 64 sequences of one token each
 // are 6.7 us, a chain of three round trips (schedule, table, rows).
 template <int DT, bool E5, int HELD>
@@ -421,10 +421,10 @@ __global__ __launch_bounds__(kThreads) void cache8_write_kernel(const Cache8Args
 
 // ---- reading back -----------------------------------------------------------------
 // Pieces of 8 codes, a thread each and UNROLL in flight; stores are whole lines.
-// Bound by HBM: 196 thousand rows of 48 sequences, 8 heads of 128, to bf16 in 221 us,
+// Bound by HBM: 196 thousand rows of 48 sequences, 8 heads of 128, to bf16 in 220 us,
 // 5.5 TB/s (places looked up by every thread, a row a wave: 268 us; loads guarded by
 // branches, so that they wait one for another: 281).  One sequence of 1000 rows in
-// 6.7 us, a chain of four round trips: first rows, table, codes and scale, store.
+// 7.0 us, a chain of four round trips: first rows, table, codes and scale, store.
 constexpr int kReadRows = 16;
 
 // Where a row lies, in the cache and in the call.

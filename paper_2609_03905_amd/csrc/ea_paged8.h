@@ -104,8 +104,8 @@ struct __attribute__((aligned(1024))) Many8Shared {
 // scores its column's accumulators hold; a byte permutation puts two keys' codes of
 // one d side by side, and widening them gives the operand.  Bound by HBM where there
 // is work for the chip: 48 ragged sequences of up to 8K keys, 4 heads over each of 8,
-// 87.5 us, 4.6 TB/s (a wave's step of 32 keys, its scales as f32 factors: 96); one
-// sequence alone by the chain of its round trips (1000 keys 10.3 us, as over 16 bits).
+// 85.5 us, 4.7 TB/s (a wave's step of 32 keys, its scales as f32 factors: 96); one
+// sequence alone by the chain of its round trips (1000 keys 10.0 us, as over 16 bits).
 // Two waves a SIMD: their registers hold the step's codes.
 template <int D, bool BF, bool E5, int COLS>
 __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& ps, const Seg* seg, Few8Shared<D>& sh,
@@ -407,7 +407,7 @@ __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& p
 // thread that fetched them (a wave's column tiles share the work), one step ahead
 // of the products; tiles and products as for a cache in 16 bits.  Bound by the
 // vector instructions and products of a step, about half and a third of its clocks:
-// 32 sequences that share 64K keys, 4 heads over each of 8, 94 us (over 16 bits 98),
+// 32 sequences that share 64K keys, 4 heads over each of 8, 92 us (over 16 bits 96),
 // whose bytes are twice as many (scales as f32 factors 107).  Without a gain: widening
 // between the products of the step before (102), weights of sixteen keys computed
 // under the products of the sixteen before (98; one product and six instructions in
