@@ -302,6 +302,17 @@ def test_the_most_sequences():
     _check(q, kv, table, lens, None, [], "e4m3", "bf16")
 
 
+def test_the_most_sequences_of_many_columns():
+    """The same beside the buffers of the walk over many columns: 40 heads over one."""
+    n, page, hq, d = ea.PAGED_MAX_SEQ, 4, 40, 64
+    rng = np.random.default_rng(16)
+    lens = [int(x) for x in rng.integers(0, 9, n)]
+    kv, table, rng = _batch(lens, [], page, 4, 1, d, "e5m2", 17)
+    q = torch.from_numpy(rng.standard_normal((n, hq, d))).to(torch.float16).cuda()
+    _check(q, kv, table, lens, None, [], "e5m2", "f16")
+    _check(q, kv, table[:-1], lens[:-1], [0] * n, [], "e5m2", "f16")  # and none with a row
+
+
 @pytest.mark.parametrize("lens", [[4000], [4090, 1], [4200], [2000, 3900, 0, 300]])
 def test_walks_joined_by_their_last_part(lens):
     """Table rows about as long as those whose parts the last one joins; the same
