@@ -195,7 +195,18 @@ def _held(x, block, code):
     cut = x.view(pages, heads, page // block, block, d)
     scale = _scale(cut.abs().amax((3, 4)), code)
     codes = (cut / scale[..., None, None]).to(TORCH[code]).view(pages, heads, page, d)
-    return codes, scale
+    return _apart(codes), scale
+
+
+def _apart(codes):
+    """The codes with pages that start at multiples of 256 bytes, as a relation's
+    blocks do (a view, where a page is no such multiple)."""
+    n = codes[0].numel()
+    if n % 256 == 0:
+        return codes
+    whole = torch.zeros((len(codes), -(-n // 256) * 256), dtype=torch.uint8, device=codes.device)
+    whole[:, :n] = _bytes(codes).view(len(codes), n)
+    return whole.view(codes.dtype)[:, :n].view(codes.shape)
 
 
 def prepare(case, seed):
@@ -252,8 +263,9 @@ def _handles(s, case):
     def whole(t):
         return ea.Relation(t.shape, names[t.dtype], ea.whole_partition(t.shape), data=t)
 
-    def pages(t):  # one block per page
-        return ea.Relation(t.shape, names[t.dtype], [range(t.shape[0] + 1)] + ea.whole_partition(t.shape[1:]), data=t)
+    def pages(t):  # one block per page, over the memory from the first one's to the last one's end
+        part = [range(t.shape[0] + 1)] + ea.whole_partition(t.shape[1:])
+        return ea.Relation(t.shape, names[t.dtype], part, data=t.as_strided((len(t) * t.stride(0),), (1,)))
 
     rows = ("q", "out") if case["kind"] == "attention" else ("xk", "xv")
     s["rel"] = {x: whole(s[x]) for x in rows + ("k_scale", "v_scale")} | {x: pages(s[x]) for x in ("k", "v")}
