@@ -7,7 +7,7 @@
 //   a = max |x| over the finite ones,   e = the least whole number with a <= M 2^e
 // (M the largest code, 448 or 57344; e in [-120, 120]), and the block's scale is
 // 2^e, or the one it has if that is larger and the block holds rows of earlier
-// calls; where the scale grows, their codes become round(c s_old / s).  Then
+// calls; where the scale is another one then, their codes become round(c s_old / s).  Then
 // c = round(x / s).  Scales being powers of two, both quotients are exact in 32
 // bits, so that a code is off by its own rounding alone, and one that is rounded
 // again changes only where it falls below the code's normal range.
@@ -348,9 +348,11 @@ __global__ __launch_bounds__(kThreads) void cache8_write_kernel(const Cache8Args
     }
     int e = least_exponent<E5>(wave_max(top));
     if (old > 0.0f && old < INFINITY) {
-      // (a scale that another program left may be no power of two: the next one)
+      // (a scale that another program left may be no power of two: the next one; or
+      // past 2^120, which then holds whatever the codes stood for: a 32-bit number's
+      // code is below 256 under it)
       const int bits = __float_as_int(old);
-      e = max(e, min(max((bits >> 23) - 127 + ((bits & 0x7fffff) != 0), -kScaleExp), 126));
+      e = max(e, min(max((bits >> 23) - 127 + ((bits & 0x7fffff) != 0), -kScaleExp), kScaleExp));
       const float ratio = old * power(-e);
       if (ratio != 1.0f)
 #pragma unroll 1

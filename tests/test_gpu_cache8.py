@@ -342,3 +342,24 @@ def test_captured_writes_follow_lengths_on_their_stream():
             vals = C.values(codes, scale)
             want = np.stack([vals[table[s][(lens[s] - 1) // page], :, (lens[s] - 1) % page] for s in range(3)])
             C.same(C.f64(get(r)), torch.from_numpy(want).bfloat16().double().numpy())
+
+
+@pytest.mark.parametrize("code", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("old", [np.nan, np.inf, -np.inf, -1.0, 0.0, 2.0 ** -149, 2.0 ** -130, 1.5 * 2.0 ** -121,
+                                 2.0 ** 120, 2.0 ** 121, 1.5 * 2.0 ** 121, 2.0 ** 126, 2.0 ** 127, 1.75 * 2.0 ** 127])
+def test_scales_that_another_program_left(code, old):
+    """Blocks that go on under any scale: one that is no positive number counts as
+    none, one that is no power of two as the next, one past 2^120 as 2^120, and the
+    codes before stand for what they stood for (they are at most 1: 224 under the
+    largest)."""
+    kv, table, lens, starts, rng = _state([5, 8], [2, 3], 8, 4, 2, 32, code, 31)
+    for i, (codes, scale) in enumerate(kv):
+        kv[i] = (C.rounded(codes / 2 ** 18 if code == "e5m2" else codes / 512, code), np.full(scale.shape, old))
+        assert np.abs(kv[i][0]).max() <= 1
+    before = C.values(kv[0][0], kv[0][1]) if 2.0 ** 120 <= old < np.inf else None
+    xs = [_rows(rng, starts[-1], 2, 32, "f32") for _ in range(2)]
+    dev = _check_write(kv, xs, table, lens, starts, code)
+    assert (dev[0].scale[table[0, 0], :, 1] <= 2.0 ** 120).all()
+    if before is not None and np.log2(old) % 1 == 0:  # nothing is lost: the same values, exactly
+        now = C.values(C.f64(dev[0].get()), dev[0].scale.double().cpu().numpy())
+        C.same(now[table[0, 0], :, 4], before[table[0, 0], :, 4])
