@@ -143,12 +143,13 @@ __device__ __forceinline__ int least_exponent(float a) {
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 
 // c f, where it is no 32-bit number the neighbour whose last bit is set, so that
-// rounding it to a code (of far fewer bits) is one rounding of the product.
+// rounding it to fewer bits is one rounding of the product (28 bits: exact in 64).
 __device__ __forceinline__ float product_to_odd(float c, float f) {
-  const float p = c * f, rest = fmaf(c, f, -p);
+  const double exact = (double)c * (double)f;
+  const float p = (float)exact;
   const int bits = __float_as_int(p);
-  if (rest == 0.0f || !(fabsf(p) < INFINITY) || (bits & 1)) return p;
-  return __int_as_float(bits + ((rest > 0.0f) == (p > 0.0f) ? 1 : -1));
+  if ((double)p == exact || !(fabsf(p) < INFINITY) || (bits & 1)) return p;
+  return __int_as_float(bits + (fabs(exact) > fabs((double)p) ? 1 : -1));
 }
 
 __device__ __forceinline__ int first_row(const Cache8Args& a, int s) { return min(max(a.q_start[s], 0), a.rows); }
@@ -491,8 +492,15 @@ __global__ __launch_bounds__(kThreads) void cache8_read_kernel(const Cache8Args 
         float y[8];
         decode4<E5>(c[k].x, y);
         decode4<E5>(c[k].y, y + 4);
+        // (the product with a power of two is exact; another's is rounded once, as
+        // the output)
+        if (DT != EA_F32 && __builtin_expect((__float_as_uint(f[k]) & 0x7fffffu) != 0, 0)) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] *= f[k];
+          for (int j = 0; j < 8; ++j) y[j] = product_to_odd(y[j], f[k]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] *= f[k];
+        }
         if constexpr (DT == EA_F32) {
 #pragma unroll
           for (int j = 0; j < 2; ++j)

@@ -363,3 +363,42 @@ def test_scales_that_another_program_left(code, old):
     if before is not None and np.log2(old) % 1 == 0:  # nothing is lost: the same values, exactly
         now = C.values(C.f64(dev[0].get()), dev[0].scale.double().cpu().numpy())
         C.same(now[table[0, 0], :, 4], before[table[0, 0], :, 4])
+
+
+def _once(y, bits, least):
+    """y to the nearest number of `bits` significant bits, ties to even; the least
+    step is 2^least."""
+    step = 2.0 ** np.maximum(np.frexp(y)[1] - bits, least)
+    return np.round(y / step) * step
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("code", ["e4m3", "e5m2"])
+def test_values_are_rounded_once_under_any_scale(code, dtype):
+    """Scales that are no powers of two: code times scale just beside a tie of the
+    output's type, nearer than 32 bits tell, and among its subnormal numbers."""
+    bits, least = {"bf16": (8, -133), "f16": (11, -24)}[dtype]
+    parts = 2 ** C.FORM[code][0]
+    pairs = []
+    for c in [1 + i / parts for i in range(1, parts)]:
+        for i in range(0, 2 ** (bits - 1), 1 if bits == 8 else 8):
+            pairs.append((c, np.float32((1 + (2 * i + 1) * 2.0 ** -bits) / c)))
+    normal = len(pairs)
+    for i in range(64):
+        pairs.append((pairs[i][0], np.float32((1 + i / 64) * 2.0 ** (least + 1 - i % 4))))
+    n, d = len(pairs), 16
+    kv, table, lens, starts, _ = _state([0], [n], 8, 1, 1, d, code, 32)
+    for codes, scale in kv:
+        for r, (c, s) in enumerate(pairs):
+            codes[table[0, r // 8], 0, r % 8] = c * np.where(np.arange(d) % 2, -1, 1)
+            scale[table[0, r // 8], 0, r % 8] = s
+    y = np.array([c * np.float64(s) for c, s in pairs])  # exact: 28 bits
+    want = _once(y, bits, least)
+    twice = _once(y.astype(np.float32).astype(np.float64), bits, least)
+    assert (want != twice)[:normal].sum() > normal // 8  # what the test is about
+    dev = [C.Cache(codes, scale, code) for codes, scale in kv]
+    outs = [_laid(torch.zeros((n, 1, d), device="cuda").to(R.TORCH[dtype]), "tokens") for _ in range(2)]
+    ea.pages_read(dev[0].rel, dev[1].rel, outs[0][0], outs[1][0], k_scale=dev[0].scale_rel, v_scale=dev[1].scale_rel,
+                  table=R.i32(table), lengths=R.i32(lens), q_start=R.i32(starts))
+    for r, get in outs:
+        C.same(C.f64(get(r))[:, 0], want[:, None] * np.where(np.arange(d) % 2, -1, 1))
