@@ -254,3 +254,49 @@ def test_captured_steps_as_eager_ones():
             for a, b in zip(d.cache.k + d.cache.v + d.cache.k_scale + d.cache.v_scale,
                             e.cache.k + e.cache.v + e.cache.k_scale + e.cache.v_scale):
                 assert torch.equal(a.bytes(), b.bytes())
+
+
+@pytest.mark.parametrize("code,page,block", [("e4m3", 16, 8), ("e5m2", 20, None), ("e4m3", 20, 5)])
+def test_a_forked_prompt_holds_what_it_held(code, page, block):
+    """Continuations forked off a prompt, reordered and compacted on the way: the
+    codes and scales of every sequence's prompt, in blocks that no later token goes
+    to, are those of before, in the layer that is written and in the other one."""
+    w, tokens = _weights(9)
+    prefill = _share(PROMPT, w, tokens(PROMPT))
+    prefill.forward()
+    n, layer = 4, 1
+    cache = KVCache(2, 64, HEADS_KV, page, 128, n, 20, dtype=code, block=block)
+    g = torch.Generator(device="cuda").manual_seed(10)
+    cache.data.bytes().copy_(torch.randint(0, 112, cache.data.bytes().shape, generator=g, device="cuda"))
+    cache.scales.bytes().view(torch.int32).copy_(
+        torch.randint(100, 140, (cache.scales.nbytes // 4,), generator=g, device="cuda") << 23)
+    cache.extend(R.i32([0, 0, 6 * page, 0]), 1)  # of a sequence that goes: holes for compact to fill
+    cache.extend(R.i32([PROMPT, 0, 0, 0]), PROMPT)
+    prefill.store(cache, None, layer, q_start=R.i32([0] + [PROMPT] * n))
+    b = block or page
+    whole = torch.arange(PROMPT // b * b, device="cuda")
+
+    def prompt(s):
+        out = []
+        for rel, scale in zip(cache.k + cache.v, cache.k_scale + cache.v_scale):
+            pg = cache.table[s][whole // page].long()
+            z = scale.bytes().view(torch.float32).view(scale.shape)
+            out += [_codes(rel).view(torch.uint8)[pg, :, whole % page], z[pg, :, whole % page // b]]
+        return out
+
+    held = prompt(0)
+    cache.select(R.i32([0, 0, -1, 0]))
+    decode = LlamaBlockDecode(prefill, cache, 3, layer)
+    shared = PROMPT // page * page
+    batch = dict(q_start=R.i32([0, 1, 2, 2, 3]), group_start=R.i32([0, 2, 3, 4]), group_shared=R.i32([shared, 0, 0]))
+    for i in range(12):
+        if i == 5:
+            cache.select(R.i32([3, 1, -1, 0]))
+            table = cache.table.clone()
+            cache.compact()
+            assert not torch.equal(table, cache.table)
+        slots, po = cache.extend(R.i32([1, 1, 0, 1]), 3)
+        _set(decode.x, tokens(3))
+        decode.step(slots, po, **batch)
+        for s in (0, 1, 3):
+            assert all(torch.equal(x, y) for x, y in zip(prompt(s), held)), (i, s)
