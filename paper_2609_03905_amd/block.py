@@ -138,9 +138,11 @@ class LlamaBlockShare:
     def store(self, cache: KVCache, slots: torch.Tensor | None, layer: int = 0, q_start: torch.Tensor | None = None):
         """The last forward's keys and values to the cache: token t to slot
         slots[t] (queries are written again, as they are).  A cache in 8 bits takes
-        tokens q_start[s] .. q_start[s + 1] - 1 as the newest of its sequence s
-        (None: token s); slots, if given, say whether they have places."""
+        tokens q_start[s] .. q_start[s + 1] - 1 as the newest of its sequence s, and
+        needs to be told so: its slots (or None) say only whether they have places."""
         if cache.scales is not None:
+            if q_start is None:
+                raise ea.EAError(ea.ERR_ARG, "a cache in 8 bits is stored to by sequence: no q_start")
             cache.write(layer, self.k, self.v, q_start, slots)
             return
         ea.heads(self.qkv, self.q, cache.k[layer], cache.v[layer], slots=slots, **self.head_options(self.positions))

@@ -64,7 +64,8 @@ class KVCache:
               slots: torch.Tensor | None = None):
         """Rows q_start[s] .. q_start[s + 1] - 1 (None: row s) of keys and values
         quantised into the newest places of sequence s (8 bits: ea.pages_write);
-        with the slots that extend gave, none where it was not served."""
+        with the slots that extend gave, none where it was not served.  Rows behind
+        the last sequence's (a padded batch) go nowhere."""
         ea.pages_write(xk, xv, self.k[layer], self.v[layer], **self._rows(layer, q_start, slots))
 
     def read(self, layer: int, xk: ea.Relation, xv: ea.Relation, q_start: torch.Tensor | None = None,

@@ -248,3 +248,19 @@ def test_kv_cache_refuses():
     with pytest.raises(E.EAError):  # one list entry a cache
         E.pages_select([c.data], c.lengths, c.table, c.lengths, c.refs, out_table=c.table, out_lengths=c.lengths,
                        out_refs=c.refs, status=c.status, scales=[])
+
+
+def test_store_to_eight_bits_needs_the_sequences():
+    """Slots place every token of a prompt in a cache in 16 bits; in 8 bits they
+    place none: without q_start it would be a token a sequence."""
+    from paper_2609_03905_amd.block import LlamaBlockShare
+    from paper_2609_03905_amd.cache import KVCache
+
+    share = LlamaBlockShare(8, 256, 2, 128, 256, device="meta")
+    slots = torch.zeros(8, dtype=torch.int32)
+    for sequences in (2, 8):  # fewer than the tokens, and as many
+        cache = KVCache(1, 4, 2, 16, 128, sequences, 2, dtype="e4m3", device="meta")
+        for given in (slots, None):
+            with pytest.raises(E.EAError, match="q_start") as e:
+                share.store(cache, given)
+            assert e.value.code == ARG
