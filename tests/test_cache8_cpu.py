@@ -264,3 +264,14 @@ def test_store_to_eight_bits_needs_the_sequences():
             with pytest.raises(E.EAError, match="q_start") as e:
                 share.store(cache, given)
             assert e.value.code == ARG
+
+
+def test_steps_are_counted_as_they_are_walked():
+    """2500 tiles over table rows of 160 million keys: 2^31 steps of 128 keys and
+    more, but not of 256, as the walk over codes takes them.  (What is refused then
+    is the workspace, which is looked at after the steps.)"""
+    q, out = fake([1000, 1024]), fake([8, 1000, 128])
+    for keys, want in ((160_000_000, CAPACITY), (230_000_000, UNSUPPORTED)):
+        assert paged8(q=q, out=out, n_seq=1000, stride=keys // 16, n=4096) == want, ea.lib().ea_last_error()
+    sixteen = dict(k=cache(30, 2, 16, 128), v=cache(30, 2, 16, 128))
+    assert paged(q=q, out=out, n_seq=1000, stride=10_000_000, n=4096, **sixteen) == UNSUPPORTED
