@@ -59,18 +59,19 @@ __device__ __forceinline__ void copy_range(const RepTask* __restrict__ tp, const
   const RepTask& t = *tp;  // fields read from global memory, never copied to the stack
   const char* s0 = src + t.src_off;
   char* d0 = dst + t.dst_off;
-  const int32_t end = t.end;
+  const int32_t begin = t.begin, n = t.end - begin;
   // UNROLL loads in flight per thread, then their stores.  A vector past the
   // range is redirected to the range's first vector: it loads that vector and
   // stores it to its own destination again (the same bytes that lane 0
   // writes), so neither loads nor stores carry a condition and all the loads
-  // are issued before the first store.
-  for (int32_t L0 = t.begin + threadIdx.x * VEC; L0 < end; L0 += kThreads * VEC * UNROLL) {
+  // are issued before the first store.  Counted from the range's begin: a box
+  // may end at byte 2^31 - 1, and what lies behind has no 31-bit offset.
+  for (int32_t r0 = threadIdx.x * VEC; r0 < n; r0 += kThreads * VEC * UNROLL) {
     int64_t sos[UNROLL], dofs[UNROLL];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-      const int32_t L = L0 + u * kThreads * VEC;
-      box_offsets(t, L < end ? L : t.begin, sos[u], dofs[u]);
+      const int32_t r = r0 + u * kThreads * VEC;
+      box_offsets(t, begin + (r < n ? r : 0), sos[u], dofs[u]);
     }
     T v[UNROLL];
 #pragma unroll
