@@ -586,9 +586,12 @@ int ea_pages_read(const ea_relation* k, const ea_relation* v, const ea_relation*
 /* ea_attention_paged over such a cache, of keys and values code * scale.  Scales
    are powers of two, as ea_pages_write gives them; any other stands for NaN.
    q and out are bf16 or f16; the weights' products with V take them as two bf16
-   values.  Sums are in 32 bits: values of 2^112 and more may come out as
-   infinities or NaN in the rows that see them.  Everything else, the workspace
-   and its size's call among it, is as there. */
+   values.  Sums are in 32 bits, of weights of up to 2^8 (the running maximum
+   moves in steps of more): a row that sees a scale of V above 2^119, or whose
+   largest |value| times its keys is 2^119 or more, may come out as infinities or
+   NaN.  Values and weights times scales are bf16's there, of 2^-133 and more: an
+   output may be off by 2^-134 times the largest code for every key.  Everything
+   else, the workspace and its size's call among it, is as there. */
 int ea_attention_paged8(const ea_relation* q, const ea_relation* k, const ea_relation* v, const ea_relation* k_scale,
                         const ea_relation* v_scale, ea_relation* out, const ea_paged* batch, void* workspace,
                         int64_t ws_bytes, void* stream);

@@ -394,3 +394,53 @@ def test_captured_calls_follow_lengths_with_workspaces_of_their_own():
             call(s, want, ea.new_workspace(s[5].numel()))
             assert torch.equal(s[2], want) and want.isfinite().all()
             assert not s[5][:ea.WS_COUNTER_BYTES].any()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("walk", ["few", "many", "both"])
+@pytest.mark.parametrize("keys,scale,top", [(6000, 97, 448.0), (400, 119, 2.0 ** -9)])
+def test_large_values_of_many_keys(keys, scale, top, walk, code):
+    """V of one sign under a scale of up to 2^119, the largest value times the keys
+    just under 2^119, and later keys whose weights are 2^7.2 of the first ones': all
+    finite, as in 64 bits."""
+    n_q, d, page = {"few": 1, "many": 20, "both": 1}[walk], 64, 16
+    lens = [keys, keys - 1]
+    groups = [(0, 2, keys // 2 // page * page)] if walk == "both" else []
+    kv, table, rng = _batch(lens, groups, page, 1, 1, d, code, 40)
+    (kc, ks), (vc, vs) = kv
+    kc[...], ks[...], vs[...] = 0, 1, 2.0 ** scale
+    vc[...] = C.rounded(rng.uniform(top / 2, top, vc.shape), code) if top > 1 else top
+    assert vc.max() * 2.0 ** scale * keys < 2.0 ** 119
+    for s, n in enumerate(lens):
+        for j in range(256, n):
+            kc[table[s, j // page], 0, j % page, 0] = 5
+    q = torch.zeros(2 * n_q, 4, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1
+    got = _check(q, kv, table, lens, [n_q * i for i in range(3)], groups, code, "bf16", scale=1.0)
+    assert got.isfinite().all()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("walk", ["few", "many", "both"])
+@pytest.mark.parametrize("scale", [-120, -112])
+def test_small_values_of_many_keys(scale, walk, code):
+    """V under the smallest scales, most keys of weights of 2^-7.2: off by half of
+    bf16's smallest number (2^-134) times a code for every key, and in the store by
+    as much."""
+    keys, n_q, d, page = 700, {"few": 1, "many": 20, "both": 1}[walk], 64, 16
+    lens = [keys, keys - 1]
+    groups = [(0, 2, 320)] if walk == "both" else []
+    kv, table, rng = _batch(lens, groups, page, 1, 1, d, code, 41)
+    (kc, ks), (vc, vs) = kv
+    kc[...], ks[...], vs[...] = 0, 1, 2.0 ** scale
+    vc[...] = C.rounded(rng.uniform(-C.TOP[code], C.TOP[code], vc.shape) * 2.0 ** -rng.integers(0, 20, vc.shape), code)
+    for s in range(2):
+        for j in range(0, 300, 7):
+            kc[table[s, j // page], 0, j % page, 0] = 5
+    q = torch.zeros(2 * n_q, 4, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1
+    starts = [n_q * i for i in range(3)]
+    dev = [C.Cache(codes, s, code) for codes, s in kv]
+    got = _run(q, dev, table, lens, starts, groups, 1.0)
+    ref, info = R.attention(R.f64(q), C.values(*kv[0]), C.values(*kv[1]), table, lens, page, starts, 1.0)
+    R.check(R.f64(got), ref, C.attention_tol(ref, info, "bf16", d) + 2.0 ** -134 * (1 + keys * C.TOP[code]))
