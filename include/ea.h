@@ -566,9 +566,11 @@ typedef struct ea_page_rows {
    key (more rows than keys, or its slots say so), is not written.  Of scales that
    another program left, one that is no positive number counts as none, and one
    that is no power of two of that range as the next one in it, under which the
-   codes before are rounded again (past 2^120: as 2^120).  Pages that several
-   sequences share, or a block's rows given twice, must not be among those
-   written.
+   codes before are rounded again (past 2^120: as 2^120).  What a block holds
+   so depends on all that was written to it since it was begun: a row that was
+   taken back (a draft not accepted) may leave a larger scale, and codes that were
+   rounded again under it.  Pages that several sequences share, or a block's rows
+   given twice, must not be among those written.
    xk, xv: [T, Hkv d], or [.., Hkv, T, d] (forms and partitions as ea_heads' q),
    f32, bf16 or f16; d a multiple of 16 from 16 to 512; Hkv d < 2^26,
    Hkv T < 2^30, (stride + 1) * page_size < 2^31 - 1024, n_seq <=

@@ -361,6 +361,11 @@ int plan_paged(const ea_relation* q, const ea_relation* k, const ea_paged* b, bo
   // Over codes, in steps of 256 keys, 16 (one sequence, 32 heads over 8: 2000 keys
   // 11.0 us and 12.5 with the launch, 4000 keys 12.6 and 13.1, 6000 keys 15.4 and
   // 14.1; 4 over 1 11.8 and 13.3 at 4000 keys, 12.9 and 13.3 at 6000).
+  // These figures are of tables as wide as the longest sequence.  Lengths are on
+  // the device: the rule sees a row's width alone, and a short sequence in a wide
+  // table takes the launch (1000 keys in a table of 32K: 10.6 us instead of 9.4 over
+  // 16 bits, 12.1 instead of 10.0 over codes; 2000 keys over codes 12.1 instead of
+  // 10.5, over 16 bits 10.7 either way).
   const bool codes = is_code(k->dtype);
   const int64_t keys = codes ? kPaged8Step : kPagedStep, steps = (b->stride * k->shape[2] + keys - 1) / keys;
   p->own.fused = b->n_group == 0 && p->own.cols <= 32 && p->own.tiles <= kWsCounterBytes / 4 &&

@@ -4,11 +4,13 @@
 //   s_j = scale log2(e) k_j q.ck_j
 // Codes are widened on their way to the matrix cores, K's to q's type, V's to bf16.
 // A scale is a power of two, and a code has at most four significant bits: c s is
-// exact in bf16, so that there the widening instruction applies the scale.  Where
-// it does not, the scales enter in f32: k_j a score (fp16 queries), v_j a weight
-// (the walk over few columns, which widens the codes of two keys at once).  The
-// weights, whose exponents may be as far apart as f32's, go to the product with V
-// as two bf16 values.
+// exact in bf16 from 2^-133 to below 2^128, so that there the widening instruction
+// applies the scale.  (e5m2's least codes are below under scales of 2^-118 and less,
+// codes of 2^8 and more above under 2^120: V's are taken out, see below.)  Where it
+// does not, the scales enter in f32: k_j a score (fp16 queries), v_j a weight (the
+// walk over few columns, which widens the codes of two keys at once).  The weights,
+// whose exponents may be as far apart as f32's, go to the product with V as two bf16
+// values.
 #pragma once
 
 #include "ea_paged.h"
@@ -21,8 +23,9 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
 // Two codes of a word, the lower or the upper, times a power of two, as two values
 // of a type.  (The instruction takes the scale's exponent alone; NaN gives NaN.
-// Every code times every power from 2^-120 to 2^120 was compared: exact, bf16's
-// subnormal numbers among them, which the matrix cores take as they are.)
+// Every code times every power from 2^-120 to 2^120 was compared: exact where bf16
+// has the number, its subnormal ones among them, which the matrix cores take as they
+// are; below them rounded, above them an infinity.)
 template <bool BF, bool E5, bool UP>
 __device__ __forceinline__ uint32_t widen2(uint32_t w, float s) {
   if constexpr (BF && E5) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, UP));
@@ -105,7 +108,7 @@ struct __attribute__((aligned(1024))) Many8Shared {
 // one d side by side, and widening them gives the operand.  Bound by HBM where there
 // is work for the chip: 48 ragged sequences of up to 8K keys, 4 heads over each of 8,
 // 85.5 us, 4.7 TB/s (a wave's step of 32 keys, its scales as f32 factors: 96); one
-// sequence alone by the chain of its round trips (1000 keys 10.0 us, as over 16 bits).
+// sequence alone by the chain of its round trips (1000 keys 10.0 us, over 16 bits 9.4).
 // Two waves a SIMD: their registers hold the step's codes.
 template <int D, bool BF, bool E5, int COLS>
 __device__ __forceinline__ void walk_few8(const PagedArgs& a, const PagedPass& ps, const Seg* seg, Few8Shared<D>& sh,
