@@ -275,3 +275,22 @@ def test_steps_are_counted_as_they_are_walked():
         assert paged8(q=q, out=out, n_seq=1000, stride=keys // 16, n=4096) == want, ea.lib().ea_last_error()
     sixteen = dict(k=cache(30, 2, 16, 128), v=cache(30, 2, 16, 128))
     assert paged(q=q, out=out, n_seq=1000, stride=10_000_000, n=4096, **sixteen) == UNSUPPORTED
+
+
+def test_drawn_codes_lie_as_page_relations_do():
+    """Every page size that the measured cases draw: pages at multiples of 256 bytes,
+    in no less memory than their relation has."""
+    import random
+
+    from perf import more_operators as M
+
+    rng, odd = random.Random(3), 0
+    cases = {(c["hkv"], c["page"], c["d"], c["code"]) for c in M.listed() + [M.draw(rng) for _ in range(4000)]}
+    for h, page, d, code in cases:
+        n = h * page * d
+        odd += n % 256 != 0
+        codes = torch.randint(0, 100, (3, h, page, d), dtype=torch.uint8).view(C.TORCH[code])
+        x = M._apart(codes)
+        assert torch.equal(x.view(torch.uint8), codes.view(torch.uint8)) and x.stride(0) % 256 == 0
+        assert 3 * x.stride(0) >= ea.layout_nbytes(x.shape, code, [range(4), [0, h], [0, page], [0, d]])
+    assert odd > 1
